@@ -368,6 +368,112 @@ spd_status spd_decode_attention_noalloc(const float* q, const void* kv, const in
                                         int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t chunk,
                                         float* out, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Several sequences in one paged cache. A spd_cache describes device memory that the caller owns: the pools of
+ * n_layers layers in the layout of spd_decode_attention, a page table, and for every sequence its number of keys.
+ * Sequence s holds the pages of entries 0 .. ceil(lens[s] / 16) - 1 of its row of the table; several sequences may
+ * hold a page, refs counts them (0: the page is free). A cache starts with refs and lens of zeros and a table of -1.
+ * The state lives on the device and every call is asynchronous on its stream (a hipStream_t), so calls on one cache
+ * are ordered by their stream, may be captured into a HIP graph, and follow the state on replay. A call's arguments
+ * are checked on the host before anything is launched (SPD_E_INVAL, SPD_E_CAPACITY for a workspace too small,
+ * SPD_E_HIP if the launch fails; spd_last_error(NULL) has the message). What only the device knows is kept in
+ * bounds there: a length counts as at most 16 * max_pages and at least 0, a page id outside [0, num_pages) is read as
+ * page 0 and never written to, and a sequence index outside [0, max_seqs) has no rows.
+ * The workspaces of calls that may run at the same time must differ. */
+typedef struct spd_cache {
+  void* kv;              /* device, [n_layers][num_pages][K, V][n_kv_heads][16 keys][head_dim], 16-byte aligned */
+  int32_t* page_table;   /* device [max_seqs][max_pages] */
+  int32_t* lens;         /* device [max_seqs] */
+  int32_t* refs;         /* device [num_pages]; NULL where no call changes the pages */
+  int32_t n_layers;
+  int32_t num_pages;
+  int32_t max_seqs;      /* at most 65536 */
+  int32_t max_pages;     /* of a sequence, at most 2^26 */
+  int32_t n_kv_heads;
+  int32_t head_dim;      /* 64 or 128 */
+  int32_t dtype;         /* spd_dtype */
+} spd_cache;
+
+/* What a call that changes the pages leaves in its device status word; other than DONE, the cache is unchanged. */
+enum {
+  SPD_CACHE_DONE = 0,
+  SPD_CACHE_NO_PAGES = 1,  /* fewer free pages than the call takes */
+  SPD_CACHE_BAD_LEN = 2,   /* a length below 0, past the sequence's keys (fork) or past 16 * max_pages */
+  SPD_CACHE_BAD_SEQ = 3    /* a sequence outside [0, max_seqs), named twice, or (fork) a child that is not empty */
+};
+
+/* Bytes of device workspace the calls below need for n sequences of the cache. Host-only. */
+spd_status spd_cache_workspace(const spd_cache* c, int32_t n, size_t* bytes);
+
+/* Sequence seqs[i] grows by add[i] >= 0 keys (device int32[n] each, 1 <= n <= max_seqs), to be written by
+ * spd_cache_append. Pages are taken in order of i, then of the logical page, the lowest-numbered free ones first. A
+ * sequence that grows and ends inside a page that others hold too (refs > 1 before the call) gets a copy of that page,
+ * of all layers, in its place: the first page it takes. status: device int32. workspace: device, 256-byte aligned. */
+spd_status spd_cache_reserve(const spd_cache* c, const int32_t* seqs, const int32_t* add, int32_t n, int32_t* status,
+                             void* workspace, size_t ws_bytes, void* stream);
+
+/* The empty sequence dst[i] becomes the first keep[i] keys of src[i] (device int32[n] each), sharing its pages. The
+ * sources are read as they were before the call; one may be named several times. */
+spd_status spd_cache_fork(const spd_cache* c, const int32_t* src, const int32_t* dst, const int32_t* keep, int32_t n,
+                          int32_t* status, void* workspace, size_t ws_bytes, void* stream);
+
+/* Sequence seqs[i] keeps its first min(keep[i], lens[seqs[i]]) keys (device int32[n] each; 0: none) and lets go of the pages
+ * behind them; their table entries become -1. A page that no sequence holds any more is free. */
+spd_status spd_cache_truncate(const spd_cache* c, const int32_t* seqs, const int32_t* keep, int32_t n, int32_t* status,
+                              void* workspace, size_t ws_bytes, void* stream);
+
+/* The held pages move to ids 0 .. *live - 1 (live: device int32), in all layers: those with an id of *live or more go,
+ * in order, to the free ids below, in order; the table and refs follow. Workspace as for n = 1. */
+spd_status spd_cache_compact(const spd_cache* c, int32_t* live, void* workspace, size_t ws_bytes, void* stream);
+
+/* A batch's packed rows: sequence seqs[i] (i < nseqs) has rows cu_rows[i] .. cu_rows[i + 1] - 1 (device int32[nseqs]
+ * and int32[nseqs + 1], ascending), which stand for the newest of its lens[seqs[i]] keys: its last row for key
+ * lens - 1. rows (host): the rows the buffers hold; rows from cu_rows[nseqs] on belong to no sequence and are left as
+ * they are, as are rows that would stand for a key before the first.
+ *
+ * spd_cache_append writes the rows' keys and values into their sequences' pages of one layer, keys and queries
+ * rotated at their positions (rotate-half RoPE, cos and sin: device fp32 [rope_positions][head_dim / 2], with
+ * rope_positions >= 16 * max_pages; both NULL with rope_positions 0: no rotation). k, v: device [rows] of n_kv_heads *
+ * head_dim elements of dtype, rows k_stride and v_stride elements apart; q and q_out likewise, n_q_heads * head_dim
+ * (both NULL with n_q_heads 0: keys and values only; q_out may be q). The rotation is fp32, rounded once to the cache's
+ * type (to dtype for q_out). Pointers are 16-byte aligned, strides multiples of 16 bytes. A sequence has to be named
+ * once, and the pages its rows fall in have to be its own, as spd_cache_reserve leaves them. */
+spd_status spd_cache_append(const spd_cache* c, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                            int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                            int32_t n_q_heads, int32_t dtype, const float* rope_cos, const float* rope_sin,
+                            int32_t rope_positions, const int32_t* seqs, const int32_t* cu_rows, int32_t nseqs,
+                            int32_t rows, void* stream);
+
+/* Causal attention of a batch's packed rows (as above; prompts, or the next rows of one) over one layer of the cache:
+ * the row of key p attends keys 0 .. p of its sequence, query head h reads KV head h / (n_q_heads / n_kv_heads),
+ * scores are scaled by 1 / sqrt(head_dim). A row that would stand for a key before the first attends nothing: zeros.
+ *   q, out: device [rows] of n_q_heads * head_dim elements of dtype, rows q_stride and out_stride elements apart
+ *     (16-byte aligned, strides multiples of 16 bytes). dtype SPD_F32 with any cache, SPD_BF16 with a bf16 cache.
+ *   max_len (host): the keys of the longest sequence, for the choice of key splits (0: 16 * max_pages). The result
+ *     is right for any value, if not always in the same order of sums.
+ *   workspace: device, 256-byte aligned, of spd_prompt_attention_workspace(the same sizes).
+ * n_q_heads / n_kv_heads is at most 16, nseqs at most 65536. */
+spd_status spd_prompt_attention_workspace(const spd_cache* c, int32_t n_q_heads, int32_t dtype, int32_t nseqs,
+                                          int32_t rows, int32_t max_len, size_t* bytes);
+spd_status spd_prompt_attention(const spd_cache* c, int32_t layer, const void* q, int64_t q_stride, void* out,
+                                int64_t out_stride, int32_t n_q_heads, int32_t dtype, const int32_t* seqs,
+                                const int32_t* cu_rows, int32_t nseqs, int32_t rows, int32_t max_len, void* workspace,
+                                size_t ws_bytes, void* stream);
+
+/* Decode attention of a batch in which groups of sequences share a prefix, read once for all of a group. Row i of q
+ * (its query at key lens[seqs[i]] - 1) attends keys 0 .. lens[seqs[i]] - 1 of sequence seqs[i]; a sequence without
+ * keys gets zeros. Group j is rows cu_groups[j] .. cu_groups[j + 1] - 1 (device int32[ngroups + 1], ascending, from 0 to
+ * nseqs); its rows' sequences agree in their first prefix_lens[j] keys (device int32[ngroups]), as forked ones do, which
+ * are read through the pages of the group's first sequence. A row shorter than its group's prefix attends the
+ * keys it has; the first row's sequence must hold the prefix. With ngroups 0 (both arrays NULL) no row shares
+ * anything. q, out, max_len and the workspace as in spd_prompt_attention; nseqs at most 4096. */
+spd_status spd_prefix_attention_workspace(const spd_cache* c, int32_t n_q_heads, int32_t dtype, int32_t nseqs,
+                                          int32_t ngroups, int32_t max_len, size_t* bytes);
+spd_status spd_prefix_attention(const spd_cache* c, int32_t layer, const void* q, int64_t q_stride, void* out,
+                                int64_t out_stride, int32_t n_q_heads, int32_t dtype, const int32_t* seqs,
+                                int32_t nseqs, const int32_t* cu_groups, const int32_t* prefix_lens, int32_t ngroups,
+                                int32_t max_len, void* workspace, size_t ws_bytes, void* stream);
+
 /* Release the handle's events and host buffers (not the caller's memory). NULL is ignored. */
 void spd_destroy(spd_handle* h);
 

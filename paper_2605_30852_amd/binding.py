@@ -19,6 +19,7 @@ SPD_DBG_RESID, SPD_DBG_ANCHORS, SPD_DBG_PDM_HIDDEN = 1, 2, 3
 SPD_DBG_EXIT_LOGITS, SPD_DBG_PDM_LOGITS, SPD_DBG_TOKENS, SPD_DBG_STATE = 4, 5, 6, 7
 SPD_DBG_KTRACE, SPD_DBG_QDIST = 10, 11
 MAX_TOP_K = 64
+SPD_CACHE_DONE, SPD_CACHE_NO_PAGES, SPD_CACHE_BAD_LEN, SPD_CACHE_BAD_SEQ = 0, 1, 2, 3
 SPD_K_QKV, SPD_K_ATTN, SPD_K_OPROJ, SPD_K_GATEUP, SPD_K_DOWN, SPD_K_HEAD, SPD_K_SPANS = 1, 2, 3, 4, 5, 6, 7
 
 
@@ -48,6 +49,11 @@ class spd_weights(ct.Structure):
     ]
 
 
+class spd_cache(ct.Structure):
+    _fields_ = [(k, ct.c_void_p) for k in ("kv", "page_table", "lens", "refs")] + [
+        (k, ct.c_int32) for k in ("n_layers", "num_pages", "max_seqs", "max_pages", "n_kv_heads", "head_dim", "dtype")]
+
+
 class spd_step_result(ct.Structure):
     _fields_ = [(k, ct.c_int32) for k in
                 ("decision", "target_argmax", "draft", "pdm_draft", "exited_pos", "exited_token", "verified_pos",
@@ -65,6 +71,9 @@ EXPORTS = [
     "spd_step_plan_info", "spd_set_kernel_trace", "spd_set_pdm_placement",
     "spd_set_pdm_grid", "spd_set_pdm_enabled", "spd_probe_hbm_read", "spd_set_sampling",
     "spd_set_pdm_schedule", "spd_set_graph_steps", "spd_decode_attention", "spd_decode_attention_noalloc",
+    "spd_cache_workspace", "spd_cache_reserve", "spd_cache_fork", "spd_cache_truncate", "spd_cache_compact",
+    "spd_cache_append", "spd_prompt_attention_workspace", "spd_prompt_attention", "spd_prefix_attention_workspace",
+    "spd_prefix_attention",
 ]
 
 _lib: Optional[ct.CDLL] = None
@@ -85,6 +94,9 @@ def lib() -> ct.CDLL:
         L = ct.CDLL(LIB_PATH)
         P = ct.c_void_p
         I = ct.c_int32
+        L64 = ct.c_int64
+        C = ct.POINTER(spd_cache)
+        Z = ct.POINTER(ct.c_size_t)
         sig = {
             "spd_workspace_size": (I, [ct.POINTER(spd_config), ct.POINTER(ct.c_size_t)]),
             "spd_stage_bounds": (I, [ct.POINTER(spd_config), ct.POINTER(ct.c_int32)]),
@@ -118,6 +130,16 @@ def lib() -> ct.CDLL:
             "spd_decode_attention": (I, [P, P, P, I, ct.POINTER(ct.c_int32), I, I, I, I, I, I, P, P, ct.c_size_t,
                                          P]),
             "spd_decode_attention_noalloc": (I, [P, P, P, I, ct.POINTER(ct.c_int32), I, I, I, I, I, I, P, P]),
+            "spd_cache_workspace": (I, [C, I, Z]),
+            "spd_cache_reserve": (I, [C, P, P, I, P, P, ct.c_size_t, P]),
+            "spd_cache_fork": (I, [C, P, P, P, I, P, P, ct.c_size_t, P]),
+            "spd_cache_truncate": (I, [C, P, P, I, P, P, ct.c_size_t, P]),
+            "spd_cache_compact": (I, [C, P, P, ct.c_size_t, P]),
+            "spd_cache_append": (I, [C, I, P, L64, P, L64, P, L64, P, L64, I, I, P, P, I, P, P, I, I, P]),
+            "spd_prompt_attention_workspace": (I, [C, I, I, I, I, I, Z]),
+            "spd_prompt_attention": (I, [C, I, P, L64, P, L64, I, I, P, P, I, I, I, P, ct.c_size_t, P]),
+            "spd_prefix_attention_workspace": (I, [C, I, I, I, I, I, Z]),
+            "spd_prefix_attention": (I, [C, I, P, L64, P, L64, I, I, P, I, P, P, I, I, P, ct.c_size_t, P]),
             "spd_destroy": (None, [P]),
             "spd_status_str": (ct.c_char_p, [I]),
             "spd_last_error": (ct.c_char_p, [P]),
@@ -338,6 +360,70 @@ def spd_decode_attention_noalloc(q: int, kv: int, page_table: int, num_pages: in
                                               ln.ctypes.data_as(ct.POINTER(ct.c_int32)), len(ln), int(n_q_heads),
                                               int(n_kv_heads), int(head_dim), int(dtype), int(chunk), out, stream),
            None)
+
+
+# Calls on a spd_cache: device pointers as ints, 0 or None for NULL.
+def spd_cache_workspace(cache: spd_cache, n: int) -> int:
+    b = ct.c_size_t(0)
+    _check("spd_cache_workspace", lib().spd_cache_workspace(ct.byref(cache), n, ct.byref(b)))
+    return b.value
+
+
+def spd_cache_reserve(cache: spd_cache, seqs: int, add: int, n: int, status: int, workspace: int, ws_bytes: int,
+                      stream: int) -> None:
+    _check("spd_cache_reserve", lib().spd_cache_reserve(ct.byref(cache), seqs, add, n, status, workspace, ws_bytes, stream))
+
+
+def spd_cache_fork(cache: spd_cache, src: int, dst: int, keep: int, n: int, status: int, workspace: int, ws_bytes: int,
+                   stream: int) -> None:
+    _check("spd_cache_fork", lib().spd_cache_fork(ct.byref(cache), src, dst, keep, n, status, workspace, ws_bytes, stream))
+
+
+def spd_cache_truncate(cache: spd_cache, seqs: int, keep: int, n: int, status: int, workspace: int, ws_bytes: int,
+                       stream: int) -> None:
+    _check("spd_cache_truncate", lib().spd_cache_truncate(ct.byref(cache), seqs, keep, n, status, workspace, ws_bytes, stream))
+
+
+def spd_cache_compact(cache: spd_cache, live: int, workspace: int, ws_bytes: int, stream: int) -> None:
+    _check("spd_cache_compact", lib().spd_cache_compact(ct.byref(cache), live, workspace, ws_bytes, stream))
+
+
+def spd_cache_append(cache: spd_cache, layer: int, k: int, k_stride: int, v: int, v_stride: int, q: int, q_stride: int,
+                     q_out: int, q_out_stride: int, n_q_heads: int, dtype: int, rope_cos: int, rope_sin: int,
+                     rope_positions: int, seqs: int, cu_rows: int, nseqs: int, rows: int, stream: int) -> None:
+    _check("spd_cache_append",
+           lib().spd_cache_append(ct.byref(cache), layer, k, k_stride, v, v_stride, q, q_stride, q_out, q_out_stride, n_q_heads,
+                                  dtype, rope_cos, rope_sin, rope_positions, seqs, cu_rows, nseqs, rows, stream))
+
+
+def spd_prompt_attention_workspace(cache: spd_cache, n_q_heads: int, dtype: int, nseqs: int, rows: int, max_len: int) -> int:
+    b = ct.c_size_t(0)
+    _check("spd_prompt_attention_workspace",
+           lib().spd_prompt_attention_workspace(ct.byref(cache), n_q_heads, dtype, nseqs, rows, max_len, ct.byref(b)))
+    return b.value
+
+
+def spd_prompt_attention(cache: spd_cache, layer: int, q: int, q_stride: int, out: int, out_stride: int, n_q_heads: int,
+                         dtype: int, seqs: int, cu_rows: int, nseqs: int, rows: int, max_len: int, workspace: int,
+                         ws_bytes: int, stream: int) -> None:
+    _check("spd_prompt_attention",
+           lib().spd_prompt_attention(ct.byref(cache), layer, q, q_stride, out, out_stride, n_q_heads, dtype, seqs, cu_rows,
+                                      nseqs, rows, max_len, workspace, ws_bytes, stream))
+
+
+def spd_prefix_attention_workspace(cache: spd_cache, n_q_heads: int, dtype: int, nseqs: int, ngroups: int, max_len: int) -> int:
+    b = ct.c_size_t(0)
+    _check("spd_prefix_attention_workspace",
+           lib().spd_prefix_attention_workspace(ct.byref(cache), n_q_heads, dtype, nseqs, ngroups, max_len, ct.byref(b)))
+    return b.value
+
+
+def spd_prefix_attention(cache: spd_cache, layer: int, q: int, q_stride: int, out: int, out_stride: int, n_q_heads: int,
+                         dtype: int, seqs: int, nseqs: int, cu_groups: int, prefix_lens: int, ngroups: int, max_len: int,
+                         workspace: int, ws_bytes: int, stream: int) -> None:
+    _check("spd_prefix_attention",
+           lib().spd_prefix_attention(ct.byref(cache), layer, q, q_stride, out, out_stride, n_q_heads, dtype, seqs, nseqs,
+                                      cu_groups, prefix_lens, ngroups, max_len, workspace, ws_bytes, stream))
 
 
 def spd_destroy(h: int) -> None:

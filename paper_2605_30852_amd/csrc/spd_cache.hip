@@ -1,0 +1,551 @@
+// The pages of a cache of several sequences: growing (with copies of shared pages), forking, truncating and compacting
+// them, and the rows that enter them.
+//
+// The state (table, lens, refs) lives on the device. A call that changes pages is two launches. The plan, one
+// workgroup, checks the request and decides everything: a call that does not fit changes nothing. It works in tiles of
+// entries or page ids with a prefix sum over the workgroup, so that pages are handed out in one fixed order, whatever
+// the order in which waves run. Then many workgroups apply the plan: entries, counts (integer atomics, whose order
+// does not show) and the copies of pages, which are what takes time: page bytes x layers, read and written once.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "spd_cachefn.h"
+
+namespace spd {
+
+spd_status check_cache(const char* call, const spd_cache* c, bool pages) {
+  if (!c) return invalid(call, "NULL cache");
+  if (!c->kv || !c->page_table || !c->lens || (pages && !c->refs)) return invalid(call, "NULL pointer in the cache");
+  if (misaligned(c->kv, 16)) return invalid(call, "kv must be 16-byte aligned");
+  if (misaligned(c->page_table, 4) || misaligned(c->lens, 4) || misaligned(c->refs, 4))
+    return invalid(call, "page_table, lens and refs must be 4-byte aligned");
+  if (c->n_layers < 1 || c->num_pages < 1) return invalid(call, "n_layers and num_pages must be positive");
+  if (c->max_seqs < 1 || c->max_seqs > kMaxSeqs) return invalid(call, "max_seqs must be in [1, 65536]");
+  if (c->max_pages < 1 || c->max_pages > kMaxPages) return invalid(call, "max_pages must be in [1, 2^26]");
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 1024) return invalid(call, "n_kv_heads must be in [1, 1024]");
+  if (c->head_dim != 64 && c->head_dim != 128) return invalid(call, "head_dim must be 64 or 128");
+  if (c->dtype != SPD_F32 && c->dtype != SPD_BF16) return invalid(call, "the cache's dtype must be SPD_F32 or SPD_BF16");
+  return SPD_OK;
+}
+
+spd_status check_workspace(const char* call, const void* ws, size_t bytes, size_t need) {
+  if (need == 0) return SPD_OK;
+  if (!ws || misaligned(ws, 256)) return invalid(call, "workspace must be non-NULL and 256-byte aligned");
+  if (bytes < need) {
+    set_call_error(std::string(call) + ": workspace too small, " + std::to_string(need) + " bytes needed");
+    return SPD_E_CAPACITY;
+  }
+  return SPD_OK;
+}
+
+spd_status check_rows(const char* call, const void* p, int64_t stride, int heads, int head_dim, int dtype) {
+  const int64_t e = (int64_t)elem_bytes(dtype);
+  if (!p) return invalid(call, "NULL pointer");
+  if (misaligned(p, 16) || stride % (16 / e)) return invalid(call, "rows must be 16-byte aligned, strides multiples of 16 bytes");
+  if (stride < (int64_t)heads * head_dim || stride > ((int64_t)1 << 40)) return invalid(call, "a row's stride is below its length (or past 2^40)");
+  return SPD_OK;
+}
+
+spd_status check_launch(const char* call) {
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) return SPD_OK;
+  set_call_error(std::string(call) + " launch: " + hipGetErrorString(e));
+  return SPD_E_HIP;
+}
+
+namespace {
+
+constexpr int kPlanWG = 1024, kPlanWaves = kPlanWG / 64;
+constexpr int kIdsPerWave = 16 * 64, kIdsPerTile = kPlanWaves * kIdsPerWave;  // page ids of a tile of a plan
+
+// Workspace of a plan, in ints: the header, four arrays of n entries, three of num_pages.
+enum { PH_STATUS = 0, PH_MOVES = 1, PH_LIVE = 2, PH_INTS = 16 };
+struct Plan {
+  int* head;
+  int *first, *begin, *want, *src;  // reserve: an entry's first page in `ids`, the logical pages it takes, the page it copies
+  int* ids;                         // reserve: free pages; compact: holes
+  int* late;                        // compact: held pages that move
+  int* map;                         // compact: where page id goes
+};
+
+size_t plan_ints(const spd_cache& c, int n) { return PH_INTS + 4 * (size_t)n + 3 * (size_t)c.num_pages; }
+
+Plan plan_of(const spd_cache& c, int n, void* ws) {
+  Plan p;
+  p.head = (int*)ws;
+  p.first = p.head + PH_INTS;
+  p.begin = p.first + n;
+  p.want = p.begin + n;
+  p.src = p.want + n;
+  p.ids = p.src + n;
+  p.late = p.ids + c.num_pages;
+  p.map = p.late + c.num_pages;
+  return p;
+}
+
+__device__ __forceinline__ int pages_of(int keys) { return (keys + kPage - 1) / kPage; }
+
+// Exclusive prefix sum of v over the workgroup, and the total; sums: kPlanWaves + 1 entries of LDS.
+__device__ __forceinline__ long long plan_scan(long long v, long long* sums, long long* total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  long long x = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const long long y = __shfl_up(x, d, 64);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();  // the last tile's sums are read
+  if (lane == 63) sums[w] = x;
+  __syncthreads();
+  long long before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < kPlanWaves; i++) {
+    if (i < w) before += sums[i];
+    all += sums[i];
+  }
+  *total = all;
+  return before + x - v;
+}
+
+// Which sequences a call has named.
+struct Named {
+  uint32_t* bits;
+  __device__ __forceinline__ void clear(int max_seqs) const {
+    for (int i = threadIdx.x; i < (max_seqs + 31) / 32; i += kPlanWG) bits[i] = 0u;
+  }
+  __device__ __forceinline__ bool first(int s) const { return !(atomicOr(&bits[s >> 5], 1u << (s & 31)) >> (s & 31) & 1u); }
+};
+
+__global__ __launch_bounds__(kPlanWG) void k_plan_reserve(spd_cache c, const int* seqs, const int* add, int n, int* status,
+                                                          Plan P) {
+  __shared__ uint32_t bits[kMaxSeqs / 32];
+  __shared__ long long sums[kPlanWaves];
+  __shared__ int s_status;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, cap = kPage * c.max_pages;
+  const Named named{bits};
+  named.clear(c.max_seqs);
+  if (tid == 0) s_status = SPD_CACHE_DONE;
+  __syncthreads();
+  long long total = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlanWG) {
+    const int i = i0 + tid;
+    int bad = SPD_CACHE_DONE, need = 0;
+    if (i < n) {
+      const int s = seqs[i], a = add[i];
+      if ((unsigned)s >= (unsigned)c.max_seqs || !named.first(s)) {
+        bad = SPD_CACHE_BAD_SEQ;
+      } else {
+        const int len = c.lens[s];
+        if (a < 0 || len < 0 || len > cap || a > cap - len) {
+          bad = SPD_CACHE_BAD_LEN;
+        } else {
+          const int have = pages_of(len), want = pages_of(len + a);
+          int src = -1;
+          if (a > 0 && len % kPage) {
+            const int last = c.page_table[(size_t)s * c.max_pages + have - 1];
+            if ((unsigned)last < (unsigned)c.num_pages && c.refs[last] > 1) src = last;
+          }
+          const int begin = src >= 0 ? have - 1 : have;
+          need = want - begin;
+          P.begin[i] = begin;
+          P.want[i] = want;
+          P.src[i] = src;
+        }
+      }
+    }
+    if (bad) atomicMax(&s_status, bad);
+    long long all;
+    const long long at = total + plan_scan(need, sums, &all);
+    if (i < n) P.first[i] = (int)min(at, (long long)c.num_pages);
+    total += all;
+  }
+  __syncthreads();
+  // the first `total` free pages: a wave takes 64 ids a load, 16 loads at once
+  long long found = 0;
+  if (s_status == SPD_CACHE_DONE && total <= c.num_pages) {
+    for (long long t0 = 0; t0 < c.num_pages && found < total; t0 += kIdsPerTile) {
+      const long long id0 = t0 + w * kIdsPerWave + lane;
+      bool f[16];
+#pragma unroll
+      for (int k = 0; k < 16; k++) f[k] = id0 + k * 64 < c.num_pages && c.refs[id0 + k * 64] == 0;
+      unsigned long long m[16];
+      int mine = 0;
+#pragma unroll
+      for (int k = 0; k < 16; k++) {
+        m[k] = __ballot(f[k]);
+        mine += __popcll(m[k]);
+      }
+      long long all, at = found + plan_scan(lane == 0 ? mine : 0, sums, &all);
+      at = __shfl(at, 0, 64);
+#pragma unroll
+      for (int k = 0; k < 16; k++) {
+        const long long r = at + __popcll(m[k] & ((1ull << lane) - 1ull));
+        if (f[k] && r < total) P.ids[r] = (int)(id0 + k * 64);
+        at += __popcll(m[k]);
+      }
+      found += all;
+    }
+  }
+  if (tid == 0) {
+    const int st = s_status != SPD_CACHE_DONE ? s_status : found < total ? SPD_CACHE_NO_PAGES : SPD_CACHE_DONE;
+    P.head[PH_STATUS] = st;
+    *status = st;
+  }
+}
+
+// A page of one layer: `bytes` is a multiple of 4096. Eight loads of a thread are under way at once.
+__device__ __forceinline__ void copy_page(char* dst, const char* src, size_t bytes) {
+  constexpr int U = 8;
+  for (size_t b = threadIdx.x * 16; b < bytes; b += (size_t)U * kWG * 16) {
+    uint4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; u++)
+      if (b + (size_t)u * kWG * 16 < bytes) v[u] = *reinterpret_cast<const uint4*>(src + b + (size_t)u * kWG * 16);
+#pragma unroll
+    for (int u = 0; u < U; u++)
+      if (b + (size_t)u * kWG * 16 < bytes) *reinterpret_cast<uint4*>(dst + b + (size_t)u * kWG * 16) = v[u];
+  }
+}
+
+// Grid: x = entry, y = a layer's copy (strided); the entry's table and counts with y = 0.
+__global__ __launch_bounds__(kWG) void k_apply_reserve(spd_cache c, const int* seqs, const int* add, Plan P, size_t page_bytes) {
+  if (P.head[PH_STATUS] != SPD_CACHE_DONE) return;
+  const int i = blockIdx.x, s = seqs[i], begin = P.begin[i], want = P.want[i], src = P.src[i], first = P.first[i];
+  if (src >= 0) {
+    const size_t layer = page_bytes * c.num_pages;
+    for (int l = blockIdx.y; l < c.n_layers; l += gridDim.y) {
+      char* base = (char*)c.kv + l * layer;
+      copy_page(base + P.ids[first] * page_bytes, base + src * page_bytes, page_bytes);
+    }
+  }
+  if (blockIdx.y != 0) return;
+  for (int j = begin + threadIdx.x; j < want; j += kWG) {
+    const int p = P.ids[first + j - begin];
+    c.page_table[(size_t)s * c.max_pages + j] = p;
+    c.refs[p] = 1;
+  }
+  if (threadIdx.x == 0) {
+    if (src >= 0) atomicSub(&c.refs[src], 1);
+    c.lens[s] += add[i];
+  }
+}
+
+__global__ __launch_bounds__(kPlanWG) void k_plan_fork(spd_cache c, const int* src, const int* dst, const int* keep, int n,
+                                                       int* status, Plan P) {
+  __shared__ uint32_t bits[kMaxSeqs / 32];
+  __shared__ int s_status;
+  const Named named{bits};
+  named.clear(c.max_seqs);
+  if (threadIdx.x == 0) s_status = SPD_CACHE_DONE;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kPlanWG) {
+    const int s = src[i], d = dst[i], k = keep[i];
+    int bad = SPD_CACHE_DONE;
+    if ((unsigned)s >= (unsigned)c.max_seqs || (unsigned)d >= (unsigned)c.max_seqs || !named.first(d) || c.lens[d] != 0)
+      bad = SPD_CACHE_BAD_SEQ;
+    else if (k < 0 || k > c.lens[s] || k > kPage * c.max_pages)
+      bad = SPD_CACHE_BAD_LEN;
+    if (bad) atomicMax(&s_status, bad);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    P.head[PH_STATUS] = s_status;
+    *status = s_status;
+  }
+}
+
+// Grid: x = child. A source is no child of this call unless it is empty, so nothing read here is written here.
+__global__ __launch_bounds__(kWG) void k_apply_fork(spd_cache c, const int* src, const int* dst, const int* keep, Plan P) {
+  if (P.head[PH_STATUS] != SPD_CACHE_DONE) return;
+  const int i = blockIdx.x, n = pages_of(keep[i]);
+  const int* from = c.page_table + (size_t)src[i] * c.max_pages;
+  int* to = c.page_table + (size_t)dst[i] * c.max_pages;
+  for (int j = threadIdx.x; j < n; j += kWG) {
+    const int p = from[j];
+    to[j] = p;
+    if ((unsigned)p < (unsigned)c.num_pages) atomicAdd(&c.refs[p], 1);
+  }
+  if (threadIdx.x == 0) c.lens[dst[i]] = keep[i];
+}
+
+__global__ __launch_bounds__(kPlanWG) void k_plan_truncate(spd_cache c, const int* seqs, const int* keep, int n, int* status,
+                                                           Plan P) {
+  __shared__ uint32_t bits[kMaxSeqs / 32];
+  __shared__ int s_status;
+  const Named named{bits};
+  named.clear(c.max_seqs);
+  if (threadIdx.x == 0) s_status = SPD_CACHE_DONE;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kPlanWG) {
+    const int s = seqs[i];
+    int bad = SPD_CACHE_DONE;
+    if ((unsigned)s >= (unsigned)c.max_seqs || !named.first(s))
+      bad = SPD_CACHE_BAD_SEQ;
+    else if (keep[i] < 0 || c.lens[s] < 0 || c.lens[s] > kPage * c.max_pages)
+      bad = SPD_CACHE_BAD_LEN;
+    if (bad) atomicMax(&s_status, bad);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    P.head[PH_STATUS] = s_status;
+    *status = s_status;
+  }
+}
+
+// Grid: x = sequence.
+__global__ __launch_bounds__(kWG) void k_apply_truncate(spd_cache c, const int* seqs, const int* keep, Plan P) {
+  if (P.head[PH_STATUS] != SPD_CACHE_DONE) return;
+  const int s = seqs[blockIdx.x], len = c.lens[s], k = min(keep[blockIdx.x], len), end = pages_of(len);
+  int* row = c.page_table + (size_t)s * c.max_pages;
+  for (int j = pages_of(k) + threadIdx.x; j < end; j += kWG) {
+    const int p = row[j];
+    row[j] = -1;
+    if ((unsigned)p < (unsigned)c.num_pages) atomicSub(&c.refs[p], 1);
+  }
+  __syncthreads();  // every wave has read the length
+  if (threadIdx.x == 0) c.lens[s] = k;
+}
+
+// Held pages are counted (n), then those at n and above and the holes below n are listed, in order: as many of each.
+__global__ __launch_bounds__(kPlanWG) void k_plan_compact(spd_cache c, int* live, Plan P) {
+  __shared__ long long sums[kPlanWaves];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  long long n = 0;
+  for (long long t0 = 0; t0 < c.num_pages; t0 += kIdsPerTile) {
+    const long long id0 = t0 + w * kIdsPerWave + lane;
+    int mine = 0;
+#pragma unroll
+    for (int k = 0; k < 16; k++) mine += id0 + k * 64 < c.num_pages && c.refs[id0 + k * 64] > 0;
+    long long all;
+    plan_scan(mine, sums, &all);
+    n += all;
+  }
+  long long moves = 0;  // holes seen; late pages seen
+  long long lates = 0;
+  for (long long t0 = 0; t0 < c.num_pages; t0 += kIdsPerTile) {
+    const long long id0 = t0 + w * kIdsPerWave + lane;
+    bool hole[16], late[16];
+#pragma unroll
+    for (int k = 0; k < 16; k++) {
+      const long long id = id0 + k * 64;
+      const bool in = id < c.num_pages, held = in && c.refs[id] > 0;
+      hole[k] = in && !held && id < n;
+      late[k] = held && id >= n;
+      if (in && !held && id >= n) P.map[id] = (int)id;
+    }
+    int h = 0, l = 0;
+#pragma unroll
+    for (int k = 0; k < 16; k++) {
+      h += __popcll(__ballot(hole[k]));
+      l += __popcll(__ballot(late[k]));
+    }
+    long long all;  // both counts in one sum: ids are below 2^31
+    long long at = plan_scan(lane == 0 ? (long long)h << 32 | l : 0, sums, &all);
+    at = __shfl(at, 0, 64);
+    long long ah = moves + (at >> 32), al = lates + (at & 0xffffffffll);
+#pragma unroll
+    for (int k = 0; k < 16; k++) {
+      const unsigned long long mh = __ballot(hole[k]), ml = __ballot(late[k]), below = (1ull << lane) - 1ull;
+      if (hole[k]) P.ids[ah + __popcll(mh & below)] = (int)(id0 + k * 64);
+      if (late[k]) P.late[al + __popcll(ml & below)] = (int)(id0 + k * 64);
+      ah += __popcll(mh);
+      al += __popcll(ml);
+    }
+    moves += all >> 32;
+    lates += all & 0xffffffffll;
+  }
+  __syncthreads();  // the lists are whole
+  for (long long k = tid; k < moves; k += kPlanWG) P.map[P.late[k]] = P.ids[k];
+  if (tid == 0) {
+    P.head[PH_MOVES] = (int)moves;
+    P.head[PH_LIVE] = (int)n;
+    *live = (int)n;
+  }
+}
+
+// Sources are at n and above, destinations below: no copy reads what another writes.
+__global__ __launch_bounds__(kWG) void k_apply_compact(spd_cache c, Plan P, size_t page_bytes) {
+  const int moves = P.head[PH_MOVES], n = P.head[PH_LIVE];
+  const size_t layer = page_bytes * c.num_pages;
+  for (long long i = blockIdx.x; i < (long long)moves * c.n_layers; i += gridDim.x) {
+    const int k = (int)(i % moves), l = (int)(i / moves), src = P.late[k], dst = P.ids[k];
+    char* base = (char*)c.kv + l * layer;
+    copy_page(base + dst * page_bytes, base + src * page_bytes, page_bytes);
+    if (l == 0 && threadIdx.x == 0) {
+      c.refs[dst] = c.refs[src];
+      c.refs[src] = 0;
+    }
+  }
+  const size_t entries = (size_t)c.max_seqs * c.max_pages;
+  for (size_t e = (size_t)blockIdx.x * kWG + threadIdx.x; e < entries; e += (size_t)gridDim.x * kWG) {
+    const int p = c.page_table[e];
+    if (p >= n && p < c.num_pages) c.page_table[e] = P.map[p];
+  }
+}
+
+// ------------------------------------------------------------------------------------------------- new rows
+struct AppendArgs {
+  const void *k, *v, *q;
+  void* qo;
+  int64_t ks, vs, qs, qos;
+  const float *cos, *sin;
+  const int *seqs, *cu_rows;
+  int layer, hq, nseqs, rows;
+};
+
+// A workgroup takes a row. A thread's unit is eight dims of a head and the eight that rotate with them.
+template <typename T, typename KVT, int DH>
+__global__ __launch_bounds__(kWG) void k_append(spd_cache c, AppendArgs A) {
+  constexpr int H = DH / 2, UPH = H / 8;
+  const int r = blockIdx.x;
+  const RowAt at = row_at(c, A.seqs, A.cu_rows, A.nseqs, r);
+  if (at.seq < 0 || at.key < 0) return;
+  const int page = c.page_table[(size_t)at.seq * c.max_pages + at.key / kPage];
+  const bool own = (unsigned)page < (unsigned)c.num_pages;
+  const size_t half = (size_t)c.n_kv_heads * kPage * DH;  // a page's keys, then as many values
+  KVT* base = (KVT*)c.kv + (((size_t)A.layer * c.num_pages + (own ? page : 0)) * 2) * half + (size_t)(at.key % kPage) * DH;
+  const int nq = A.hq * UPH, nk = c.n_kv_heads * UPH;
+  for (int u = threadIdx.x; u < nq + 2 * nk; u += kWG) {
+    const int kind = u < nq ? 0 : u < nq + nk ? 1 : 2;
+    const int x = u - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk), h = x / UPH, d = x % UPH * 8;
+    const T* in = kind == 0 ? (const T*)A.q + r * A.qs : kind == 1 ? (const T*)A.k + r * A.ks : (const T*)A.v + r * A.vs;
+    float a[8], b[8];
+    load8(in + h * DH + d, a);
+    load8(in + h * DH + H + d, b);
+    if (A.cos != nullptr && kind < 2) {
+      float cs[8], sn[8];
+      load8(A.cos + (size_t)at.key * H + d, cs);
+      load8(A.sin + (size_t)at.key * H + d, sn);
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const float ra = fmaf(a[e], cs[e], -(b[e] * sn[e])), rb = fmaf(b[e], cs[e], a[e] * sn[e]);
+        a[e] = ra;
+        b[e] = rb;
+      }
+    }
+    if (kind == 0) {
+      T* o = (T*)A.qo + r * A.qos + h * DH + d;
+      store8(o, a);
+      store8(o + H, b);
+    } else if (own) {
+      KVT* o = base + (kind == 2 ? half : 0) + (size_t)h * kPage * DH + d;
+      store8(o, a);
+      store8(o + H, b);
+    }
+  }
+}
+
+template <typename T, typename KVT>
+void launch_append(const spd_cache& c, const AppendArgs& a, hipStream_t s) {
+  if (c.head_dim == 128)
+    hipLaunchKernelGGL((k_append<T, KVT, 128>), dim3(a.rows), dim3(kWG), 0, s, c, a);
+  else
+    hipLaunchKernelGGL((k_append<T, KVT, 64>), dim3(a.rows), dim3(kWG), 0, s, c, a);
+}
+
+size_t page_bytes_of(const spd_cache& c) { return (size_t)2 * c.n_kv_heads * kPage * c.head_dim * elem_bytes(c.dtype); }
+
+// The checks that reserve, fork, truncate and compact share.
+spd_status check_change(const char* call, const spd_cache* c, std::initializer_list<const void*> arrays, int n, void* ws,
+                        size_t ws_bytes) {
+  const spd_status st = check_cache(call, c, true);
+  if (st != SPD_OK) return st;
+  for (const void* p : arrays)
+    if (!p || misaligned(p, 4)) return invalid(call, "NULL or misaligned pointer");
+  if (n < 1 || n > c->max_seqs) return invalid(call, "n must be in [1, max_seqs]");
+  return check_workspace(call, ws, ws_bytes, plan_ints(*c, n) * sizeof(int));
+}
+
+}  // namespace
+}  // namespace spd
+
+using namespace spd;
+
+extern "C" spd_status spd_cache_workspace(const spd_cache* c, int32_t n, size_t* bytes) {
+  const spd_status st = check_cache("cache workspace", c, false);
+  if (st != SPD_OK) return st;
+  if (!bytes || n < 1 || n > c->max_seqs) return invalid("cache workspace", "NULL pointer, or n outside [1, max_seqs]");
+  *bytes = (plan_ints(*c, n) * sizeof(int) + 255) / 256 * 256;
+  return SPD_OK;
+}
+
+extern "C" spd_status spd_cache_reserve(const spd_cache* c, const int32_t* seqs, const int32_t* add, int32_t n, int32_t* status,
+                                        void* workspace, size_t ws_bytes, void* stream) {
+  const spd_status st = check_change("cache reserve", c, {seqs, add, status}, n, workspace, ws_bytes);
+  if (st != SPD_OK) return st;
+  const Plan p = plan_of(*c, n, workspace);
+  hipStream_t s = (hipStream_t)stream;
+  hipLaunchKernelGGL(k_plan_reserve, dim3(1), dim3(kPlanWG), 0, s, *c, seqs, add, n, status, p);
+  hipLaunchKernelGGL(k_apply_reserve, dim3(n, std::min(c->n_layers, 256)), dim3(kWG), 0, s, *c, seqs, add, p,
+                     page_bytes_of(*c));
+  return check_launch("cache reserve");
+}
+
+extern "C" spd_status spd_cache_fork(const spd_cache* c, const int32_t* src, const int32_t* dst, const int32_t* keep, int32_t n,
+                                     int32_t* status, void* workspace, size_t ws_bytes, void* stream) {
+  const spd_status st = check_change("cache fork", c, {src, dst, keep, status}, n, workspace, ws_bytes);
+  if (st != SPD_OK) return st;
+  const Plan p = plan_of(*c, n, workspace);
+  hipStream_t s = (hipStream_t)stream;
+  hipLaunchKernelGGL(k_plan_fork, dim3(1), dim3(kPlanWG), 0, s, *c, src, dst, keep, n, status, p);
+  hipLaunchKernelGGL(k_apply_fork, dim3(n), dim3(kWG), 0, s, *c, src, dst, keep, p);
+  return check_launch("cache fork");
+}
+
+extern "C" spd_status spd_cache_truncate(const spd_cache* c, const int32_t* seqs, const int32_t* keep, int32_t n,
+                                         int32_t* status, void* workspace, size_t ws_bytes, void* stream) {
+  const spd_status st = check_change("cache truncate", c, {seqs, keep, status}, n, workspace, ws_bytes);
+  if (st != SPD_OK) return st;
+  const Plan p = plan_of(*c, n, workspace);
+  hipStream_t s = (hipStream_t)stream;
+  hipLaunchKernelGGL(k_plan_truncate, dim3(1), dim3(kPlanWG), 0, s, *c, seqs, keep, n, status, p);
+  hipLaunchKernelGGL(k_apply_truncate, dim3(n), dim3(kWG), 0, s, *c, seqs, keep, p);
+  return check_launch("cache truncate");
+}
+
+extern "C" spd_status spd_cache_compact(const spd_cache* c, int32_t* live, void* workspace, size_t ws_bytes, void* stream) {
+  const spd_status st = check_change("cache compact", c, {live}, 1, workspace, ws_bytes);
+  if (st != SPD_OK) return st;
+  const Plan p = plan_of(*c, 1, workspace);
+  hipStream_t s = (hipStream_t)stream;
+  hipLaunchKernelGGL(k_plan_compact, dim3(1), dim3(kPlanWG), 0, s, *c, live, p);
+  hipLaunchKernelGGL(k_apply_compact, dim3(2048), dim3(kWG), 0, s, *c, p, page_bytes_of(*c));
+  return check_launch("cache compact");
+}
+
+extern "C" spd_status spd_cache_append(const spd_cache* c, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                                       int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                                       int32_t n_q_heads, int32_t dtype, const float* rope_cos, const float* rope_sin,
+                                       int32_t rope_positions, const int32_t* seqs, const int32_t* cu_rows, int32_t nseqs,
+                                       int32_t rows, void* stream) {
+  const char* call = "cache append";
+  spd_status st = check_cache(call, c, false);
+  if (st != SPD_OK) return st;
+  if (dtype != SPD_F32 && dtype != SPD_BF16) return invalid(call, "dtype must be SPD_F32 or SPD_BF16");
+  if (layer < 0 || layer >= c->n_layers) return invalid(call, "no such layer");
+  if (!seqs || !cu_rows || misaligned(seqs, 4) || misaligned(cu_rows, 4)) return invalid(call, "NULL or misaligned pointer");
+  if (nseqs < 1 || nseqs > c->max_seqs) return invalid(call, "nseqs must be in [1, max_seqs]");
+  if (rows < 0) return invalid(call, "rows must not be negative");
+  if ((st = check_rows(call, k, k_stride, c->n_kv_heads, c->head_dim, dtype)) != SPD_OK) return st;
+  if ((st = check_rows(call, v, v_stride, c->n_kv_heads, c->head_dim, dtype)) != SPD_OK) return st;
+  if (n_q_heads < 0 || n_q_heads > 16384 || (n_q_heads == 0) != (q == nullptr) || (q == nullptr) != (q_out == nullptr))
+    return invalid(call, "q and q_out come with n_q_heads in [1, 16384], or are NULL with n_q_heads 0");
+  if (q) {
+    if ((st = check_rows(call, q, q_stride, n_q_heads, c->head_dim, dtype)) != SPD_OK) return st;
+    if ((st = check_rows(call, q_out, q_out_stride, n_q_heads, c->head_dim, dtype)) != SPD_OK) return st;
+  }
+  if ((rope_cos == nullptr) != (rope_sin == nullptr)) return invalid(call, "cos and sin come together");
+  if (misaligned(rope_cos, 16) || misaligned(rope_sin, 16)) return invalid(call, "cos and sin must be 16-byte aligned");
+  if (rope_cos ? rope_positions < kPage * c->max_pages : rope_positions != 0)
+    return invalid(call, "rope_positions must be at least 16 * max_pages (0 without cos and sin)");
+  if (rows == 0) return SPD_OK;
+  const AppendArgs a{k, v, q, q_out, k_stride, v_stride, q_stride, q_out_stride, rope_cos, rope_sin, seqs, cu_rows, layer,
+                     n_q_heads, nseqs, rows};
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == SPD_BF16)
+    c->dtype == SPD_BF16 ? launch_append<uint16_t, uint16_t>(*c, a, s) : launch_append<uint16_t, float>(*c, a, s);
+  else
+    c->dtype == SPD_BF16 ? launch_append<float, uint16_t>(*c, a, s) : launch_append<float, float>(*c, a, s);
+  return check_launch(call);
+}
