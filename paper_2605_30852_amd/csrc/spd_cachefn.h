@@ -42,12 +42,11 @@ __device__ __forceinline__ RowAt row_at(const spd_cache& c, const int* seqs, con
 // A page to read: an id that is none becomes page 0.
 __device__ __forceinline__ int page_to_read(const spd_cache& c, int id) { return (unsigned)id < (unsigned)c.num_pages ? id : 0; }
 
-// fp32 to a storage type, to nearest even; infinities and NaN stay what they are.
-__device__ __forceinline__ uint16_t to_bf16(float f) {
-  const __bf16 b = (__bf16)f;
-  uint16_t u;
-  __builtin_memcpy(&u, &b, 2);
-  return u;
+// Two fp32 values as bf16, to nearest even; infinities and NaN stay what they are.
+typedef float fp32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(fp32x2{a, b}, bf16x2));
 }
 
 // Eight elements (16-byte aligned) as floats, and back.
@@ -65,7 +64,7 @@ __device__ __forceinline__ void store8(float* p, const float (&f)[8]) {
 __device__ __forceinline__ void store8(uint16_t* p, const float (&f)[8]) {
   uint32_t u[4];
 #pragma unroll
-  for (int i = 0; i < 4; i++) u[i] = to_bf16(f[2 * i]) | (uint32_t)to_bf16(f[2 * i + 1]) << 16;
+  for (int i = 0; i < 4; i++) u[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
   *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
 }
 

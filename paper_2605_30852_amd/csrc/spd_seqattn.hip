@@ -26,27 +26,19 @@ struct SeqArgs {
   float scale;
 };
 
-// Where a row's keys are: those below `shared` through `first`, the others through `own` (rows of the page table).
-struct Keys {
-  const int *first, *own;
-  int shared;
-  __device__ __forceinline__ int page(const spd_cache& c, int key) const {
-    return page_to_read(c, (key < shared ? first : own)[key / kPage]);
-  }
-};
-
-// A query over the keys [0, n) in plain fp32, by the whole workgroup: scores in passes of 256 keys, computed twice
+// A query over the keys [k0, k1) in plain fp32, by the whole workgroup, which a query, key or value that is not finite
+// needs: there 0 times a value behind the query's own keys, or a plane's 0 * inf, is NaN on matrix cores. Scores in passes of 256 keys, computed twice
 // rather than kept. M, L and a (dims 4 d4 .. + 3 of thread d4 = tid % (DH / 4)) are the maximum, the sum and the
 // output; true in the threads that hold them. lds: kWG * 6 floats.
 template <typename T, typename KVT, int DH>
-__device__ bool plain_query(const spd_cache& c, const KVT* pool, const Keys keys, int g, const T* q, float scale, int k0, int k1,
-                            float* lds, float& M, float& L, float (&a)[4]) {
+__device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* table, int g, const T* q, float scale, int k0,
+                            int k1, float* lds, float& M, float& L, float (&a)[4]) {
   constexpr int TPQ = DH / 4, NG = kWG / TPQ;
   const int tid = threadIdx.x, d4 = tid % TPQ, grp = tid / TPQ;
   const size_t half = (size_t)c.n_kv_heads * kPage * DH;
   float* sp = lds;
   float* sr = lds + kWG;
-  auto row = [&](int key) { return pool + keys.page(c, key) * 2 * half + (size_t)(g * kPage + key % kPage) * DH; };
+  auto row = [&](int key) { return pool + page_to_read(c, table[key / kPage]) * 2 * half + (size_t)(g * kPage + key % kPage) * DH; };
   auto score = [&](int key) {
     const KVT* k = row(key);
     float s = 0.f;
@@ -123,68 +115,916 @@ __device__ __forceinline__ void store4(float* p, const float (&a)[4], float f) {
   *reinterpret_cast<float4*>(p) = make_float4(a[0] * f, a[1] * f, a[2] * f, a[3] * f);
 }
 __device__ __forceinline__ void store4(uint16_t* p, const float (&a)[4], float f) {
-  *reinterpret_cast<uint2*>(p) = make_uint2(to_bf16(a[0] * f) | (uint32_t)to_bf16(a[1] * f) << 16,
-                                            to_bf16(a[2] * f) | (uint32_t)to_bf16(a[3] * f) << 16);
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(a[0] * f, a[1] * f), pack_bf16(a[2] * f, a[3] * f));
 }
 
-// Row r's heads of KV head g over keys [0, n).
+// What a query's plain pass leaves in the place of its result in a piece: keys [k0, n) of the piece's.
+struct Item;
+struct Records;
 template <typename T, typename KVT, int DH>
-__device__ void plain_row(const SeqArgs& A, const Keys keys, int r, int g, int n, float* lds) {
-  for (int h = g * A.G; h < (g + 1) * A.G; h++) {
-    float a[4], M, L;
-    T* out = (T*)A.out + r * A.os + h * DH + 4 * (threadIdx.x % (DH / 4));
-    if (n <= 0) {
-      const float z[4] = {0.f, 0.f, 0.f, 0.f};
-      if (threadIdx.x < DH / 4) store4(out, z, 0.f);
-    } else if (plain_query<T, KVT, DH>(A.c, (const KVT*)A.kv, keys, g, (const T*)A.q + r * A.qs + h * DH, A.scale, 0, n, lds, M, L, a)) {
-      store4(out, a, 1.0f / L);
+__device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, int r, int head, int j, int nq, int n, float* lds);
+
+// --------------------------------------------------------------------------------------- pieces of the work
+// A call's work is cut on the device, by one workgroup, into pieces: some queries of a KV head (rows times its G
+// heads) over a run of keys. A prompt's tile of rows is a job over the keys up to its last row; a group's rows are jobs
+// over its prefix, and each row one over the keys behind it. Jobs longer than a `chunk` are split, so that a few rows
+// behind long caches fill the GPU: chunk = all jobs' keys / pieces wanted of a KV head. The pieces are
+// handed out longest first (a counting sort of their lengths), which is what keeps the last workgroups short.
+// A job of one piece writes its rows' outputs; the pieces of others leave records (o, m, l), which the merge joins in
+// the order of the keys.
+struct Item {
+  int row0, nrows;  // rows of q
+  int table;        // the sequence whose pages hold the keys
+  int k0, k1;       // keys
+  int rec;          // first record, -1: outputs
+  int lim0;         // causal: row row0 + i attends keys below lim0 + i
+  int mode;
+};
+enum { ITEM_NARROW = 1, ITEM_FLAT = 2 };  // at most 64 queries; each row attends its sequence's keys
+
+// Rows whose pieces' records are to be joined: those of up to two jobs.
+struct Merge {
+  int row0, nrows;
+  int rec[2], pieces[2];
+  int queries[2], first[2];  // queries of the job (a KV head's records of a piece), and the first one of these rows
+  int lim0, mode;
+};
+
+constexpr int kPlanWG = 1024;
+constexpr int kMinChunk = 256;
+constexpr int kWantedWGs = 512;
+constexpr int kBuckets = 256;
+
+struct PlanArgs {
+  spd_cache c;
+  const int *seqs, *cu, *prefix;
+  int nseqs, rows, ngroups, G, wanted;  // wanted: pieces of a KV head
+  int rpt;                              // rows of a tile
+  unsigned long long records;           // room for them
+  int* count;                           // items, merges
+  Item* items;
+  Merge* merges;
+};
+
+struct Job {
+  int row0, nrows, table, a, b, lim0, mode;
+};
+
+// Job t of a prompt call. The tiles of sequence i have the numbers cu[i] / rpt + i and up: enough of them, in order,
+// without a sum over the sequences before.
+__device__ bool prompt_job(const PlanArgs& P, int t, Job& j) {
+  int lo = 0, hi = P.nseqs - 1;
+  while (lo < hi) {  // last i with cu[i] / rpt + i <= t
+    const int mid = (lo + hi + 1) >> 1;
+    if (P.cu[mid] / P.rpt + mid <= t)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  const int begin = P.cu[lo], end = min(P.cu[lo + 1], P.rows), s = P.seqs[lo];
+  if (begin < 0 || begin >= end || (unsigned)s >= (unsigned)P.c.max_seqs) return false;
+  const long long row0 = begin + (long long)(t - begin / P.rpt - lo) * P.rpt;
+  if (row0 < begin || row0 >= end) return false;
+  j.row0 = (int)row0;
+  j.nrows = min(P.rpt, end - j.row0);
+  j.table = s;
+  j.a = 0;
+  // sequence cu[lo + 1] may lie behind the buffers' rows: the keys are those of its own rows
+  const long long lim0 = (long long)seq_len(P.c, s) - P.cu[lo + 1] + j.row0 + 1;
+  j.lim0 = (int)max(lim0, -(1ll << 30));
+  j.b = max(0, j.lim0 + j.nrows - 1);
+  j.mode = j.nrows * P.G <= 64 ? ITEM_NARROW : 0;
+  return true;
+}
+
+// The prefix that row r's group shares: its length (0: none), the first row and the number of rows.
+__device__ int shared_prefix(const PlanArgs& P, int j, int& first, int& rows) {
+  first = P.cu[j];
+  rows = min(P.cu[j + 1], P.nseqs) - first;
+  if (first < 0 || rows < 2) return 0;
+  const int s = P.seqs[first];
+  return (unsigned)s < (unsigned)P.c.max_seqs ? min(max(P.prefix[j], 0), seq_len(P.c, s)) : 0;
+}
+
+__device__ int group_of(const PlanArgs& P, int r) {
+  int lo = 0, hi = P.ngroups - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (P.cu[mid] <= r)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return lo;
+}
+
+// Job t of a decode call: below `tiles` a tile of a group's rows over the prefix, else a row over the keys behind it.
+// shared: a row's own job is joined with its prefix's.
+__device__ bool prefix_job(const PlanArgs& P, int t, int tiles, Job& j, bool& shared) {
+  shared = false;
+  if (t < tiles) {
+    int lo = 0, hi = P.ngroups - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (P.cu[mid] / P.rpt + mid <= t)
+        lo = mid;
+      else
+        hi = mid - 1;
     }
+    int first, rows;
+    const int n = shared_prefix(P, lo, first, rows);
+    if (n == 0) return false;
+    const long long at = (long long)(t - first / P.rpt - lo) * P.rpt;
+    if (at < 0 || at >= rows) return false;
+    j.row0 = first + (int)at;
+    j.nrows = min(P.rpt, rows - (int)at);
+    j.table = P.seqs[first];
+    j.a = 0;
+    j.b = n;
+    j.mode = ITEM_FLAT | (j.nrows * P.G <= 64 ? ITEM_NARROW : 0);
+    j.lim0 = 0;
+    shared = true;
+    return true;
+  }
+  const int r = t - tiles, s = P.seqs[r];
+  if ((unsigned)s >= (unsigned)P.c.max_seqs) return false;
+  j.row0 = r;
+  j.nrows = 1;
+  j.table = s;
+  j.b = seq_len(P.c, s);
+  j.a = 0;
+  j.lim0 = 0;
+  j.mode = ITEM_FLAT | ITEM_NARROW;
+  if (P.ngroups > 0) {
+    int first, rows;
+    const int g = group_of(P, r), n = shared_prefix(P, g, first, rows);
+    if (n > 0 && r >= first && r < first + rows) {
+      shared = true;
+      j.a = min(n, j.b);
+    }
+  }
+  return true;
+}
+
+// A prompt's merge is known with its job. A decode row's takes its own job's records and those of its tile, which the
+// tile's thread leaves in tile_rec (in LDS order: by tile number, kept in global memory behind the items).
+template <bool PREFIX>
+__global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P, int jobs, int tiles, int4* tile_rec) {
+  __shared__ unsigned long long s_total, s_rec;
+  __shared__ int s_max, s_count[kBuckets], s_merges;
+  const int tid = threadIdx.x;
+  if (tid < kBuckets) s_count[tid] = 0;
+  if (tid == 0) {
+    s_total = 0ull;
+    s_max = 1;
+    s_rec = 0ull;
+    s_merges = 0;
+  }
+  __syncthreads();
+  auto job = [&](int t, Job& j, bool& shared) {
+    if constexpr (PREFIX) return prefix_job(P, t, tiles, j, shared);
+    shared = false;
+    return prompt_job(P, t, j);
+  };
+  {
+    unsigned long long sum = 0ull;
+    int longest = 1;
+    for (int t = tid; t < jobs; t += kPlanWG) {
+      Job j;
+      bool sh;
+      if (!job(t, j, sh)) continue;
+      sum += (unsigned)(j.b - j.a);
+      longest = max(longest, j.b - j.a);
+    }
+    atomicAdd(&s_total, sum);
+    atomicMax(&s_max, longest);
+  }
+  __syncthreads();
+  const unsigned long long want = (s_total + P.wanted - 1) / P.wanted;
+  const int chunk = want >= (unsigned)s_max ? (s_max + 63) / 64 * 64 : max(kMinChunk, (int)((want + 63) / 64 * 64));
+  const int longest = min(s_max, chunk);
+  auto bucket = [&](int n, int mode) {  // the longest first; a key of a wide piece costs about twice a narrow one's
+    const long long x = (long long)n * (mode & ITEM_NARROW ? 1 : 2) * (kBuckets - 1) / (2ll * longest);
+    return kBuckets - 1 - (int)min(x, (long long)kBuckets - 1);
+  };
+  // a job's pieces; 0: nothing to do (a row that ends with its prefix)
+  auto pieces_of = [&](const Job& j, bool sh) { return j.b > j.a ? (j.b - j.a + chunk - 1) / chunk : sh ? 0 : 1; };
+  for (int t = tid; t < jobs; t += kPlanWG) {
+    Job j;
+    bool sh;
+    if (!job(t, j, sh)) continue;
+    const int n = pieces_of(j, sh);
+    for (int p = 0; p < n; p++) atomicAdd(&s_count[bucket(min(chunk, j.b - j.a - p * chunk), j.mode)], 1);
+  }
+  __syncthreads();
+  if (tid < 64) {  // bucket counts to their first places
+    int before = 0;
+    for (int b0 = 0; b0 < kBuckets; b0 += 64) {
+      const int v = s_count[b0 + tid];
+      int x = v;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d, 64);
+        if (tid >= d) x += y;
+      }
+      s_count[b0 + tid] = before + x - v;
+      before += __shfl(x, 63, 64);
+    }
+    if (tid == 0) P.count[0] = before;
+  }
+  __syncthreads();
+  for (int t = tid; t < jobs; t += kPlanWG) {
+    Job j;
+    bool sh;
+    if (!job(t, j, sh)) {
+      if (PREFIX && t < tiles) tile_rec[t] = make_int4(0, 0, 0, 0);
+      continue;
+    }
+    int n = pieces_of(j, sh), rec = -1;
+    const int nq = j.nrows * P.G;
+    if (n > 1 || sh) {
+      const long long need = (long long)n * P.c.n_kv_heads * nq;
+      const unsigned long long at = atomicAdd(&s_rec, (unsigned long long)need);
+      rec = (int)at;
+      if (at + need > P.records) n = 0;  // only where cu_groups does not ascend
+      if (PREFIX && t < tiles) {
+        tile_rec[t] = make_int4(rec, n, nq, 0);
+      } else {
+        Merge m;
+        m.row0 = j.row0;
+        m.nrows = j.nrows;
+        m.rec[0] = m.pieces[0] = m.queries[0] = m.first[0] = 0;
+        m.rec[1] = rec;
+        m.pieces[1] = n;
+        m.queries[1] = nq;
+        m.first[1] = 0;
+        m.lim0 = j.lim0;
+        m.mode = j.mode;
+        if (PREFIX && sh) {
+          int first, rows;
+          const int g = group_of(P, j.row0);
+          shared_prefix(P, g, first, rows);
+          m.queries[0] = first / P.rpt + g + (j.row0 - first) / P.rpt;  // the tile's number, replaced below
+          m.first[0] = (j.row0 - first) % P.rpt * P.G;
+          m.pieces[0] = -1;
+        }
+        P.merges[atomicAdd(&s_merges, 1)] = m;
+      }
+    }
+    for (int p = 0; p < n; p++) {
+      const int a = j.a + p * chunk, b = min(j.b, a + chunk);
+      const int at = atomicAdd(&s_count[bucket(b - a, j.mode)], 1);
+      P.items[at] = Item{j.row0, j.nrows, j.table, a, max(a, b), rec < 0 ? -1 : rec + p * P.c.n_kv_heads * nq, j.lim0, j.mode};
+    }
+  }
+  __syncthreads();
+  if (PREFIX) {
+    __threadfence_block();
+    for (int i = tid; i < s_merges; i += kPlanWG) {
+      Merge& m = P.merges[i];
+      if (m.pieces[0] < 0) {
+        const int4 r = tile_rec[m.queries[0]];
+        m.rec[0] = r.x;
+        m.pieces[0] = m.first[0] + m.nrows * P.G <= r.z ? r.y : 0;
+        m.queries[0] = r.z;
+      }
+    }
+  }
+  if (tid == 0) P.count[1] = s_merges;
+}
+
+// Records: o, then (m, l) with m in units of log2.
+struct Records {
+  float* o;
+  float2* ml;
+};
+
+// ------------------------------------------------------------------------------------------ a piece on matrix cores
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(1))) const char gbytes;
+typedef __attribute__((address_space(3))) char lbytes;
+typedef __attribute__((address_space(3))) bf16x4 lbf16x4;
+
+// x as three bf16 values by truncation, whose sum it is exactly (finite x).
+__device__ __forceinline__ void planes3(float x, uint32_t& h, uint32_t& m, uint32_t& l) {
+  const uint32_t a = __float_as_uint(x);
+  const float r1 = x - __uint_as_float(a & 0xffff0000u);
+  const uint32_t b = __float_as_uint(r1);
+  h = a >> 16;
+  m = b >> 16;
+  l = __float_as_uint(r1 - __uint_as_float(b & 0xffff0000u)) >> 16;
+}
+
+constexpr float kLog2e = 1.44269504088896341f;
+
+// A piece of bf16 keys for 32 QB queries a wave. Query j of the tile is row row0 + j / G, head g * G + j % G.
+//   S^T = K Q^T (v_mfma_f32_32x32x16_bf16: lane l supplies 8 consecutive k of A row l % 32 and of B column l % 32, from
+//     k = 8 (l / 32); accumulator register v of lane l is row 8 (v / 4) + 4 (l / 32) + v % 4, column l % 32): lane l
+//     holds 16 of a 32-key block's scores of query l % 32, lane l ^ 32 the others.
+//   The softmax is in powers of two with a running maximum; the sums are only rescaled when the maximum of some query of the wave
+//     has grown by more than 2^8, so p stays below 2^8 (its rounding is relative, the sums are fp32).
+//   O^T += V^T P^T: registers 8 s .. 8 s + 7 of half h are the probabilities of keys 16 s + 4 h + 0..3 and 16 s + 8 + 4 h
+//     + 0..3, which two transposing LDS reads of V rows give as the A operand.
+// bf16 queries: q as it is, the scale in the exponent's FMA, p rounded to bf16 (half a step, 2^-8 of each p: as much as the
+// rounding of the output). fp32 queries: q (scaled in fp32) and p as three exact planes, three products each.
+// WK waves share a tile's 64 keys, 4 / WK the queries. K and V go to LDS by direct loads, two tiles deep, the
+// 16-byte chunks of a row permuted by its key so that neither kind of read meets itself in a bank.
+template <typename T, int DH, int QB, int WK>
+__device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, char* lds) {
+  constexpr int NP = sizeof(T) == 4 ? 3 : 1;
+  constexpr int KT = 64, NT = DH / 32, KS = DH / 16, NCH = DH / 8, NB = KT / 32 / WK;
+  constexpr int KBUF = KT * DH * 2, BUF = 2 * KBUF, LPT = KT * NCH / kWG;
+  constexpr int VROT = DH == 128 ? 2 : 1;  // V: chunk c of key k sits at c ^ (k % 4) << VROT
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
+  const int wk = WK == 1 ? 0 : w % WK, wq = WK == 1 ? w : w / WK;
+  const int g = blockIdx.x, G = A.G, nq = it.nrows * G;
+  const spd_cache& C = A.c;
+  const int last = it.k1 - 1;
+  const int start = it.k0 & ~(kPage - 1), tiles = (it.k1 - start + KT - 1) / KT;
+  const size_t half = (size_t)C.n_kv_heads * kPage * DH;
+  const uint16_t* pool = (const uint16_t*)A.kv + (size_t)g * kPage * DH;
+  const int* table = C.page_table + (size_t)it.table * C.max_pages;
+  const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;  // from scores to exponents
+
+  bf16x8 qf[QB][NP][KS];
+  int lim[QB], row[QB], head[QB];
+  bool mine[QB];
+  const bool active = wq * QB * 32 < nq;
+#pragma unroll
+  for (int b = 0; b < QB; b++) {
+    const int j = (wq * QB + b) * 32 + col, jj = min(j, nq - 1);
+    mine[b] = j < nq;
+    row[b] = it.row0 + jj / G;
+    head[b] = g * G + jj % G;
+    int n = it.lim0 + jj / G;
+    if (it.mode & ITEM_FLAT) {
+      const int s = A.seqs[row[b]];
+      n = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
+    }
+    lim[b] = min(n, it.k1);
+    const T* q = (const T*)A.q + row[b] * A.qs + head[b] * DH + h * 8;
+#pragma unroll
+    for (int s = 0; s < KS; s++) {
+      if constexpr (NP == 1) {
+        qf[b][0][s] = *reinterpret_cast<const bf16x8*>(q + s * 16);
+      } else {
+        float f[8];
+        load8(q + s * 16, f);
+        union { uint16_t u[8]; bf16x8 v; } t[3];
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          uint32_t x, y, z;
+          planes3(f[e] * (A.scale * kLog2e), x, y, z);
+          t[0].u[e] = (uint16_t)x;
+          t[1].u[e] = (uint16_t)y;
+          t[2].u[e] = (uint16_t)z;
+        }
+#pragma unroll
+        for (int p = 0; p < 3; p++) qf[b][p][s] = t[p].v;
+      }
+    }
+  }
+  // keys that every query of the wave attends need no mask
+  int wmin = lim[0];
+#pragma unroll
+  for (int b = 1; b < QB; b++) wmin = min(wmin, lim[b]);
+  int wmax = lim[0];
+#pragma unroll
+  for (int b = 1; b < QB; b++) wmax = max(wmax, lim[b]);
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    wmin = min(wmin, __shfl_xor(wmin, d, 64));
+    wmax = max(wmax, __shfl_xor(wmax, d, 64));
+  }
+  wmin = __builtin_amdgcn_readfirstlane(wmin);
+  wmax = __builtin_amdgcn_readfirstlane(wmax);
+
+  // The four pages of a tile, one a lane (mod 4), are read a tile ahead of their use.
+  auto pages = [&](int t) { return page_to_read(C, table[min(start / kPage + t * (KT / kPage) + (lane & 3), last / kPage)]); };
+  // Keys outside [k0, k1) are read as the nearest one inside: their probability is 0, and 0 times a value must be 0.
+  auto issue = [&](int buf, int t, int pg) {
+#pragma unroll
+    for (int i = 0; i < LPT; i++) {
+      const int ch = i * kWG + tid, k = ch / NCH, key = start + t * KT + k;
+      const int page = __builtin_amdgcn_readlane(pg, (i * kWG + w * 64) / (NCH * kPage));
+      const int in = min(max(key, it.k0), last) % kPage;
+      const uint16_t* p = pool + (size_t)page * 2 * half + in * DH;
+      lbytes* to = (lbytes*)(lds + buf * BUF + (i * kWG + w * 64) * 16);
+      __builtin_amdgcn_global_load_lds((gbytes*)(p + (ch % NCH ^ (k & 7)) * 8), to, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gbytes*)(p + half + (ch % NCH ^ (k & 3) << VROT) * 8), to + KBUF, 16, 0, 0);
+    }
+  };
+
+  f32x16 o[QB][NT];
+  float m_run[QB], l_run[QB];
+#pragma unroll
+  for (int b = 0; b < QB; b++) {
+    m_run[b] = -INFINITY;
+    l_run[b] = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; t++) o[b][t] = (f32x16)(0.f);
+  }
+  int pg = 0;
+  if (tiles > 0) {
+    pg = pages(0);
+    issue(0, 0, pg);
+    pg = pages(1);
+  }
+  for (int t = 0; t < tiles; t++) {
+    const int buf = t & 1;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t + 1 < tiles) {
+      issue(buf ^ 1, t + 1, pg);
+      pg = pages(t + 2);
+    }
+    const char* kt = lds + buf * BUF;
+    const char* vt = kt + KBUF;
+    if (!active) continue;
+#pragma unroll 1
+    for (int nb = 0; nb < NB; nb++) {
+      const int blk = NB == 1 ? wk : nb, kb = start + t * KT + blk * 32;  // the block's first key
+      if (kb >= wmax) continue;
+      f32x16 s[QB];
+      const int key = blk * 32 + col;
+#pragma unroll
+      for (int k = 0; k < KS; k++) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + key * DH * 2 + (((2 * k + h) ^ (col & 7)) << 4));
+#pragma unroll
+        for (int b = 0; b < QB; b++)
+#pragma unroll
+          for (int p = NP - 1; p >= 0; p--)
+            s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[b][p][k], (p == NP - 1 && k == 0) ? (f32x16)(0.f) : s[b], 0, 0, 0);
+      }
+      union { uint32_t u[8]; bf16x8 f[2]; } pf[QB][NP];
+#pragma unroll
+      for (int b = 0; b < QB; b++) {
+        if (kb + 32 > wmin || kb < it.k0) {
+#pragma unroll
+          for (int v = 0; v < 16; v++) {
+            const int kk = kb + 8 * (v >> 2) + 4 * h + (v & 3);
+            s[b][v] = kk < lim[b] && kk >= it.k0 ? s[b][v] : -INFINITY;
+          }
+        }
+        float mx = s[b][0];
+#pragma unroll
+        for (int v = 1; v < 16; v++) mx = fmaxf(mx, s[b][v]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sc;
+        if (__any(mx > m_run[b] + 8.0f)) {  // -inf + 8 is -inf: the first keys of a query come through here
+          const float mn = fmaxf(m_run[b], mx);
+          const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[b] - mn);
+          l_run[b] *= al;
+#pragma unroll
+          for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+            for (int v = 0; v < 16; v++) o[b][tt][v] *= al;
+          m_run[b] = mn;
+        }
+        const float off = m_run[b] == -INFINITY ? 0.f : m_run[b];  // a query without a key yet: every p is 0
+        float ps = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[b][e], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(s[b][e + 1], sc, -off));
+          ps += p0 + p1;
+          if constexpr (NP == 1) {
+            pf[b][0].u[e >> 1] = pack_bf16(p0, p1);
+          } else {
+            const uint32_t h0 = __float_as_uint(p0), h1 = __float_as_uint(p1);
+            const float r0 = p0 - __uint_as_float(h0 & 0xffff0000u), r1 = p1 - __uint_as_float(h1 & 0xffff0000u);
+            const uint32_t m0 = __float_as_uint(r0), m1 = __float_as_uint(r1);
+            const uint32_t l0 = __float_as_uint(r0 - __uint_as_float(m0 & 0xffff0000u));
+            const uint32_t l1 = __float_as_uint(r1 - __uint_as_float(m1 & 0xffff0000u));
+            pf[b][0].u[e >> 1] = __builtin_amdgcn_perm(h1, h0, 0x07060302u);
+            pf[b][1].u[e >> 1] = __builtin_amdgcn_perm(m1, m0, 0x07060302u);
+            pf[b][2].u[e >> 1] = __builtin_amdgcn_perm(l1, l0, 0x07060302u);
+          }
+        }
+        l_run[b] += ps;
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ks++)
+#pragma unroll
+        for (int tt = 0; tt < NT; tt++) {
+          // lane (l % 16) of each 16: 8 bytes of row (l % 16) / 4 of its four keys; it gets dim l % 16 of all four
+          union { bf16x4 q[2]; bf16x8 f; } vf;
+#pragma unroll
+          for (int x = 0; x < 2; x++) {
+            const int vk = blk * 32 + ks * 16 + x * 8 + h * 4 + (lane & 15) / 4;
+            const int c = tt * 4 + (lane & 16) / 8 + (lane & 3) / 2;
+            vf.q[x] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+                (lbf16x4*)(lbytes*)(vt + vk * DH * 2 + ((c ^ (vk & 3) << VROT) << 4) + (lane & 1) * 8));
+          }
+#pragma unroll
+          for (int b = 0; b < QB; b++)
+#pragma unroll
+            for (int p = NP - 1; p >= 0; p--)
+              o[b][tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.f, pf[b][p].f[ks], o[b][tt], 0, 0, 0);
+        }
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < QB; b++) l_run[b] += __shfl_xor(l_run[b], 32, 64);
+
+  __shared__ uint32_t s_bad[4 * QB];  // queries whose result here is not a number
+  if constexpr (WK > 1) {             // the waves of other keys hand their sums to the first
+    __syncthreads();
+    float* ox = (float*)lds + (size_t)wq * (NT * 16 + 2) * 64;
+    if (wk == 1 && active) {
+#pragma unroll
+      for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) ox[(tt * 16 + v) * 64 + lane] = o[0][tt][v];
+      ox[NT * 16 * 64 + lane] = m_run[0];
+      ox[(NT * 16 + 1) * 64 + lane] = l_run[0];
+    }
+    __syncthreads();
+    if (wk == 0 && active) {
+      const float m1 = ox[NT * 16 * 64 + lane], l1 = ox[(NT * 16 + 1) * 64 + lane];
+      const float mn = fmaxf(m_run[0], m1);
+      const float f0 = m_run[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[0] - mn);
+      const float f1 = m1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1 - mn);
+      l_run[0] = l_run[0] * f0 + l1 * f1;
+      m_run[0] = mn;
+#pragma unroll
+      for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) o[0][tt][v] = fmaf(ox[(tt * 16 + v) * 64 + lane], f1, o[0][tt][v] * f0);
+    }
+  }
+  if (tid < 4 * QB) s_bad[tid] = 0u;
+  __syncthreads();
+  if (wk == 0 && active) {
+#pragma unroll
+    for (int b = 0; b < QB; b++) {
+      bool bad = !(l_run[b] > 0.f) && lim[b] > it.k0;  // NaN, or nothing but scores of -inf
+#pragma unroll
+      for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) bad = bad || o[b][tt][v] != o[b][tt][v];
+      const unsigned long long bads = __ballot(bad && mine[b]);
+      if (lane == 0) s_bad[wq * QB + b] = (uint32_t)bads | (uint32_t)(bads >> 32);
+      if (!mine[b]) continue;
+      if (it.rec < 0) {
+        const float inv = lim[b] > 0 ? 1.0f / l_run[b] : 0.f;
+        T* out = (T*)A.out + row[b] * A.os + head[b] * DH + 4 * h;
+#pragma unroll
+        for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+          for (int v = 0; v < 16; v += 4) {
+            const float x[4] = {o[b][tt][v], o[b][tt][v + 1], o[b][tt][v + 2], o[b][tt][v + 3]};
+            store4(out + tt * 32 + 2 * v, x, inv);
+          }
+      } else {
+        const size_t at = (size_t)it.rec + (size_t)g * nq + (wq * QB + b) * 32 + col;
+        float* rec = R.o + at * DH + 4 * h;
+#pragma unroll
+        for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+          for (int v = 0; v < 16; v += 4) {
+            const float x[4] = {o[b][tt][v], o[b][tt][v + 1], o[b][tt][v + 2], o[b][tt][v + 3]};
+            store4(rec + tt * 32 + 2 * v, x, 1.0f);
+          }
+        if (h == 0) R.ml[at] = make_float2(m_run[b], l_run[b]);
+      }
+    }
+  }
+  __syncthreads();  // every result is stored, and the tiles are free
+  for (int i = 0; i < 4 * QB; i++)
+    for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u) {
+      const int j = i * 32 + __builtin_ctz(m), r = it.row0 + j / G, hd = g * G + j % G;
+      int n = it.lim0 + j / G;
+      if (it.mode & ITEM_FLAT) {
+        const int s = A.seqs[r];
+        n = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
+      }
+      plain_piece<T, uint16_t, DH>(A, it, R, r, hd, j, nq, min(n, it.k1), (float*)lds);
+    }
+}
+
+template <typename T, typename KVT, int DH>
+__device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, int r, int head, int j, int nq, int n, float* lds) {
+  const int g = head / A.G, d = 4 * (threadIdx.x % (DH / 4));
+  float a[4] = {0.f, 0.f, 0.f, 0.f}, M = -INFINITY, L = 0.f;
+  bool holds = threadIdx.x < DH / 4;
+  if (n > it.k0)
+    holds = plain_query<T, KVT, DH>(A.c, (const KVT*)A.kv, A.c.page_table + (size_t)it.table * A.c.max_pages, g,
+                                    (const T*)A.q + r * A.qs + head * DH, A.scale, it.k0, n, lds, M, L, a);
+  if (!holds) return;
+  if (it.rec < 0) {
+    store4((T*)A.out + r * A.os + head * DH + d, a, n > 0 ? 1.0f / L : 0.f);
+  } else {
+    const size_t at = (size_t)it.rec + (size_t)g * nq + j;
+    store4(R.o + at * DH + d, a, 1.0f);
+    if (d == 0) R.ml[at] = make_float2(M * kLog2e, L);
   }
 }
 
-template <typename T, typename KVT, int DH>
-__global__ __launch_bounds__(kWG) void k_prompt_plain(SeqArgs A) {
-  __shared__ float lds[kWG * 6];
-  const RowAt at = row_at(A.c, A.seqs, A.cu, A.nseqs, blockIdx.x);
-  if (at.seq < 0) return;
-  const int* table = A.c.page_table + (size_t)at.seq * A.c.max_pages;
-  plain_row<T, KVT, DH>(A, Keys{table, table, 0}, blockIdx.x, blockIdx.y, at.key + 1, lds);
-}
-
-template <typename T, typename KVT, int DH>
-__global__ __launch_bounds__(kWG) void k_prefix_plain(SeqArgs A) {
-  __shared__ float lds[kWG * 6];
-  const int r = blockIdx.x, s = A.seqs[r];
-  if ((unsigned)s >= (unsigned)A.c.max_seqs) return;
-  const int* own = A.c.page_table + (size_t)s * A.c.max_pages;
-  Keys keys{own, own, 0};
-  if (A.ngroups > 0) {
-    const int j = find_last(A.cu, A.ngroups, r), b = A.cu[j];
-    const int f = (unsigned)b < (unsigned)A.nseqs ? A.seqs[b] : -1;
-    if ((unsigned)f < (unsigned)A.c.max_seqs) {
-      keys.first = A.c.page_table + (size_t)f * A.c.max_pages;
-      keys.shared = min(A.prefix[j], seq_len(A.c, f));
+// The same over an fp32 cache, for 32 queries a wave, with v_mfma_f32_32x32x2_f32 (lane l supplies k = l / 32 of A row
+// and B column l % 32; accumulators as above): a lane's four dims of a chunk are four steps, so the halves take chunks in
+// turn. P is used as it is. Tiles of 32 keys.
+template <int DH>
+__device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, char* lds) {
+  constexpr int KT = 32, NT = DH / 32, KS = DH / 8, NCH = DH / 4;
+  constexpr int KBUF = KT * DH * 4, BUF = 2 * KBUF, LPT = KT * NCH / kWG;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
+  const int g = blockIdx.x, G = A.G, nq = it.nrows * G;
+  const spd_cache& C = A.c;
+  const int last = it.k1 - 1;
+  const int start = it.k0 & ~(kPage - 1), tiles = (it.k1 - start + KT - 1) / KT;
+  const size_t half = (size_t)C.n_kv_heads * kPage * DH;
+  const float* pool = (const float*)A.kv + (size_t)g * kPage * DH;
+  const int* table = C.page_table + (size_t)it.table * C.max_pages;
+  const bool active = w * 32 < nq;
+  const int j = w * 32 + col, jj = min(j, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
+  const bool mine = j < nq;
+  int lim = it.lim0 + jj / G;
+  if (it.mode & ITEM_FLAT) {
+    const int s = A.seqs[row];
+    lim = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
+  }
+  lim = min(lim, it.k1);
+  float4 qf[KS];
+  {
+    const float* q = (const float*)A.q + row * A.qs + head * DH + h * 4;
+#pragma unroll
+    for (int s = 0; s < KS; s++) {
+      const float4 x = *reinterpret_cast<const float4*>(q + s * 8);
+      const float f = A.scale * kLog2e;
+      qf[s] = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
     }
   }
-  plain_row<T, KVT, DH>(A, keys, r, blockIdx.y, seq_len(A.c, s), lds);
+  auto pages = [&](int t) { return page_to_read(C, table[min(start / kPage + t * (KT / kPage) + (lane & 1), last / kPage)]); };
+  auto issue = [&](int buf, int t, int pg) {
+#pragma unroll
+    for (int i = 0; i < LPT; i++) {
+      const int ch = i * kWG + tid, k = ch / NCH, key = start + t * KT + k;
+      const int page = __builtin_amdgcn_readlane(pg, (i * kWG + w * 64) / (NCH * kPage));
+      const int in = min(max(key, it.k0), last) % kPage;
+      const float* p = pool + (size_t)page * 2 * half + in * DH;
+      lbytes* to = (lbytes*)(lds + buf * BUF + (i * kWG + w * 64) * 16);
+      __builtin_amdgcn_global_load_lds((gbytes*)(p + (ch % NCH ^ (k & 7)) * 4), to, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gbytes*)(p + half + (ch % NCH ^ (k >> 2 & 1) << 3) * 4), to + KBUF, 16, 0, 0);
+    }
+  };
+  f32x16 o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; t++) o[t] = (f32x16)(0.f);
+  float m_run = -INFINITY, l_run = 0.f;
+  int pg = 0;
+  if (tiles > 0) {
+    pg = pages(0);
+    issue(0, 0, pg);
+    pg = pages(1);
+  }
+  for (int t = 0; t < tiles; t++) {
+    const int buf = t & 1;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t + 1 < tiles) {
+      issue(buf ^ 1, t + 1, pg);
+      pg = pages(t + 2);
+    }
+    const char* kt = lds + buf * BUF;
+    const char* vt = kt + KBUF;
+    const int kb = start + t * KT;
+    if (!active || !__any(kb < lim)) continue;
+    f32x16 s = (f32x16)(0.f);
+#pragma unroll
+    for (int k = 0; k < KS; k++) {
+      const float4 kf = *reinterpret_cast<const float4*>(kt + col * DH * 4 + (((2 * k + h) ^ (col & 7)) << 4));
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.x, qf[k].x, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.y, qf[k].y, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.z, qf[k].z, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.w, qf[k].w, s, 0, 0, 0);
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < 16; v++) {
+      const int kk = kb + 8 * (v >> 2) + 4 * h + (v & 3);
+      s[v] = kk < lim && kk >= it.k0 ? s[v] : -INFINITY;
+      mx = fmaxf(mx, s[v]);
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    if (__any(mx > m_run + 8.0f)) {
+      const float mn = fmaxf(m_run, mx);
+      const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - mn);
+      l_run *= al;
+#pragma unroll
+      for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) o[tt][v] *= al;
+      m_run = mn;
+    }
+    const float off = m_run == -INFINITY ? 0.f : m_run;
+    float ps = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; v++) {
+      s[v] = __builtin_amdgcn_exp2f(s[v] - off);
+      ps += s[v];
+    }
+    l_run += ps;
+#pragma unroll
+    for (int v = 0; v < 16; v++) {
+      const int vk = 8 * (v >> 2) + 4 * h + (v & 3);
+#pragma unroll
+      for (int tt = 0; tt < NT; tt++) {
+        const float vf = *reinterpret_cast<const float*>(vt + vk * DH * 4 + (((tt * 8 + col / 4) ^ h << 3) << 4) + (col & 3) * 4);
+        o[tt] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[v], o[tt], 0, 0, 0);
+      }
+    }
+  }
+  l_run += __shfl_xor(l_run, 32, 64);
+  __shared__ uint32_t s_bad[4];
+  if (tid < 4) s_bad[tid] = 0u;
+  __syncthreads();
+  if (active) {
+    bool bad = !(l_run > 0.f) && lim > it.k0;
+#pragma unroll
+    for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) bad = bad || o[tt][v] != o[tt][v];
+    const unsigned long long bads = __ballot(bad && mine);
+    if (lane == 0) s_bad[w] = (uint32_t)bads | (uint32_t)(bads >> 32);
+    if (mine) {
+      const size_t at = (size_t)it.rec + (size_t)g * nq + j;
+      float* to = it.rec < 0 ? (float*)A.out + row * A.os + head * DH + 4 * h : R.o + at * DH + 4 * h;
+      const float f = it.rec >= 0 ? 1.0f : lim > 0 ? 1.0f / l_run : 0.f;
+#pragma unroll
+      for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4) {
+          const float x[4] = {o[tt][v], o[tt][v + 1], o[tt][v + 2], o[tt][v + 3]};
+          store4(to + tt * 32 + 2 * v, x, f);
+        }
+      if (it.rec >= 0 && h == 0) R.ml[at] = make_float2(m_run, l_run);
+    }
+  }
+  __syncthreads();
+  for (int i = 0; i < 4; i++)
+    for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u) {
+      const int jb = i * 32 + __builtin_ctz(m), r = it.row0 + jb / G;
+      int n = it.lim0 + jb / G;
+      if (it.mode & ITEM_FLAT) {
+        const int s = A.seqs[r];
+        n = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
+      }
+      plain_piece<float, float, DH>(A, it, R, r, g * G + jb % G, jb, nq, min(n, it.k1), (float*)lds);
+    }
 }
 
-template <typename T, typename KVT, int DH>
-void launch_plain(const SeqArgs& a, bool prefix, hipStream_t s) {
+// Grid: x = KV head (with 8 of them a head's keys stay in one XCD's L2), y = piece.
+template <typename T, int DH, int QB>
+__global__ __launch_bounds__(kWG, QB == 1 ? 2 : 1) void k_attend_bf16(SeqArgs A, const int* count, const Item* items, Records R) {
+  extern __shared__ __align__(16) char lds[];
+  if ((int)blockIdx.y >= count[0]) return;
+  const Item it = items[blockIdx.y];
+  if (it.mode & ITEM_NARROW)
+    piece_bf16<T, DH, 1, 2>(A, it, R, lds);
+  else
+    piece_bf16<T, DH, QB, 1>(A, it, R, lds);
+}
+
+template <int DH>
+__global__ __launch_bounds__(kWG, 2) void k_attend_f32(SeqArgs A, const int* count, const Item* items, Records R) {
+  extern __shared__ __align__(16) char lds[];
+  if ((int)blockIdx.y >= count[0]) return;
+  piece_f32<DH>(A, items[blockIdx.y], R, lds);
+}
+
+// Records to outputs. Grid: x = KV head, y = rows to join, z = every kMergeZ-th set of queries.
+constexpr int kMergeZ = 4;
+
+template <typename T, int DH>
+__global__ __launch_bounds__(kWG) void k_merge(SeqArgs A, const int* count, const Merge* merges, Records R) {
+  if ((int)blockIdx.y >= count[1]) return;
+  const Merge m = merges[blockIdx.y];
+  constexpr int TPQ = DH / 4, QPI = kWG / TPQ;
+  const int g = blockIdx.x, G = A.G, d = 4 * (threadIdx.x % TPQ);
+  for (int j = blockIdx.z * QPI + threadIdx.x / TPQ; j < m.nrows * G; j += kMergeZ * QPI) {
+    const int r = m.row0 + j / G, head = g * G + j % G;
+    int lim = m.lim0 + j / G;
+    if (m.mode & ITEM_FLAT) lim = seq_len(A.c, A.seqs[r]);
+    float M = -INFINITY;
+    for (int x = 0; x < 2; x++)
+      for (int p = 0; p < m.pieces[x]; p++)
+        M = fmaxf(M, R.ml[(size_t)m.rec[x] + (size_t)(p * A.c.n_kv_heads + g) * m.queries[x] + m.first[x] + j].x);
+    float a[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
+    for (int x = 0; x < 2; x++)
+      for (int p = 0; p < m.pieces[x]; p++) {
+        const size_t at = (size_t)m.rec[x] + (size_t)(p * A.c.n_kv_heads + g) * m.queries[x] + m.first[x] + j;
+        const float2 ml = R.ml[at];
+        if (ml.y == 0.f) continue;  // no key of this row; a sum that is NaN goes on
+        const float f = __builtin_amdgcn_exp2f(ml.x - M);
+        const float4 o = *reinterpret_cast<const float4*>(R.o + at * DH + d);
+        L = fmaf(ml.y, f, L);
+        a[0] = fmaf(o.x, f, a[0]);
+        a[1] = fmaf(o.y, f, a[1]);
+        a[2] = fmaf(o.z, f, a[2]);
+        a[3] = fmaf(o.w, f, a[3]);
+      }
+    store4((T*)A.out + r * A.os + head * DH + d, a, lim > 0 ? 1.0f / L : 0.f);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------- launches
+// What a call takes: its tiles, and its workspace (the plan's lists, then the records).
+struct Request {
+  int qb, rpt, wanted, jobs, tiles;
+  size_t items, merges, records;
+  size_t at_items, at_merges, at_tiles, at_ml, at_o, bytes;
+};
+
+Request request(const spd_cache& c, int n_q_heads, int dtype, int nseqs, int rows, int ngroups, bool prefix) {
+  Request q{};
+  const int hkv = c.n_kv_heads, G = n_q_heads / hkv;
+  q.qb = !prefix && dtype == SPD_BF16 && (long long)rows * n_q_heads >= 512ll * 256 ? 2 : 1;
+  q.rpt = 128 * q.qb / G;
+  q.wanted = std::max(1, kWantedWGs / hkv);
+  if (prefix) {
+    q.tiles = ngroups > 0 ? nseqs / q.rpt + ngroups : 0;
+    q.jobs = q.tiles + nseqs;
+    q.merges = nseqs;
+  } else {
+    q.jobs = rows / q.rpt + nseqs;
+    q.merges = q.wanted;
+  }
+  // jobs over `chunk` >= keys / wanted: fewer than `wanted` of them, with fewer than 2 `wanted` pieces
+  q.items = (size_t)q.jobs + 2 * q.wanted;
+  q.records = 2 * (size_t)q.wanted * hkv * std::min(q.rpt, rows) * G;
+  if (prefix) q.records += 2 * (size_t)nseqs * n_q_heads;
+  auto take = [&](size_t n) {
+    const size_t at = q.bytes;
+    q.bytes += (n + 255) / 256 * 256;
+    return at;
+  };
+  take(64);  // counts
+  q.at_items = take(q.items * sizeof(Item));
+  q.at_merges = take(q.merges * sizeof(Merge));
+  q.at_tiles = take((size_t)q.tiles * sizeof(int4));
+  q.at_ml = take(q.records * sizeof(float2));
+  q.at_o = take(q.records * c.head_dim * sizeof(float));
+  return q;
+}
+
+template <typename T, int DH>
+void launch_merge(const SeqArgs& a, const Request& q, const int* count, const Merge* merges, const Records& r, hipStream_t s) {
+  hipLaunchKernelGGL((k_merge<T, DH>), dim3(a.c.n_kv_heads, (unsigned)q.merges, kMergeZ), dim3(kWG), 0, s, a, count, merges, r);
+}
+
+template <typename T, int DH>
+void launch_bf16(const SeqArgs& a, const Request& q, const int* count, const Item* items, const Records& r, hipStream_t s) {
+  const dim3 grid(a.c.n_kv_heads, (unsigned)q.items);
+  const size_t shm = 2 * 2 * 64 * DH * 2;
+  if constexpr (sizeof(T) == 2) {
+    if (q.qb == 2) {
+      hipLaunchKernelGGL((k_attend_bf16<T, DH, 2>), grid, dim3(kWG), shm, s, a, count, items, r);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((k_attend_bf16<T, DH, 1>), grid, dim3(kWG), shm, s, a, count, items, r);
+}
+
+// Plan, pieces, merge.
+void run_attention(const SeqArgs& a, int dtype, const Request& q, bool prefix, void* workspace, hipStream_t s) {
+  char* ws = (char*)workspace;
+  PlanArgs p{};
+  p.c = a.c;
+  p.seqs = a.seqs;
+  p.cu = a.cu;
+  p.prefix = a.prefix;
+  p.nseqs = a.nseqs;
+  p.rows = a.rows;
+  p.ngroups = a.ngroups;
+  p.G = a.G;
+  p.wanted = q.wanted;
+  p.rpt = q.rpt;
+  p.records = q.records;
+  p.count = (int*)ws;
+  p.items = (Item*)(ws + q.at_items);
+  p.merges = (Merge*)(ws + q.at_merges);
+  int4* tiles = (int4*)(ws + q.at_tiles);
+  const Records r{(float*)(ws + q.at_o), (float2*)(ws + q.at_ml)};
   if (prefix)
-    hipLaunchKernelGGL((k_prefix_plain<T, KVT, DH>), dim3(a.nseqs, a.c.n_kv_heads), dim3(kWG), 0, s, a);
+    hipLaunchKernelGGL((k_plan_attention<true>), dim3(1), dim3(kPlanWG), 0, s, p, q.jobs, q.tiles, tiles);
   else
-    hipLaunchKernelGGL((k_prompt_plain<T, KVT, DH>), dim3(a.rows, a.c.n_kv_heads), dim3(kWG), 0, s, a);
-}
-
-void launch_plain_typed(const SeqArgs& a, int dtype, bool prefix, hipStream_t s) {
+    hipLaunchKernelGGL((k_plan_attention<false>), dim3(1), dim3(kPlanWG), 0, s, p, q.jobs, q.tiles, tiles);
   const bool wide = a.c.head_dim == 128;
+  if (a.c.dtype == SPD_F32) {
+    const dim3 grid(a.c.n_kv_heads, (unsigned)q.items);
+    const size_t shm = (size_t)2 * 2 * 32 * a.c.head_dim * 4;
+    if (wide)
+      hipLaunchKernelGGL(k_attend_f32<128>, grid, dim3(kWG), shm, s, a, p.count, p.items, r);
+    else
+      hipLaunchKernelGGL(k_attend_f32<64>, grid, dim3(kWG), shm, s, a, p.count, p.items, r);
+  } else if (dtype == SPD_BF16) {
+    wide ? launch_bf16<uint16_t, 128>(a, q, p.count, p.items, r, s) : launch_bf16<uint16_t, 64>(a, q, p.count, p.items, r, s);
+  } else {
+    wide ? launch_bf16<float, 128>(a, q, p.count, p.items, r, s) : launch_bf16<float, 64>(a, q, p.count, p.items, r, s);
+  }
   if (dtype == SPD_BF16)
-    wide ? launch_plain<uint16_t, uint16_t, 128>(a, prefix, s) : launch_plain<uint16_t, uint16_t, 64>(a, prefix, s);
-  else if (a.c.dtype == SPD_BF16)
-    wide ? launch_plain<float, uint16_t, 128>(a, prefix, s) : launch_plain<float, uint16_t, 64>(a, prefix, s);
+    wide ? launch_merge<uint16_t, 128>(a, q, p.count, p.merges, r, s) : launch_merge<uint16_t, 64>(a, q, p.count, p.merges, r, s);
   else
-    wide ? launch_plain<float, float, 128>(a, prefix, s) : launch_plain<float, float, 64>(a, prefix, s);
+    wide ? launch_merge<float, 128>(a, q, p.count, p.merges, r, s) : launch_merge<float, 64>(a, q, p.count, p.merges, r, s);
 }
 
 // What both attentions check of their sizes.
@@ -238,7 +1078,7 @@ extern "C" spd_status spd_prompt_attention_workspace(const spd_cache* c, int32_t
   const spd_status st = check_sizes(call, c, n_q_heads, dtype, nseqs, max_len);
   if (st != SPD_OK) return st;
   if (!bytes || rows < 0) return invalid(call, "NULL pointer or negative rows");
-  *bytes = 0;
+  *bytes = request(*c, n_q_heads, dtype, nseqs, rows, 0, false).bytes;
   return SPD_OK;
 }
 
@@ -259,7 +1099,7 @@ extern "C" spd_status spd_prompt_attention(const spd_cache* c, int32_t layer, co
   SeqArgs a = args_of(c, layer, q, q_stride, out, out_stride, n_q_heads, seqs, nseqs);
   a.cu = cu_rows;
   a.rows = rows;
-  launch_plain_typed(a, dtype, false, (hipStream_t)stream);
+  run_attention(a, dtype, request(*c, n_q_heads, dtype, nseqs, rows, 0, false), false, workspace, (hipStream_t)stream);
   return check_launch(call);
 }
 
@@ -270,7 +1110,7 @@ extern "C" spd_status spd_prefix_attention_workspace(const spd_cache* c, int32_t
   if (st != SPD_OK) return st;
   if (nseqs > 4096) return invalid(call, "nseqs must be at most 4096");
   if (!bytes || ngroups < 0 || ngroups > nseqs) return invalid(call, "NULL pointer, or ngroups outside [0, nseqs]");
-  *bytes = 0;
+  *bytes = request(*c, n_q_heads, dtype, nseqs, nseqs, ngroups, true).bytes;
   return SPD_OK;
 }
 
@@ -292,6 +1132,6 @@ extern "C" spd_status spd_prefix_attention(const spd_cache* c, int32_t layer, co
   a.prefix = prefix_lens;
   a.ngroups = ngroups;
   a.rows = nseqs;
-  launch_plain_typed(a, dtype, true, (hipStream_t)stream);
+  run_attention(a, dtype, request(*c, n_q_heads, dtype, nseqs, nseqs, ngroups, true), true, workspace, (hipStream_t)stream);
   return check_launch(call);
 }

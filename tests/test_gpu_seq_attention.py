@@ -70,6 +70,29 @@ def test_more_sequences_than_a_wave(types):
     run_prompt([rng.choice([0, 1, 1, 2, 5]) for _ in range(150)], [rng.choice([0, 0, 3, 40]) for _ in range(150)], (4, 2, 64), types)
 
 
+@pytest.mark.parametrize("heads,rows,cached", [((128, 8, 64), [700, 1, 450], [0, 70, 333]), ((64, 8, 128), [1, 2300, 33], [5, 0, 1000]),
+                                               ((96, 16, 128), [1500, 15], [7, 0])], ids=str)
+def test_batches_of_many_rows(heads, rows, cached):
+    """Past the size from which a wave takes 64 queries; rows at the tiles' edges and a few others are compared."""
+    from tests.seqcache import attend, check, filled, i32
+    hq, hkv, dh = heads
+    assert sum(rows) * hq >= 512 * 256
+    lens = [r + c for r, c in zip(rows, cached)]
+    cache, kv = filled(lens, hkv, dh, torch.bfloat16, 21)
+    cu = [0]
+    for r in rows:
+        cu.append(cu[-1] + r)
+    q = (1.5 * torch.randn(cu[-1], hq, dh, generator=torch.Generator().manual_seed(22))).bfloat16()
+    out = cache.prompt_attention(0, q.cuda(), i32(list(range(len(rows)))), i32(cu)).cpu()
+    assert torch.isfinite(out).all()
+    G = hq // hkv
+    for i, n in enumerate(rows):
+        rpt = 256 // G
+        pick = sorted({r for r in (0, 1, rpt - 1, rpt, 3 * rpt - 1, n // 2, n - 2, n - 1) if 0 <= r < n})
+        want, mag = attend(q[cu[i]:cu[i + 1]][pick], kv[i][0, 0], kv[i][0, 1], [cached[i] + r + 1 for r in pick])
+        check(out[cu[i]:cu[i + 1]][pick], want, mag, ("bf16", i))
+
+
 def run_prefix(groups, prefix, lens, heads, types, seed=0, max_len=0, pad=0, use_groups=True):
     """Groups of rows that agree in their first prefix keys (in pages of their own: only the first row's are read)."""
     from tests.seqcache import attend, check, filled, i32
