@@ -419,22 +419,24 @@ __device__ __forceinline__ void planes3(float x, uint32_t& h, uint32_t& m, uint3
 
 constexpr float kLog2e = 1.44269504088896341f;
 
-// A piece of bf16 keys for 32 QB queries a wave. Query j of the tile is row row0 + j / G, head g * G + j % G.
+// A piece of bf16 keys for 32 queries a wave. Query j of the tile is row row0 + j / G, head g * G + j % G.
 //   S^T = K Q^T (v_mfma_f32_32x32x16_bf16: lane l supplies 8 consecutive k of A row l % 32 and of B column l % 32, from
 //     k = 8 (l / 32); accumulator register v of lane l is row 8 (v / 4) + 4 (l / 32) + v % 4, column l % 32): lane l
 //     holds 16 of a 32-key block's scores of query l % 32, lane l ^ 32 the others.
-//   The softmax is in powers of two with a running maximum; the sums are only rescaled when the maximum of some query of the wave
-//     has grown by more than 2^8, so p stays below 2^8 (its rounding is relative, the sums are fp32).
+//   The softmax is in powers of two. Its offset m is a maximum that is only renewed, and the sums rescaled, when a score of some
+//     query of the wave exceeds it by more than 8: p stays below 2^8, its rounding is relative and the sums are
+//     fp32, and the other steps need neither the other half's scores nor a rescaling.
 //   O^T += V^T P^T: registers 8 s .. 8 s + 7 of half h are the probabilities of keys 16 s + 4 h + 0..3 and 16 s + 8 + 4 h
 //     + 0..3, which two transposing LDS reads of V rows give as the A operand.
 // bf16 queries: q as it is, the scale in the exponent's FMA, p rounded to bf16 (half a step, 2^-8 of each p: as much as the
-// rounding of the output). fp32 queries: q (scaled in fp32) and p as three exact planes, three products each.
+// rounding of the output), l the sum of the rounded p. fp32 queries: q (scaled in fp32) and p as three exact planes, three products each.
 // WK waves share a tile's 64 keys, 4 / WK the queries. K and V go to LDS by direct loads, two tiles deep, the
 // 16-byte chunks of a row permuted by its key so that neither kind of read meets itself in a bank.
-template <typename T, int DH, int QB, int WK>
+template <typename T, int DH, int WK>
 __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, char* lds) {
   constexpr int NP = sizeof(T) == 4 ? 3 : 1;
   constexpr int KT = 64, NT = DH / 32, KS = DH / 16, NCH = DH / 8, NB = KT / 32 / WK;
+  constexpr int SB = NP == 1 ? NB : 1;  // 32-key blocks of a step (with three planes two spill)
   constexpr int KBUF = KT * DH * 2, BUF = 2 * KBUF, LPT = KT * NCH / kWG;
   constexpr int VROT = DH == 128 ? 2 : 1;  // V: chunk c of key k sits at c ^ (k % 4) << VROT
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
@@ -447,28 +449,23 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
   const uint16_t* pool = (const uint16_t*)A.kv + (size_t)g * kPage * DH;
   const int* table = C.page_table + (size_t)it.table * C.max_pages;
   const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;  // from scores to exponents
+  const bool active = wq * 32 < nq;
+  const int jq = wq * 32 + col, jj = min(jq, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
+  const bool mine = jq < nq;
+  int lim = it.lim0 + jj / G;
+  if (it.mode & ITEM_FLAT) {
+    const int s = A.seqs[row];
+    lim = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
+  }
+  lim = min(lim, it.k1);
 
-  bf16x8 qf[QB][NP][KS];
-  int lim[QB], row[QB], head[QB];
-  bool mine[QB];
-  const bool active = wq * QB * 32 < nq;
-#pragma unroll
-  for (int b = 0; b < QB; b++) {
-    const int j = (wq * QB + b) * 32 + col, jj = min(j, nq - 1);
-    mine[b] = j < nq;
-    row[b] = it.row0 + jj / G;
-    head[b] = g * G + jj % G;
-    int n = it.lim0 + jj / G;
-    if (it.mode & ITEM_FLAT) {
-      const int s = A.seqs[row[b]];
-      n = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
-    }
-    lim[b] = min(n, it.k1);
-    const T* q = (const T*)A.q + row[b] * A.qs + head[b] * DH + h * 8;
+  bf16x8 qf[NP][KS];
+  {
+    const T* q = (const T*)A.q + row * A.qs + head * DH + h * 8;
 #pragma unroll
     for (int s = 0; s < KS; s++) {
       if constexpr (NP == 1) {
-        qf[b][0][s] = *reinterpret_cast<const bf16x8*>(q + s * 16);
+        qf[0][s] = *reinterpret_cast<const bf16x8*>(q + s * 16);
       } else {
         float f[8];
         load8(q + s * 16, f);
@@ -482,17 +479,12 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
           t[2].u[e] = (uint16_t)z;
         }
 #pragma unroll
-        for (int p = 0; p < 3; p++) qf[b][p][s] = t[p].v;
+        for (int p = 0; p < 3; p++) qf[p][s] = t[p].v;
       }
     }
   }
-  // keys that every query of the wave attends need no mask
-  int wmin = lim[0];
-#pragma unroll
-  for (int b = 1; b < QB; b++) wmin = min(wmin, lim[b]);
-  int wmax = lim[0];
-#pragma unroll
-  for (int b = 1; b < QB; b++) wmax = max(wmax, lim[b]);
+  // keys below wmin are attended by every query of the wave, none at wmax and above by any
+  int wmin = lim, wmax = lim;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     wmin = min(wmin, __shfl_xor(wmin, d, 64));
@@ -503,29 +495,128 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
 
   // The four pages of a tile, one a lane (mod 4), are read a tile ahead of their use.
   auto pages = [&](int t) { return page_to_read(C, table[min(start / kPage + t * (KT / kPage) + (lane & 3), last / kPage)]); };
-  // Keys outside [k0, k1) are read as the nearest one inside: their probability is 0, and 0 times a value must be 0.
+  // A thread's bytes of a page, load i: chunk ch % NCH of key ch / NCH. All loads of a thread are of the same key of a page,
+  // or of keys 16 apart, so one offset serves them.
+  const int lk = tid / NCH, lc = tid % NCH;
+  static_assert(kWG / NCH % kPage == 0, "a pass of the workgroup is whole pages");
+  const uint32_t koff = (lk % kPage) * DH * 2 + ((lc ^ (lk & 7)) << 4);
+  const uint32_t voff = (lk % kPage) * DH * 2 + ((lc ^ (lk & 3) << VROT) << 4);
+  const size_t page_bytes = 2 * half * sizeof(uint16_t);
+  auto load_tile = [&](int buf, int t, int pg, uint32_t ko, uint32_t vo, int i) {
+    const int page = __builtin_amdgcn_readlane(pg, (i * kWG + w * 64) / (NCH * kPage));
+    gbytes* p = (gbytes*)pool + (size_t)page * page_bytes;
+    lbytes* to = (lbytes*)(lds + buf * BUF + (i * kWG + w * 64) * 16);
+    __builtin_amdgcn_global_load_lds(p + ko, to, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds(p + half * sizeof(uint16_t) + vo, to + KBUF, 16, 0, 0);
+  };
   auto issue = [&](int buf, int t, int pg) {
+    const int first = start + t * KT;
+    if (first >= it.k0 && first + KT <= it.k1) {
 #pragma unroll
-    for (int i = 0; i < LPT; i++) {
-      const int ch = i * kWG + tid, k = ch / NCH, key = start + t * KT + k;
-      const int page = __builtin_amdgcn_readlane(pg, (i * kWG + w * 64) / (NCH * kPage));
-      const int in = min(max(key, it.k0), last) % kPage;
-      const uint16_t* p = pool + (size_t)page * 2 * half + in * DH;
-      lbytes* to = (lbytes*)(lds + buf * BUF + (i * kWG + w * 64) * 16);
-      __builtin_amdgcn_global_load_lds((gbytes*)(p + (ch % NCH ^ (k & 7)) * 8), to, 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((gbytes*)(p + half + (ch % NCH ^ (k & 3) << VROT) * 8), to + KBUF, 16, 0, 0);
+      for (int i = 0; i < LPT; i++) load_tile(buf, t, pg, koff, voff, i);
+    } else {
+      // Keys outside [k0, k1) are read as the nearest one inside: their probability is 0, and 0 times a value must be 0.
+#pragma unroll
+      for (int i = 0; i < LPT; i++) {
+        const int k = i * (kWG / NCH) + lk;
+        const uint32_t in = (min(max(first + k, it.k0), last) % kPage) * DH * 2;
+        load_tile(buf, t, pg, in + (koff & (DH * 2 - 1)), in + (voff & (DH * 2 - 1)), i);
+      }
+    }
+  };
+  // A lane's bytes of a K or V tile.
+  uint32_t ka[4], va[NT];
+#pragma unroll
+  for (int k = 0; k < 4; k++) ka[k] = (WK == 1 ? 0 : wk * 32 * DH * 2) + col * DH * 2 + (((2 * k + h) ^ (col & 7)) << 4);
+#pragma unroll
+  for (int tt = 0; tt < NT; tt++) {
+    // lane l % 16 of each 16: 8 bytes of row (l % 16) / 4 of its four keys; it gets dim l % 16 of all four
+    const int vk = (WK == 1 ? 0 : wk * 32) + h * 4 + (lane & 15) / 4, c = tt * 4 + (lane & 16) / 8 + (lane & 3) / 2;
+    va[tt] = KBUF + vk * DH * 2 + ((c ^ (vk & 3) << VROT) << 4) + (lane & 1) * 8;
+  }
+
+  f32x16 o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; t++) o[t] = (f32x16)(0.f);
+  float m_run = -INFINITY, l_run = 0.f;
+
+  // SB blocks from key kb on, the first of them `at` bytes into the tile
+  auto step = [&](const char* tile, int at, int kb) {
+    f32x16 s[SB];
+#pragma unroll
+    for (int x = 0; x < SB; x++)
+#pragma unroll
+      for (int k = 0; k < KS; k++) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + ka[k & 3] + at + x * 32 * DH * 2 + (k >> 2) * 128);
+#pragma unroll
+        for (int p = NP - 1; p >= 0; p--)
+          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[p][k], (p == NP - 1 && k == 0) ? (f32x16)(0.f) : s[x], 0, 0, 0);
+      }
+    if (kb < it.k0 || kb + SB * 32 > wmin) {  // some key is not every query's
+      asm volatile("");                       // stays a branch: the masks cost a fifth of the step's vector work
+#pragma unroll
+      for (int x = 0; x < SB; x++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) {
+          const int kk = kb + x * 32 + 8 * (v >> 2) + 4 * h + (v & 3);
+          s[x][v] = kk < lim && kk >= it.k0 ? s[x][v] : -INFINITY;
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int x = 0; x < SB; x++)
+#pragma unroll
+      for (int v = 0; v < 16; v += 2) mx = fmaxf(fmaxf(mx, s[x][v]), s[x][v + 1]);
+    mx *= sc;
+    if (__any(mx > m_run + 8.0f)) {  // -inf + 8 is -inf: the first keys of a query come through here
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float mn = fmaxf(m_run, mx);
+      const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - mn);
+      l_run *= al;
+#pragma unroll
+      for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) o[tt][v] *= al;
+      m_run = mn;
+    }
+    const float off = m_run == -INFINITY ? 0.f : m_run;  // a query without a key yet: every p is 0
+    union { uint32_t u[8]; bf16x8 f[2]; } pf[SB][NP];
+#pragma unroll
+    for (int x = 0; x < SB; x++) {
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[x][e], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(s[x][e + 1], sc, -off));
+        if constexpr (NP == 1) {
+          pf[x][0].u[e >> 1] = pack_bf16(p0, p1);
+          l_run += p0 + p1;
+        } else {
+          l_run += p0 + p1;
+          const uint32_t h0 = __float_as_uint(p0), h1 = __float_as_uint(p1);
+          const float r0 = p0 - __uint_as_float(h0 & 0xffff0000u), r1 = p1 - __uint_as_float(h1 & 0xffff0000u);
+          const uint32_t m0 = __float_as_uint(r0), m1 = __float_as_uint(r1);
+          const uint32_t l0 = __float_as_uint(r0 - __uint_as_float(m0 & 0xffff0000u));
+          const uint32_t l1 = __float_as_uint(r1 - __uint_as_float(m1 & 0xffff0000u));
+          pf[x][0].u[e >> 1] = __builtin_amdgcn_perm(h1, h0, 0x07060302u);
+          pf[x][1].u[e >> 1] = __builtin_amdgcn_perm(m1, m0, 0x07060302u);
+          pf[x][2].u[e >> 1] = __builtin_amdgcn_perm(l1, l0, 0x07060302u);
+        }
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ks++)
+#pragma unroll
+        for (int tt = 0; tt < NT; tt++) {
+          union { bf16x4 q[2]; bf16x8 f; } vf;
+#pragma unroll
+          for (int y = 0; y < 2; y++)
+            vf.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+                (lbf16x4*)(lbytes*)(tile + va[tt] + at + (x * 32 + ks * 16 + y * 8) * DH * 2));
+#pragma unroll
+          for (int p = NP - 1; p >= 0; p--)
+            o[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.f, pf[x][p].f[ks], o[tt], 0, 0, 0);
+        }
     }
   };
 
-  f32x16 o[QB][NT];
-  float m_run[QB], l_run[QB];
-#pragma unroll
-  for (int b = 0; b < QB; b++) {
-    m_run[b] = -INFINITY;
-    l_run[b] = 0.f;
-#pragma unroll
-    for (int t = 0; t < NT; t++) o[b][t] = (f32x16)(0.f);
-  }
   int pg = 0;
   if (tiles > 0) {
     pg = pages(0);
@@ -539,166 +630,88 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
       issue(buf ^ 1, t + 1, pg);
       pg = pages(t + 2);
     }
-    const char* kt = lds + buf * BUF;
-    const char* vt = kt + KBUF;
+    const char* tile = lds + buf * BUF;
     if (!active) continue;
 #pragma unroll 1
-    for (int nb = 0; nb < NB; nb++) {
-      const int blk = NB == 1 ? wk : nb, kb = start + t * KT + blk * 32;  // the block's first key
+    for (int nb = 0; nb < NB; nb += SB) {
+      const int kb = start + t * KT + (WK == 1 ? nb : wk) * 32;  // the step's first key
       if (kb >= wmax) continue;
-      f32x16 s[QB];
-      const int key = blk * 32 + col;
-#pragma unroll
-      for (int k = 0; k < KS; k++) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + key * DH * 2 + (((2 * k + h) ^ (col & 7)) << 4));
-#pragma unroll
-        for (int b = 0; b < QB; b++)
-#pragma unroll
-          for (int p = NP - 1; p >= 0; p--)
-            s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[b][p][k], (p == NP - 1 && k == 0) ? (f32x16)(0.f) : s[b], 0, 0, 0);
-      }
-      union { uint32_t u[8]; bf16x8 f[2]; } pf[QB][NP];
-#pragma unroll
-      for (int b = 0; b < QB; b++) {
-        if (kb + 32 > wmin || kb < it.k0) {
-#pragma unroll
-          for (int v = 0; v < 16; v++) {
-            const int kk = kb + 8 * (v >> 2) + 4 * h + (v & 3);
-            s[b][v] = kk < lim[b] && kk >= it.k0 ? s[b][v] : -INFINITY;
-          }
-        }
-        float mx = s[b][0];
-#pragma unroll
-        for (int v = 1; v < 16; v++) mx = fmaxf(mx, s[b][v]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sc;
-        if (__any(mx > m_run[b] + 8.0f)) {  // -inf + 8 is -inf: the first keys of a query come through here
-          const float mn = fmaxf(m_run[b], mx);
-          const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[b] - mn);
-          l_run[b] *= al;
-#pragma unroll
-          for (int tt = 0; tt < NT; tt++)
-#pragma unroll
-            for (int v = 0; v < 16; v++) o[b][tt][v] *= al;
-          m_run[b] = mn;
-        }
-        const float off = m_run[b] == -INFINITY ? 0.f : m_run[b];  // a query without a key yet: every p is 0
-        float ps = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[b][e], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(s[b][e + 1], sc, -off));
-          ps += p0 + p1;
-          if constexpr (NP == 1) {
-            pf[b][0].u[e >> 1] = pack_bf16(p0, p1);
-          } else {
-            const uint32_t h0 = __float_as_uint(p0), h1 = __float_as_uint(p1);
-            const float r0 = p0 - __uint_as_float(h0 & 0xffff0000u), r1 = p1 - __uint_as_float(h1 & 0xffff0000u);
-            const uint32_t m0 = __float_as_uint(r0), m1 = __float_as_uint(r1);
-            const uint32_t l0 = __float_as_uint(r0 - __uint_as_float(m0 & 0xffff0000u));
-            const uint32_t l1 = __float_as_uint(r1 - __uint_as_float(m1 & 0xffff0000u));
-            pf[b][0].u[e >> 1] = __builtin_amdgcn_perm(h1, h0, 0x07060302u);
-            pf[b][1].u[e >> 1] = __builtin_amdgcn_perm(m1, m0, 0x07060302u);
-            pf[b][2].u[e >> 1] = __builtin_amdgcn_perm(l1, l0, 0x07060302u);
-          }
-        }
-        l_run[b] += ps;
-      }
-#pragma unroll
-      for (int ks = 0; ks < 2; ks++)
-#pragma unroll
-        for (int tt = 0; tt < NT; tt++) {
-          // lane (l % 16) of each 16: 8 bytes of row (l % 16) / 4 of its four keys; it gets dim l % 16 of all four
-          union { bf16x4 q[2]; bf16x8 f; } vf;
-#pragma unroll
-          for (int x = 0; x < 2; x++) {
-            const int vk = blk * 32 + ks * 16 + x * 8 + h * 4 + (lane & 15) / 4;
-            const int c = tt * 4 + (lane & 16) / 8 + (lane & 3) / 2;
-            vf.q[x] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-                (lbf16x4*)(lbytes*)(vt + vk * DH * 2 + ((c ^ (vk & 3) << VROT) << 4) + (lane & 1) * 8));
-          }
-#pragma unroll
-          for (int b = 0; b < QB; b++)
-#pragma unroll
-            for (int p = NP - 1; p >= 0; p--)
-              o[b][tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.f, pf[b][p].f[ks], o[b][tt], 0, 0, 0);
-        }
+      step(tile, nb * 32 * DH * 2, kb);
     }
   }
-#pragma unroll
-  for (int b = 0; b < QB; b++) l_run[b] += __shfl_xor(l_run[b], 32, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
 
-  __shared__ uint32_t s_bad[4 * QB];  // queries whose result here is not a number
-  if constexpr (WK > 1) {             // the waves of other keys hand their sums to the first
+  __shared__ uint32_t s_bad[4];  // queries whose result here is not a number
+  if constexpr (WK > 1) {         // the waves of other keys hand their sums to the first
     __syncthreads();
     float* ox = (float*)lds + (size_t)wq * (NT * 16 + 2) * 64;
     if (wk == 1 && active) {
 #pragma unroll
       for (int tt = 0; tt < NT; tt++)
 #pragma unroll
-        for (int v = 0; v < 16; v++) ox[(tt * 16 + v) * 64 + lane] = o[0][tt][v];
-      ox[NT * 16 * 64 + lane] = m_run[0];
-      ox[(NT * 16 + 1) * 64 + lane] = l_run[0];
+        for (int v = 0; v < 16; v++) ox[(tt * 16 + v) * 64 + lane] = o[tt][v];
+      ox[NT * 16 * 64 + lane] = m_run;
+      ox[(NT * 16 + 1) * 64 + lane] = l_run;
     }
     __syncthreads();
     if (wk == 0 && active) {
       const float m1 = ox[NT * 16 * 64 + lane], l1 = ox[(NT * 16 + 1) * 64 + lane];
-      const float mn = fmaxf(m_run[0], m1);
-      const float f0 = m_run[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[0] - mn);
+      const float mn = fmaxf(m_run, m1);
+      const float f0 = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mn);
       const float f1 = m1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1 - mn);
-      l_run[0] = l_run[0] * f0 + l1 * f1;
-      m_run[0] = mn;
+      l_run = l_run * f0 + l1 * f1;
+      m_run = mn;
 #pragma unroll
       for (int tt = 0; tt < NT; tt++)
 #pragma unroll
-        for (int v = 0; v < 16; v++) o[0][tt][v] = fmaf(ox[(tt * 16 + v) * 64 + lane], f1, o[0][tt][v] * f0);
+        for (int v = 0; v < 16; v++) o[tt][v] = fmaf(ox[(tt * 16 + v) * 64 + lane], f1, o[tt][v] * f0);
     }
   }
-  if (tid < 4 * QB) s_bad[tid] = 0u;
+  if (tid < 4) s_bad[tid] = 0u;
   __syncthreads();
   if (wk == 0 && active) {
+    bool bad = !(l_run > 0.f) && lim > it.k0;  // NaN, or nothing but scores of -inf
 #pragma unroll
-    for (int b = 0; b < QB; b++) {
-      bool bad = !(l_run[b] > 0.f) && lim[b] > it.k0;  // NaN, or nothing but scores of -inf
+    for (int tt = 0; tt < NT; tt++)
 #pragma unroll
-      for (int tt = 0; tt < NT; tt++)
-#pragma unroll
-        for (int v = 0; v < 16; v++) bad = bad || o[b][tt][v] != o[b][tt][v];
-      const unsigned long long bads = __ballot(bad && mine[b]);
-      if (lane == 0) s_bad[wq * QB + b] = (uint32_t)bads | (uint32_t)(bads >> 32);
-      if (!mine[b]) continue;
+      for (int v = 0; v < 16; v++) bad = bad || o[tt][v] != o[tt][v];
+    const unsigned long long bads = __ballot(bad && mine);
+    if (lane == 0) s_bad[wq] = (uint32_t)bads | (uint32_t)(bads >> 32);
+    if (mine) {
       if (it.rec < 0) {
-        const float inv = lim[b] > 0 ? 1.0f / l_run[b] : 0.f;
-        T* out = (T*)A.out + row[b] * A.os + head[b] * DH + 4 * h;
+        const float inv = lim > 0 ? 1.0f / l_run : 0.f;
+        T* out = (T*)A.out + row * A.os + head * DH + 4 * h;
 #pragma unroll
         for (int tt = 0; tt < NT; tt++)
 #pragma unroll
           for (int v = 0; v < 16; v += 4) {
-            const float x[4] = {o[b][tt][v], o[b][tt][v + 1], o[b][tt][v + 2], o[b][tt][v + 3]};
+            const float x[4] = {o[tt][v], o[tt][v + 1], o[tt][v + 2], o[tt][v + 3]};
             store4(out + tt * 32 + 2 * v, x, inv);
           }
       } else {
-        const size_t at = (size_t)it.rec + (size_t)g * nq + (wq * QB + b) * 32 + col;
+        const size_t at = (size_t)it.rec + (size_t)g * nq + jq;
         float* rec = R.o + at * DH + 4 * h;
 #pragma unroll
         for (int tt = 0; tt < NT; tt++)
 #pragma unroll
           for (int v = 0; v < 16; v += 4) {
-            const float x[4] = {o[b][tt][v], o[b][tt][v + 1], o[b][tt][v + 2], o[b][tt][v + 3]};
+            const float x[4] = {o[tt][v], o[tt][v + 1], o[tt][v + 2], o[tt][v + 3]};
             store4(rec + tt * 32 + 2 * v, x, 1.0f);
           }
-        if (h == 0) R.ml[at] = make_float2(m_run[b], l_run[b]);
+        if (h == 0) R.ml[at] = make_float2(m_run, l_run);
       }
     }
   }
   __syncthreads();  // every result is stored, and the tiles are free
-  for (int i = 0; i < 4 * QB; i++)
+  for (int i = 0; i < 4; i++)
     for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u) {
-      const int j = i * 32 + __builtin_ctz(m), r = it.row0 + j / G, hd = g * G + j % G;
-      int n = it.lim0 + j / G;
+      const int jb = i * 32 + __builtin_ctz(m), r = it.row0 + jb / G;
+      int n = it.lim0 + jb / G;
       if (it.mode & ITEM_FLAT) {
         const int s = A.seqs[r];
         n = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
       }
-      plain_piece<T, uint16_t, DH>(A, it, R, r, hd, j, nq, min(n, it.k1), (float*)lds);
+      plain_piece<T, uint16_t, DH>(A, it, R, r, g * G + jb % G, jb, nq, min(n, it.k1), (float*)lds);
     }
 }
 
@@ -873,15 +886,15 @@ __device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, cha
 }
 
 // Grid: x = KV head (with 8 of them a head's keys stay in one XCD's L2), y = piece.
-template <typename T, int DH, int QB>
-__global__ __launch_bounds__(kWG, QB == 1 ? 2 : 1) void k_attend_bf16(SeqArgs A, const int* count, const Item* items, Records R) {
+template <typename T, int DH>
+__global__ __launch_bounds__(kWG, 2) void k_attend_bf16(SeqArgs A, const int* count, const Item* items, Records R) {
   extern __shared__ __align__(16) char lds[];
   if ((int)blockIdx.y >= count[0]) return;
   const Item it = items[blockIdx.y];
   if (it.mode & ITEM_NARROW)
-    piece_bf16<T, DH, 1, 2>(A, it, R, lds);
+    piece_bf16<T, DH, 2>(A, it, R, lds);
   else
-    piece_bf16<T, DH, QB, 1>(A, it, R, lds);
+    piece_bf16<T, DH, 1>(A, it, R, lds);
 }
 
 template <int DH>
@@ -929,7 +942,7 @@ __global__ __launch_bounds__(kWG) void k_merge(SeqArgs A, const int* count, cons
 // ------------------------------------------------------------------------------------------------------- launches
 // What a call takes: its tiles, and its workspace (the plan's lists, then the records).
 struct Request {
-  int qb, rpt, wanted, jobs, tiles;
+  int rpt, wanted, jobs, tiles;
   size_t items, merges, records;
   size_t at_items, at_merges, at_tiles, at_ml, at_o, bytes;
 };
@@ -937,8 +950,7 @@ struct Request {
 Request request(const spd_cache& c, int n_q_heads, int dtype, int nseqs, int rows, int ngroups, bool prefix) {
   Request q{};
   const int hkv = c.n_kv_heads, G = n_q_heads / hkv;
-  q.qb = !prefix && dtype == SPD_BF16 && (long long)rows * n_q_heads >= 512ll * 256 ? 2 : 1;
-  q.rpt = 128 * q.qb / G;
+  q.rpt = 128 / G;
   q.wanted = std::max(1, kWantedWGs / hkv);
   if (prefix) {
     q.tiles = ngroups > 0 ? nseqs / q.rpt + ngroups : 0;
@@ -975,13 +987,7 @@ template <typename T, int DH>
 void launch_bf16(const SeqArgs& a, const Request& q, const int* count, const Item* items, const Records& r, hipStream_t s) {
   const dim3 grid(a.c.n_kv_heads, (unsigned)q.items);
   const size_t shm = 2 * 2 * 64 * DH * 2;
-  if constexpr (sizeof(T) == 2) {
-    if (q.qb == 2) {
-      hipLaunchKernelGGL((k_attend_bf16<T, DH, 2>), grid, dim3(kWG), shm, s, a, count, items, r);
-      return;
-    }
-  }
-  hipLaunchKernelGGL((k_attend_bf16<T, DH, 1>), grid, dim3(kWG), shm, s, a, count, items, r);
+  hipLaunchKernelGGL((k_attend_bf16<T, DH>), grid, dim3(kWG), shm, s, a, count, items, r);
 }
 
 // Plan, pieces, merge.
