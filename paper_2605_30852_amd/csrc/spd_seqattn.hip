@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "spd_cachefn.h"
 
@@ -27,17 +28,17 @@ struct SeqArgs {
 };
 
 // A query over the keys [k0, k1) in plain fp32, by the whole workgroup, which a query, key or value that is not finite
-// needs: there 0 times a value behind the query's own keys, or a plane's 0 * inf, is NaN on matrix cores. Scores in passes of 256 keys, computed twice
+// needs: there 0 times a value behind the query's own keys, or a plane's 0 * inf, is NaN on matrix cores. Scores in passes of NTH keys, computed twice
 // rather than kept. M, L and a (dims 4 d4 .. + 3 of thread d4 = tid % (DH / 4)) are the maximum, the sum and the
-// output; true in the threads that hold them. lds: kWG * 6 floats.
-template <typename T, typename KVT, int DH>
+// output; true in the threads that hold them. lds: NTH * 6 floats.
+template <typename T, typename KVT, int DH, int NTH>
 __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* table, int g, const T* q, float scale, int k0,
                             int k1, float* lds, float& M, float& L, float (&a)[4]) {
-  constexpr int TPQ = DH / 4, NG = kWG / TPQ;
+  constexpr int TPQ = DH / 4, NG = NTH / TPQ, NW = NTH / 64;
   const int tid = threadIdx.x, d4 = tid % TPQ, grp = tid / TPQ;
   const size_t half = (size_t)c.n_kv_heads * kPage * DH;
   float* sp = lds;
-  float* sr = lds + kWG;
+  float* sr = lds + NTH;
   auto row = [&](int key) { return pool + page_to_read(c, table[key / kPage]) * 2 * half + (size_t)(g * kPage + key % kPage) * DH; };
   auto score = [&](int key) {
     const KVT* k = row(key);
@@ -54,7 +55,7 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
   };
   float m = -INFINITY;
   bool sound = true;
-  for (int key = k0 + tid; key < k1; key += kWG) {
+  for (int key = k0 + tid; key < k1; key += NTH) {
     const float s = score(key);
     m = fmaxf(m, s);
     sound = sound && s < INFINITY;
@@ -64,18 +65,24 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
   __syncthreads();  // the area's earlier readers are done
   if ((tid & 63) == 0) {
     sp[tid >> 6] = m;
-    sp[4 + (tid >> 6)] = wave_sound ? 0.f : 1.f;
+    sp[NW + (tid >> 6)] = wave_sound ? 0.f : 1.f;
   }
   __syncthreads();
-  M = fmaxf(fmaxf(sp[0], sp[1]), fmaxf(sp[2], sp[3]));
-  const bool all_sound = sp[4] + sp[5] + sp[6] + sp[7] == 0.f;
+  float unsound = 0.f;
+  M = sp[0];
+#pragma unroll
+  for (int i = 0; i < NW; i++) {
+    M = fmaxf(M, sp[i]);
+    unsound += sp[NW + i];
+  }
+  const bool all_sound = unsound == 0.f;
   __syncthreads();
   if (!all_sound) {  // a score that is NaN or +inf makes every dim NaN
     L = a[0] = a[1] = a[2] = a[3] = NAN;
     return grp == 0;
   }
   L = a[0] = a[1] = a[2] = a[3] = 0.f;
-  for (int base = k0; base < k1; base += kWG) {
+  for (int base = k0; base < k1; base += NTH) {
     float p = 0.f;
     if (base + tid < k1) {
       const float s = score(base + tid);
@@ -83,7 +90,7 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
     }
     sp[tid] = p;
     __syncthreads();
-    const int n = min(kWG, k1 - base);
+    const int n = min(NTH, k1 - base);
     for (int i = grp; i < n; i += NG) {
       const KVT* v = row(base + i) + half + 4 * d4;
       const float2 v0 = ld2<KVT>(v), v1 = ld2<KVT>(v + 2);
@@ -121,7 +128,7 @@ __device__ __forceinline__ void store4(uint16_t* p, const float (&a)[4], float f
 // What a query's plain pass leaves in the place of its result in a piece: keys [k0, n) of the piece's.
 struct Item;
 struct Records;
-template <typename T, typename KVT, int DH>
+template <typename T, typename KVT, int DH, int NTH>
 __device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, int r, int head, int j, int nq, int n, float* lds);
 
 // --------------------------------------------------------------------------------------- pieces of the work
@@ -152,167 +159,192 @@ struct Merge {
 
 constexpr int kPlanWG = 1024;
 constexpr int kMinChunk = 256;
-constexpr int kWantedWGs = 512;
+constexpr int kWantedWGs = 256;
 constexpr int kBuckets = 256;
+
+// The sums of some queries: `query` of merge `merge` and those behind it, as many as a workgroup of the merge takes.
+struct Unit {
+  int merge, query;
+};
 
 struct PlanArgs {
   spd_cache c;
   const int *seqs, *cu, *prefix;
-  int nseqs, rows, ngroups, G, wanted;  // wanted: pieces of a KV head
+  int nseqs, rows, ngroups, G, wanted;  // wanted: pieces of a KV head; 0: no job is split
   int rpt;                              // rows of a tile
+  int tiles, jobs;
+  int qpu;                              // queries of a merge's workgroup
   unsigned long long records;           // room for them
-  int* count;                           // items, merges
+  int* count;                           // items, units
   Item* items;
   Merge* merges;
+  Unit* units;
+  int4* tile_rec;                       // decode rows: a tile's first record, pieces and queries
 };
 
 struct Job {
   int row0, nrows, table, a, b, lim0, mode;
 };
 
+// The batch's description, in LDS where it fits: the plan's searches wait for each of its loads.
+constexpr int kPlanSeqs = 4096;
+struct Batch {
+  const int *cu, *seqs, *lens, *prefix;  // LDS: cu_rows or cu_groups, sequences, their lengths by row of the batch, prefix_lens
+  const PlanArgs* P;
+  bool in_lds;
+  __device__ __forceinline__ int cu_at(int i) const { return in_lds ? cu[i] : P->cu[i]; }
+  __device__ __forceinline__ int seq_at(int i) const { return in_lds ? seqs[i] : P->seqs[i]; }
+  __device__ __forceinline__ int prefix_at(int i) const { return in_lds ? prefix[i] : P->prefix[i]; }
+  __device__ __forceinline__ int len_at(int i) const {  // -1: no such sequence
+    if (in_lds) return lens[i];
+    const int s = P->seqs[i];
+    return (unsigned)s < (unsigned)P->c.max_seqs ? seq_len(P->c, s) : -1;
+  }
+  // last i in [0, n) with cu[i] / d + i * step <= t (step 0 or 1; cu[0] = 0)
+  __device__ int last_at(int n, int t, int d, int step) const {
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (cu_at(mid) / d + mid * step <= t)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    return lo;
+  }
+};
+
 // Job t of a prompt call. The tiles of sequence i have the numbers cu[i] / rpt + i and up: enough of them, in order,
 // without a sum over the sequences before.
-__device__ bool prompt_job(const PlanArgs& P, int t, Job& j) {
-  int lo = 0, hi = P.nseqs - 1;
-  while (lo < hi) {  // last i with cu[i] / rpt + i <= t
-    const int mid = (lo + hi + 1) >> 1;
-    if (P.cu[mid] / P.rpt + mid <= t)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
-  const int begin = P.cu[lo], end = min(P.cu[lo + 1], P.rows), s = P.seqs[lo];
-  if (begin < 0 || begin >= end || (unsigned)s >= (unsigned)P.c.max_seqs) return false;
-  const long long row0 = begin + (long long)(t - begin / P.rpt - lo) * P.rpt;
+__device__ bool prompt_job(const PlanArgs& P, const Batch& B, int t, Job& j) {
+  const int i = B.last_at(P.nseqs, t, P.rpt, 1);
+  const int begin = B.cu_at(i), stop = B.cu_at(i + 1), end = min(stop, P.rows), len = B.len_at(i);
+  if (begin < 0 || begin >= end || len < 0) return false;
+  const long long row0 = begin + (long long)(t - begin / P.rpt - i) * P.rpt;
   if (row0 < begin || row0 >= end) return false;
   j.row0 = (int)row0;
   j.nrows = min(P.rpt, end - j.row0);
-  j.table = s;
+  j.table = B.seq_at(i);
   j.a = 0;
-  // sequence cu[lo + 1] may lie behind the buffers' rows: the keys are those of its own rows
-  const long long lim0 = (long long)seq_len(P.c, s) - P.cu[lo + 1] + j.row0 + 1;
-  j.lim0 = (int)max(lim0, -(1ll << 30));
+  j.lim0 = (int)max((long long)len - stop + j.row0 + 1, -(1ll << 30));
   j.b = max(0, j.lim0 + j.nrows - 1);
   j.mode = j.nrows * P.G <= 64 ? ITEM_NARROW : 0;
   return true;
 }
 
-// The prefix that row r's group shares: its length (0: none), the first row and the number of rows.
-__device__ int shared_prefix(const PlanArgs& P, int j, int& first, int& rows) {
-  first = P.cu[j];
-  rows = min(P.cu[j + 1], P.nseqs) - first;
+// The prefix that group j shares: its length (0: none), the first row and the number of rows.
+__device__ int shared_prefix(const PlanArgs& P, const Batch& B, int j, int& first, int& rows) {
+  first = B.cu_at(j);
+  rows = min(B.cu_at(j + 1), P.nseqs) - first;
   if (first < 0 || rows < 2) return 0;
-  const int s = P.seqs[first];
-  return (unsigned)s < (unsigned)P.c.max_seqs ? min(max(P.prefix[j], 0), seq_len(P.c, s)) : 0;
-}
-
-__device__ int group_of(const PlanArgs& P, int r) {
-  int lo = 0, hi = P.ngroups - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (P.cu[mid] <= r)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
-  return lo;
+  return min(max(B.prefix_at(j), 0), max(B.len_at(first), 0));
 }
 
 // Job t of a decode call: below `tiles` a tile of a group's rows over the prefix, else a row over the keys behind it.
-// shared: a row's own job is joined with its prefix's.
-__device__ bool prefix_job(const PlanArgs& P, int t, int tiles, Job& j, bool& shared) {
+// shared: a row's own job is joined with its prefix's, of tile `tile` from query `query` on.
+__device__ bool prefix_job(const PlanArgs& P, const Batch& B, int t, Job& j, bool& shared, int& tile, int& query) {
   shared = false;
-  if (t < tiles) {
-    int lo = 0, hi = P.ngroups - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (P.cu[mid] / P.rpt + mid <= t)
-        lo = mid;
-      else
-        hi = mid - 1;
-    }
-    int first, rows;
-    const int n = shared_prefix(P, lo, first, rows);
+  int first, rows;
+  j.lim0 = 0;
+  j.a = 0;
+  if (t < P.tiles) {
+    const int g = B.last_at(P.ngroups, t, P.rpt, 1), n = shared_prefix(P, B, g, first, rows);
     if (n == 0) return false;
-    const long long at = (long long)(t - first / P.rpt - lo) * P.rpt;
+    const long long at = (long long)(t - first / P.rpt - g) * P.rpt;
     if (at < 0 || at >= rows) return false;
     j.row0 = first + (int)at;
     j.nrows = min(P.rpt, rows - (int)at);
-    j.table = P.seqs[first];
-    j.a = 0;
+    j.table = B.seq_at(first);
     j.b = n;
     j.mode = ITEM_FLAT | (j.nrows * P.G <= 64 ? ITEM_NARROW : 0);
-    j.lim0 = 0;
     shared = true;
     return true;
   }
-  const int r = t - tiles, s = P.seqs[r];
-  if ((unsigned)s >= (unsigned)P.c.max_seqs) return false;
+  const int r = t - P.tiles, len = B.len_at(r);
+  if (len < 0) return false;
   j.row0 = r;
   j.nrows = 1;
-  j.table = s;
-  j.b = seq_len(P.c, s);
-  j.a = 0;
-  j.lim0 = 0;
+  j.table = B.seq_at(r);
+  j.b = len;
   j.mode = ITEM_FLAT | ITEM_NARROW;
   if (P.ngroups > 0) {
-    int first, rows;
-    const int g = group_of(P, r), n = shared_prefix(P, g, first, rows);
+    const int g = B.last_at(P.ngroups, r, 1, 0), n = shared_prefix(P, B, g, first, rows);
     if (n > 0 && r >= first && r < first + rows) {
       shared = true;
-      j.a = min(n, j.b);
+      j.a = min(n, len);
+      tile = first / P.rpt + g + (r - first) / P.rpt;
+      query = (r - first) % P.rpt * P.G;
     }
   }
   return true;
 }
 
 // A prompt's merge is known with its job. A decode row's takes its own job's records and those of its tile, which the
-// tile's thread leaves in tile_rec (in LDS order: by tile number, kept in global memory behind the items).
+// tile's thread leaves in tile_rec.
 template <bool PREFIX>
-__global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P, int jobs, int tiles, int4* tile_rec) {
+__global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
+  __shared__ int s_cu[kPlanSeqs + 1], s_seqs[kPlanSeqs], s_lens[kPlanSeqs], s_prefix[PREFIX ? kPlanSeqs : 1];
   __shared__ unsigned long long s_total, s_rec;
-  __shared__ int s_max, s_count[kBuckets], s_merges;
+  __shared__ int s_max, s_count[kBuckets], s_merges, s_units;
   const int tid = threadIdx.x;
+  const Batch B{s_cu, s_seqs, s_lens, s_prefix, &P, P.nseqs <= kPlanSeqs};
+  if (B.in_lds) {
+    for (int i = tid; i < P.nseqs; i += kPlanWG) {
+      const int s = P.seqs[i];
+      s_seqs[i] = s;
+      s_lens[i] = (unsigned)s < (unsigned)P.c.max_seqs ? seq_len(P.c, s) : -1;
+    }
+    const int n = PREFIX ? P.ngroups : P.nseqs;
+    if (n > 0)
+      for (int i = tid; i <= n; i += kPlanWG) {
+        s_cu[i] = P.cu[i];
+        if (PREFIX && i < n) s_prefix[i] = P.prefix[i];
+      }
+  }
   if (tid < kBuckets) s_count[tid] = 0;
   if (tid == 0) {
-    s_total = 0ull;
+    s_total = s_rec = 0ull;
     s_max = 1;
-    s_rec = 0ull;
-    s_merges = 0;
+    s_merges = s_units = 0;
   }
   __syncthreads();
-  auto job = [&](int t, Job& j, bool& shared) {
-    if constexpr (PREFIX) return prefix_job(P, t, tiles, j, shared);
+  auto job = [&](int t, Job& j, bool& shared, int& tile, int& query) {
+    if constexpr (PREFIX) return prefix_job(P, B, t, j, shared, tile, query);
     shared = false;
-    return prompt_job(P, t, j);
+    return prompt_job(P, B, t, j);
   };
+  Job j;
+  bool sh;
+  int tile, query;
   {
     unsigned long long sum = 0ull;
     int longest = 1;
-    for (int t = tid; t < jobs; t += kPlanWG) {
-      Job j;
-      bool sh;
-      if (!job(t, j, sh)) continue;
+    for (int t = tid; t < P.jobs; t += kPlanWG) {
+      if (!job(t, j, sh, tile, query)) continue;
       sum += (unsigned)(j.b - j.a);
       longest = max(longest, j.b - j.a);
     }
-    atomicAdd(&s_total, sum);
-    atomicMax(&s_max, longest);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      sum += __shfl_xor(sum, d, 64);
+      longest = max(longest, __shfl_xor(longest, d, 64));
+    }
+    if ((tid & 63) == 0) {
+      atomicAdd(&s_total, sum);
+      atomicMax(&s_max, longest);
+    }
   }
   __syncthreads();
-  const unsigned long long want = (s_total + P.wanted - 1) / P.wanted;
+  const unsigned long long want = P.wanted > 0 ? (s_total + P.wanted - 1) / P.wanted : ~0ull;
   const int chunk = want >= (unsigned)s_max ? (s_max + 63) / 64 * 64 : max(kMinChunk, (int)((want + 63) / 64 * 64));
-  const int longest = min(s_max, chunk);
+  const float per_key = (float)(kBuckets - 1) / (2.0f * (float)min(s_max, chunk));
   auto bucket = [&](int n, int mode) {  // the longest first; a key of a wide piece costs about twice a narrow one's
-    const long long x = (long long)n * (mode & ITEM_NARROW ? 1 : 2) * (kBuckets - 1) / (2ll * longest);
-    return kBuckets - 1 - (int)min(x, (long long)kBuckets - 1);
+    return kBuckets - 1 - min((int)((float)n * (mode & ITEM_NARROW ? 1.0f : 2.0f) * per_key), kBuckets - 1);
   };
   // a job's pieces; 0: nothing to do (a row that ends with its prefix)
   auto pieces_of = [&](const Job& j, bool sh) { return j.b > j.a ? (j.b - j.a + chunk - 1) / chunk : sh ? 0 : 1; };
-  for (int t = tid; t < jobs; t += kPlanWG) {
-    Job j;
-    bool sh;
-    if (!job(t, j, sh)) continue;
+  for (int t = tid; t < P.jobs; t += kPlanWG) {
+    if (!job(t, j, sh, tile, query)) continue;
     const int n = pieces_of(j, sh);
     for (int p = 0; p < n; p++) atomicAdd(&s_count[bucket(min(chunk, j.b - j.a - p * chunk), j.mode)], 1);
   }
@@ -333,11 +365,9 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P, int jobs
     if (tid == 0) P.count[0] = before;
   }
   __syncthreads();
-  for (int t = tid; t < jobs; t += kPlanWG) {
-    Job j;
-    bool sh;
-    if (!job(t, j, sh)) {
-      if (PREFIX && t < tiles) tile_rec[t] = make_int4(0, 0, 0, 0);
+  for (int t = tid; t < P.jobs; t += kPlanWG) {
+    if (!job(t, j, sh, tile, query)) {
+      if (PREFIX && t < P.tiles) P.tile_rec[t] = make_int4(0, 0, 0, 0);
       continue;
     }
     int n = pieces_of(j, sh), rec = -1;
@@ -347,8 +377,8 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P, int jobs
       const unsigned long long at = atomicAdd(&s_rec, (unsigned long long)need);
       rec = (int)at;
       if (at + need > P.records) n = 0;  // only where cu_groups does not ascend
-      if (PREFIX && t < tiles) {
-        tile_rec[t] = make_int4(rec, n, nq, 0);
+      if (PREFIX && t < P.tiles) {
+        P.tile_rec[t] = make_int4(rec, n, nq, 0);
       } else {
         Merge m;
         m.row0 = j.row0;
@@ -361,14 +391,14 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P, int jobs
         m.lim0 = j.lim0;
         m.mode = j.mode;
         if (PREFIX && sh) {
-          int first, rows;
-          const int g = group_of(P, j.row0);
-          shared_prefix(P, g, first, rows);
-          m.queries[0] = first / P.rpt + g + (j.row0 - first) / P.rpt;  // the tile's number, replaced below
-          m.first[0] = (j.row0 - first) % P.rpt * P.G;
           m.pieces[0] = -1;
+          m.queries[0] = tile;  // replaced below
+          m.first[0] = query;
         }
-        P.merges[atomicAdd(&s_merges, 1)] = m;
+        const int at_merge = atomicAdd(&s_merges, 1);
+        P.merges[at_merge] = m;
+        const int units = (nq + P.qpu - 1) / P.qpu, at_unit = atomicAdd(&s_units, units);
+        for (int u = 0; u < units; u++) P.units[at_unit + u] = Unit{at_merge, u * P.qpu};
       }
     }
     for (int p = 0; p < n; p++) {
@@ -379,18 +409,17 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P, int jobs
   }
   __syncthreads();
   if (PREFIX) {
-    __threadfence_block();
     for (int i = tid; i < s_merges; i += kPlanWG) {
       Merge& m = P.merges[i];
       if (m.pieces[0] < 0) {
-        const int4 r = tile_rec[m.queries[0]];
+        const int4 r = P.tile_rec[m.queries[0]];
         m.rec[0] = r.x;
         m.pieces[0] = m.first[0] + m.nrows * P.G <= r.z ? r.y : 0;
         m.queries[0] = r.z;
       }
     }
   }
-  if (tid == 0) P.count[1] = s_merges;
+  if (tid == 0) P.count[1] = s_units;
 }
 
 // Records: o, then (m, l) with m in units of log2.
@@ -430,15 +459,29 @@ constexpr float kLog2e = 1.44269504088896341f;
 //     + 0..3, which two transposing LDS reads of V rows give as the A operand.
 // bf16 queries: q as it is, the scale in the exponent's FMA, p rounded to bf16 (half a step, 2^-8 of each p: as much as the
 // rounding of the output), l the sum of the rounded p. fp32 queries: q (scaled in fp32) and p as three exact planes, three products each.
-// WK waves share a tile's 64 keys, 4 / WK the queries. K and V go to LDS by direct loads, two tiles deep, the
-// 16-byte chunks of a row permuted by its key so that neither kind of read meets itself in a bank.
-template <typename T, int DH, int WK>
+// K and V go to LDS by direct loads, the 16-byte chunks of a row permuted by its key so that neither kind of read
+// meets itself in a bank.
+//
+// Wide (256 queries, eight waves on 32 each): a wave's step has a matrix phase, the scores of the next tile and the
+// products of this one, and a vector phase, the next tile's softmax, each about 1000 cycles for 64 keys. The waves
+// of a SIMD, w and w + 4, take turns: barriers between the phases keep one in its matrix phase while the other is in its
+// vector phase. Slot 2 t is wave 0..3's matrix phase of step t and wave 4..7's vector phase of step t - 1. Tiles
+// K(t + 2) and V(t + 1) are requested at the start of slot 2 t, when the last reads of K(t) and V(t - 1) are
+// over, and waited for at the end of slot 2 t + 1.
+// Narrow (up to 64 queries): four waves share a tile's 128 keys, two the queries; what bounds it is the stream of keys,
+// two tiles deep.
+constexpr int kAttWG = 512;
+
+template <typename T, int DH, bool NARROW>
 __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, char* lds) {
   constexpr int NP = sizeof(T) == 4 ? 3 : 1;
-  constexpr int KT = 64, NT = DH / 32, KS = DH / 16, NCH = DH / 8, NB = KT / 32 / WK;
-  constexpr int SB = NP == 1 ? NB : 1;  // 32-key blocks of a step (with three planes two spill)
-  constexpr int KBUF = KT * DH * 2, BUF = 2 * KBUF, LPT = KT * NCH / kWG;
-  constexpr int VROT = DH == 128 ? 2 : 1;  // V: chunk c of key k sits at c ^ (k % 4) << VROT
+  constexpr int WK = NARROW ? 4 : 1;
+  constexpr int KT = NARROW ? 128 : NP == 3 && DH == 128 ? 32 : 64;  // 32: three planes of q leave no registers for 64
+  constexpr int NT = DH / 32, KS = DH / 16, NCH = DH / 8;
+  constexpr int SB = NARROW ? 1 : KT / 32;  // 32-key blocks of a wave's step
+  constexpr int KBUF = KT * DH * 2, LPT = KT * NCH / kAttWG;
+  constexpr int KROT = DH == 128 ? 0 : 1;  // K: chunk c of key k sits at c ^ (k >> KROT) % NCH: 16 keys in 64 banks
+  constexpr int VROT = DH == 128 ? 0 : 1;  // V: chunk c of key k sits at c ^ (k % 8 >> VROT) << 1
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
   const int wk = WK == 1 ? 0 : w % WK, wq = WK == 1 ? w : w / WK;
   const int g = blockIdx.x, G = A.G, nq = it.nrows * G;
@@ -493,46 +536,48 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
   wmin = __builtin_amdgcn_readfirstlane(wmin);
   wmax = __builtin_amdgcn_readfirstlane(wmax);
 
-  // The four pages of a tile, one a lane (mod 4), are read a tile ahead of their use.
-  auto pages = [&](int t) { return page_to_read(C, table[min(start / kPage + t * (KT / kPage) + (lane & 3), last / kPage)]); };
+  // The pages of a tile, one a lane (mod their number), are read a tile ahead of their use, and looked at only there: a look
+  // at them here would wait for them and for the keys requested before them.
+  auto pages = [&](int t) { return table[min(start / kPage + t * (KT / kPage) + (lane & (KT / kPage - 1)), last / kPage)]; };
   // A thread's bytes of a page, load i: chunk ch % NCH of key ch / NCH. All loads of a thread are of the same key of a page,
   // or of keys 16 apart, so one offset serves them.
   const int lk = tid / NCH, lc = tid % NCH;
-  static_assert(kWG / NCH % kPage == 0, "a pass of the workgroup is whole pages");
-  const uint32_t koff = (lk % kPage) * DH * 2 + ((lc ^ (lk & 7)) << 4);
-  const uint32_t voff = (lk % kPage) * DH * 2 + ((lc ^ (lk & 3) << VROT) << 4);
+  static_assert(kAttWG / NCH % kPage == 0 && LPT >= 1, "a pass of the workgroup is whole pages");
+  const uint32_t koff = (lc ^ (lk >> KROT) % NCH) << 4;
+  const uint32_t voff = (lc ^ (lk & 7) >> VROT << 1) << 4;
   const size_t page_bytes = 2 * half * sizeof(uint16_t);
-  auto load_tile = [&](int buf, int t, int pg, uint32_t ko, uint32_t vo, int i) {
-    const int page = __builtin_amdgcn_readlane(pg, (i * kWG + w * 64) / (NCH * kPage));
-    gbytes* p = (gbytes*)pool + (size_t)page * page_bytes;
-    lbytes* to = (lbytes*)(lds + buf * BUF + (i * kWG + w * 64) * 16);
-    __builtin_amdgcn_global_load_lds(p + ko, to, 16, 0, 0);
-    __builtin_amdgcn_global_load_lds(p + half * sizeof(uint16_t) + vo, to + KBUF, 16, 0, 0);
+  // The pages of a thread's loads, in scalar registers: looked at between loads, a lane's register would wait for those before it.
+  struct Pages {
+    int p[LPT];
   };
-  auto issue = [&](int buf, int t, int pg) {
+  auto own_pages = [&](int pg) {
+    Pages x;
+#pragma unroll
+    for (int i = 0; i < LPT; i++) x.p[i] = page_to_read(C, __builtin_amdgcn_readlane(pg, (i * kAttWG + w * 64) / (NCH * kPage)));
+    return x;
+  };
+  // Tile t's keys or values to `to`. Keys outside [k0, k1) are read as the nearest one inside: their probability is 0, and 0
+  // times a value must be 0. (So is a tile behind the last one, which saves the loop a branch and is not used.)
+  auto load = [&](int to, int t, const Pages& pages, uint32_t off, size_t plane) {
     const int first = start + t * KT;
-    if (first >= it.k0 && first + KT <= it.k1) {
 #pragma unroll
-      for (int i = 0; i < LPT; i++) load_tile(buf, t, pg, koff, voff, i);
-    } else {
-      // Keys outside [k0, k1) are read as the nearest one inside: their probability is 0, and 0 times a value must be 0.
-#pragma unroll
-      for (int i = 0; i < LPT; i++) {
-        const int k = i * (kWG / NCH) + lk;
-        const uint32_t in = (min(max(first + k, it.k0), last) % kPage) * DH * 2;
-        load_tile(buf, t, pg, in + (koff & (DH * 2 - 1)), in + (voff & (DH * 2 - 1)), i);
-      }
+    for (int i = 0; i < LPT; i++) {
+      const uint32_t at = (uint32_t)(min(max(first + i * (kAttWG / NCH) + lk, it.k0), last) & (kPage - 1)) * (DH * 2) + off;
+      __builtin_amdgcn_global_load_lds((gbytes*)pool + (size_t)pages.p[i] * page_bytes + plane + at,
+                                       (lbytes*)(lds + to + (i * kAttWG + w * 64) * 16), 16, 0, 0);
     }
   };
+  auto load_k = [&](int to, int t, const Pages& p) { load(to, t, p, koff, 0); };
+  auto load_v = [&](int to, int t, const Pages& p) { load(to, t, p, voff, half * sizeof(uint16_t)); };
   // A lane's bytes of a K or V tile.
-  uint32_t ka[4], va[NT];
+  uint32_t ka[KS], va[NT];
 #pragma unroll
-  for (int k = 0; k < 4; k++) ka[k] = (WK == 1 ? 0 : wk * 32 * DH * 2) + col * DH * 2 + (((2 * k + h) ^ (col & 7)) << 4);
+  for (int k = 0; k < KS; k++) ka[k] = (WK == 1 ? 0 : wk * 32 * DH * 2) + col * DH * 2 + (((2 * k + h) ^ (col >> KROT) % NCH) << 4);
 #pragma unroll
   for (int tt = 0; tt < NT; tt++) {
     // lane l % 16 of each 16: 8 bytes of row (l % 16) / 4 of its four keys; it gets dim l % 16 of all four
     const int vk = (WK == 1 ? 0 : wk * 32) + h * 4 + (lane & 15) / 4, c = tt * 4 + (lane & 16) / 8 + (lane & 3) / 2;
-    va[tt] = KBUF + vk * DH * 2 + ((c ^ (vk & 3) << VROT) << 4) + (lane & 1) * 8;
+    va[tt] = vk * DH * 2 + ((c ^ (vk & 7) >> VROT << 1) << 4) + (lane & 1) * 8;
   }
 
   f32x16 o[NT];
@@ -540,20 +585,24 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
   for (int t = 0; t < NT; t++) o[t] = (f32x16)(0.f);
   float m_run = -INFINITY, l_run = 0.f;
 
-  // SB blocks from key kb on, the first of them `at` bytes into the tile
-  auto step = [&](const char* tile, int at, int kb) {
-    f32x16 s[SB];
+  f32x16 s[SB];
+  union { uint32_t u[8]; bf16x8 f[2]; } pf[SB][NP];
+  // s = scores of the SB blocks at kt
+  auto scores = [&](const char* kt) {
 #pragma unroll
     for (int x = 0; x < SB; x++)
 #pragma unroll
       for (int k = 0; k < KS; k++) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + ka[k & 3] + at + x * 32 * DH * 2 + (k >> 2) * 128);
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + ka[k] + x * 32 * DH * 2);
 #pragma unroll
         for (int p = NP - 1; p >= 0; p--)
           s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[p][k], (p == NP - 1 && k == 0) ? (f32x16)(0.f) : s[x], 0, 0, 0);
       }
+  };
+  // p of the scores of the keys from kb on
+  auto softmax = [&](int kb) {
     if (kb < it.k0 || kb + SB * 32 > wmin) {  // some key is not every query's
-      asm volatile("");                       // stays a branch: the masks cost a fifth of the step's vector work
+      asm volatile("");                       // stays a branch: the masks cost as much as a third of the step's vector work
 #pragma unroll
       for (int x = 0; x < SB; x++)
 #pragma unroll
@@ -580,17 +629,15 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
       m_run = mn;
     }
     const float off = m_run == -INFINITY ? 0.f : m_run;  // a query without a key yet: every p is 0
-    union { uint32_t u[8]; bf16x8 f[2]; } pf[SB][NP];
 #pragma unroll
-    for (int x = 0; x < SB; x++) {
+    for (int x = 0; x < SB; x++)
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
         const float p0 = __builtin_amdgcn_exp2f(fmaf(s[x][e], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(s[x][e + 1], sc, -off));
+        l_run += p0 + p1;
         if constexpr (NP == 1) {
           pf[x][0].u[e >> 1] = pack_bf16(p0, p1);
-          l_run += p0 + p1;
         } else {
-          l_run += p0 + p1;
           const uint32_t h0 = __float_as_uint(p0), h1 = __float_as_uint(p1);
           const float r0 = p0 - __uint_as_float(h0 & 0xffff0000u), r1 = p1 - __uint_as_float(h1 & 0xffff0000u);
           const uint32_t m0 = __float_as_uint(r0), m1 = __float_as_uint(r1);
@@ -602,72 +649,200 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
         }
       }
 #pragma unroll
+    for (int x = 0; x < SB; x++)
+#pragma unroll
+      for (int p = 0; p < NP; p++) asm volatile("" : "+v"(pf[x][p].f[0]), "+v"(pf[x][p].f[1]));  // here, not behind a barrier
+  };
+  // o += p V of the blocks at vt
+  auto products = [&](const char* vt) {
+#pragma unroll
+    for (int x = 0; x < SB; x++)
+#pragma unroll
       for (int ks = 0; ks < 2; ks++)
 #pragma unroll
         for (int tt = 0; tt < NT; tt++) {
           union { bf16x4 q[2]; bf16x8 f; } vf;
 #pragma unroll
           for (int y = 0; y < 2; y++)
-            vf.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-                (lbf16x4*)(lbytes*)(tile + va[tt] + at + (x * 32 + ks * 16 + y * 8) * DH * 2));
+            vf.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lbf16x4*)(lbytes*)(vt + va[tt] + (x * 32 + ks * 16 + y * 8) * DH * 2));
 #pragma unroll
           for (int p = NP - 1; p >= 0; p--)
             o[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.f, pf[x][p].f[ks], o[tt], 0, 0, 0);
         }
-    }
   };
+  // A wave comes to the barrier with its own LDS reads over, and landed all but its newest `outstanding` direct loads (-1: any).
+  auto barrier = [&](auto outstanding) {
+    constexpr int N = decltype(outstanding)::value;
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (N >= 0)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+    else
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  using All = std::integral_constant<int, 0>;
+  using None = std::integral_constant<int, -1>;
 
-  int pg = 0;
-  if (tiles > 0) {
-    pg = pages(0);
-    issue(0, 0, pg);
-    pg = pages(1);
-  }
-  for (int t = 0; t < tiles; t++) {
-    const int buf = t & 1;
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (t + 1 < tiles) {
-      issue(buf ^ 1, t + 1, pg);
-      pg = pages(t + 2);
+  if constexpr (NARROW) {
+    int pg = 0;
+    if (tiles > 0) {
+      const Pages p = own_pages(pages(0));
+      load_k(0, 0, p);
+      load_v(KBUF, 0, p);
+      pg = pages(1);
     }
-    const char* tile = lds + buf * BUF;
-    if (!active) continue;
+    for (int t = 0; t < tiles; t++) {
+      const int buf = (t & 1) * 2 * KBUF, next = (t & 1 ^ 1) * 2 * KBUF, kb = start + t * KT + wk * 32;
+      barrier(All{});
+      if (t + 1 < tiles) {
+        const Pages p = own_pages(pg);
+        pg = pages(t + 2);
+        load_k(next, t + 1, p);
+        load_v(next + KBUF, t + 1, p);
+      }
+      if (!active || kb >= wmax) continue;
+      scores(lds + buf);
+      softmax(kb);
+      products(lds + buf + KBUF);
+    }
+  } else if (tiles > 0) {
+    const bool late = w >= kAttWG / 128;
+    // K(t) is at t % 3 KBUF, V(t) at (3 + t % 3) KBUF: places of K(t + 1), V(t), K(t + 3) and V(t + 2)
+    int kat = 0, vat = 2 * KBUF;
+    auto turn = [&](int& at) { at = at == 2 * KBUF ? 0 : at + KBUF; };
+    Pages pk = own_pages(pages(0)), pv = pk;  // of K(t + 3) and V(t + 2)
+    int pg = pages(1);
+    load_k(0, 0, pk);
+    load_v(3 * KBUF, 0, pv);
+    pk = own_pages(pg);
+    load_k(KBUF, 1, pk);
+    pv = pk;
+    pg = pages(2);
+    // Behind a phase's LDS reads: the compiler lets a read of LDS wait for every direct load before it.
+    auto request = [&](int t) {
+      pk = own_pages(pg);
+      pg = pages(t + 4);
+      load_k(kat == 0 ? 2 * KBUF : kat - KBUF, t + 3, pk);
+      load_v(3 * KBUF + (vat == 0 ? 2 * KBUF : vat - KBUF), t + 2, pv);
+      pv = pk;
+      turn(kat);
+      turn(vat);
+    };
+    const int mine_tiles = active ? min(max((wmax - start + KT - 1) / KT, 0), tiles) : 0;  // tiles with keys of this wave's queries
+    barrier(All{});
+    if (late) barrier(None{});
+    if (mine_tiles > 0) scores(lds);
+    barrier(All{});
+    request(-1);
+    if (mine_tiles > 0) softmax(start);
+    barrier(None{});
+    int t;
 #pragma unroll 1
-    for (int nb = 0; nb < NB; nb += SB) {
-      const int kb = start + t * KT + (WK == 1 ? nb : wk) * 32;  // the step's first key
-      if (kb >= wmax) continue;
-      step(tile, nb * 32 * DH * 2, kb);
+    for (t = 0; t < mine_tiles - 1; t++) {
+      const char *kt = lds + kat, *vt = lds + 3 * KBUF + vat;
+      if constexpr (NP == 1) {
+        // fragments are read a batch ahead of the products that take them; p first: its registers are free when the scores come
+        bf16x8 f[2][2 * NT > KS ? 2 * NT : KS];
+        auto read_k = [&](bf16x8* f, int x) {
+#pragma unroll
+          for (int k = 0; k < KS; k++) f[k] = *reinterpret_cast<const bf16x8*>(kt + ka[k] + x * 32 * DH * 2);
+        };
+        auto read_v = [&](bf16x8* f, int x) {
+#pragma unroll
+          for (int i = 0; i < 2 * NT; i++) {
+            union { bf16x4 q[2]; bf16x8 f; } vf;
+#pragma unroll
+            for (int y = 0; y < 2; y++)
+              vf.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+                  (lbf16x4*)(lbytes*)(vt + va[i % NT] + (x * 32 + i / NT * 16 + y * 8) * DH * 2));
+            f[i] = vf.f;
+          }
+        };
+        read_v(f[0], 0);
+        read_v(f[1], 1);
+#pragma unroll
+        for (int x = 0; x < SB; x++)
+#pragma unroll
+          for (int i = 0; i < 2 * NT; i++)
+            o[i % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[x][i], pf[x][0].f[i / NT], o[i % NT], 0, 0, 0);
+        bf16x8 fk[2][KS];
+        read_k(fk[0], 0);
+        read_k(fk[1], 1);
+#pragma unroll
+        for (int x = 0; x < SB; x++)
+#pragma unroll
+          for (int k = 0; k < KS; k++) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[x][k], qf[0][k], k == 0 ? (f32x16)(0.f) : s[x], 0, 0, 0);
+        // reads of LDS a batch ahead of the products that take them
+        __builtin_amdgcn_sched_group_barrier(0x100, 4 * NT, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * NT; i++) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * KS; i++) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 2 * NT, 0);
+      } else {
+        products(vt);
+        scores(kt);
+      }
+      barrier(All{});
+      request(t);
+      softmax(start + (t + 1) * KT);
+      barrier(None{});
     }
+    if (mine_tiles > 0) {
+      products(lds + 3 * KBUF + vat);
+      barrier(All{});
+      request(t++);
+      barrier(None{});
+    }
+#pragma unroll 1
+    for (; t < tiles; t++) {
+      barrier(All{});
+      request(t);
+      barrier(None{});
+    }
+    if (!late) barrier(None{});
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the tiles behind the last one, before the memory has another use
   }
   l_run += __shfl_xor(l_run, 32, 64);
 
-  __shared__ uint32_t s_bad[4];  // queries whose result here is not a number
+  constexpr int NQB = kAttWG / 64 / WK;  // sets of 32 queries
+  __shared__ uint32_t s_bad[NQB];  // queries whose result here is not a number
   if constexpr (WK > 1) {         // the waves of other keys hand their sums to the first
     __syncthreads();
-    float* ox = (float*)lds + (size_t)wq * (NT * 16 + 2) * 64;
-    if (wk == 1 && active) {
+    float* ox = (float*)lds + (size_t)wq * (WK - 1) * (NT * 16 + 2) * 64 + lane;
+    if (wk > 0 && active) {
+      float* mine_x = ox + (wk - 1) * (NT * 16 + 2) * 64;
 #pragma unroll
       for (int tt = 0; tt < NT; tt++)
 #pragma unroll
-        for (int v = 0; v < 16; v++) ox[(tt * 16 + v) * 64 + lane] = o[tt][v];
-      ox[NT * 16 * 64 + lane] = m_run;
-      ox[(NT * 16 + 1) * 64 + lane] = l_run;
+        for (int v = 0; v < 16; v++) mine_x[(tt * 16 + v) * 64] = o[tt][v];
+      mine_x[NT * 16 * 64] = m_run;
+      mine_x[(NT * 16 + 1) * 64] = l_run;
     }
     __syncthreads();
     if (wk == 0 && active) {
-      const float m1 = ox[NT * 16 * 64 + lane], l1 = ox[(NT * 16 + 1) * 64 + lane];
-      const float mn = fmaxf(m_run, m1);
-      const float f0 = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mn);
-      const float f1 = m1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1 - mn);
-      l_run = l_run * f0 + l1 * f1;
-      m_run = mn;
+#pragma unroll 1
+      for (int x = 1; x < WK; x++, ox += (NT * 16 + 2) * 64) {
+        const float m1 = ox[NT * 16 * 64], l1 = ox[(NT * 16 + 1) * 64];
+        const float mn = fmaxf(m_run, m1);
+        const float f0 = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mn);
+        const float f1 = m1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1 - mn);
+        l_run = l_run * f0 + l1 * f1;
+        m_run = mn;
 #pragma unroll
-      for (int tt = 0; tt < NT; tt++)
+        for (int tt = 0; tt < NT; tt++)
 #pragma unroll
-        for (int v = 0; v < 16; v++) o[tt][v] = fmaf(ox[(tt * 16 + v) * 64 + lane], f1, o[tt][v] * f0);
+          for (int v = 0; v < 16; v++) o[tt][v] = fmaf(ox[(tt * 16 + v) * 64], f1, o[tt][v] * f0);
+      }
     }
   }
-  if (tid < 4) s_bad[tid] = 0u;
+  if (tid < NQB) s_bad[tid] = 0u;
   __syncthreads();
   if (wk == 0 && active) {
     bool bad = !(l_run > 0.f) && lim > it.k0;  // NaN, or nothing but scores of -inf
@@ -703,7 +878,7 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
     }
   }
   __syncthreads();  // every result is stored, and the tiles are free
-  for (int i = 0; i < 4; i++)
+  for (int i = 0; i < NQB; i++)
     for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u) {
       const int jb = i * 32 + __builtin_ctz(m), r = it.row0 + jb / G;
       int n = it.lim0 + jb / G;
@@ -711,17 +886,17 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
         const int s = A.seqs[r];
         n = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
       }
-      plain_piece<T, uint16_t, DH>(A, it, R, r, g * G + jb % G, jb, nq, min(n, it.k1), (float*)lds);
+      plain_piece<T, uint16_t, DH, kAttWG>(A, it, R, r, g * G + jb % G, jb, nq, min(n, it.k1), (float*)lds);
     }
 }
 
-template <typename T, typename KVT, int DH>
+template <typename T, typename KVT, int DH, int NTH>
 __device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, int r, int head, int j, int nq, int n, float* lds) {
   const int g = head / A.G, d = 4 * (threadIdx.x % (DH / 4));
   float a[4] = {0.f, 0.f, 0.f, 0.f}, M = -INFINITY, L = 0.f;
   bool holds = threadIdx.x < DH / 4;
   if (n > it.k0)
-    holds = plain_query<T, KVT, DH>(A.c, (const KVT*)A.kv, A.c.page_table + (size_t)it.table * A.c.max_pages, g,
+    holds = plain_query<T, KVT, DH, NTH>(A.c, (const KVT*)A.kv, A.c.page_table + (size_t)it.table * A.c.max_pages, g,
                                     (const T*)A.q + r * A.qs + head * DH, A.scale, it.k0, n, lds, M, L, a);
   if (!holds) return;
   if (it.rec < 0) {
@@ -767,12 +942,12 @@ __device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, cha
       qf[s] = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
     }
   }
-  auto pages = [&](int t) { return page_to_read(C, table[min(start / kPage + t * (KT / kPage) + (lane & 1), last / kPage)]); };
+  auto pages = [&](int t) { return table[min(start / kPage + t * (KT / kPage) + (lane & 1), last / kPage)]; };
   auto issue = [&](int buf, int t, int pg) {
 #pragma unroll
     for (int i = 0; i < LPT; i++) {
       const int ch = i * kWG + tid, k = ch / NCH, key = start + t * KT + k;
-      const int page = __builtin_amdgcn_readlane(pg, (i * kWG + w * 64) / (NCH * kPage));
+      const int page = page_to_read(C, __builtin_amdgcn_readlane(pg, (i * kWG + w * 64) / (NCH * kPage)));
       const int in = min(max(key, it.k0), last) % kPage;
       const float* p = pool + (size_t)page * 2 * half + in * DH;
       lbytes* to = (lbytes*)(lds + buf * BUF + (i * kWG + w * 64) * 16);
@@ -881,20 +1056,20 @@ __device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, cha
         const int s = A.seqs[r];
         n = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
       }
-      plain_piece<float, float, DH>(A, it, R, r, g * G + jb % G, jb, nq, min(n, it.k1), (float*)lds);
+      plain_piece<float, float, DH, kWG>(A, it, R, r, g * G + jb % G, jb, nq, min(n, it.k1), (float*)lds);
     }
 }
 
 // Grid: x = KV head (with 8 of them a head's keys stay in one XCD's L2), y = piece.
 template <typename T, int DH>
-__global__ __launch_bounds__(kWG, 2) void k_attend_bf16(SeqArgs A, const int* count, const Item* items, Records R) {
+__global__ __launch_bounds__(kAttWG, 2) void k_attend_bf16(SeqArgs A, const int* count, const Item* items, Records R) {
   extern __shared__ __align__(16) char lds[];
   if ((int)blockIdx.y >= count[0]) return;
   const Item it = items[blockIdx.y];
   if (it.mode & ITEM_NARROW)
-    piece_bf16<T, DH, 2>(A, it, R, lds);
+    piece_bf16<T, DH, true>(A, it, R, lds);
   else
-    piece_bf16<T, DH, 1>(A, it, R, lds);
+    piece_bf16<T, DH, false>(A, it, R, lds);
 }
 
 template <int DH>
@@ -904,66 +1079,93 @@ __global__ __launch_bounds__(kWG, 2) void k_attend_f32(SeqArgs A, const int* cou
   piece_f32<DH>(A, items[blockIdx.y], R, lds);
 }
 
-// Records to outputs. Grid: x = KV head, y = rows to join, z = every kMergeZ-th set of queries.
-constexpr int kMergeZ = 4;
+// Records to outputs. Grid: x = KV head, y = units (strided). The DH / 4 lanes of a query first hold a piece's (m, l) each,
+// which gives the query's maximum and the pieces' factors by shuffles, then four dims each, over eight pieces at once.
+constexpr int kMergeRows = 128;
+
+template <int DH>
+constexpr int merge_queries() { return kWG / (DH / 4); }
 
 template <typename T, int DH>
-__global__ __launch_bounds__(kWG) void k_merge(SeqArgs A, const int* count, const Merge* merges, Records R) {
-  if ((int)blockIdx.y >= count[1]) return;
-  const Merge m = merges[blockIdx.y];
-  constexpr int TPQ = DH / 4, QPI = kWG / TPQ;
-  const int g = blockIdx.x, G = A.G, d = 4 * (threadIdx.x % TPQ);
-  for (int j = blockIdx.z * QPI + threadIdx.x / TPQ; j < m.nrows * G; j += kMergeZ * QPI) {
-    const int r = m.row0 + j / G, head = g * G + j % G;
-    int lim = m.lim0 + j / G;
+__global__ __launch_bounds__(kWG) void k_merge(SeqArgs A, const int* count, const Unit* units, const Merge* merges, Records R) {
+  constexpr int TPQ = DH / 4;
+  const int n = count[1], g = blockIdx.x, G = A.G, hkv = A.c.n_kv_heads, lane = threadIdx.x % TPQ;
+  for (int u = blockIdx.y; u < n; u += gridDim.y) {
+    const Unit un = units[u];
+    const Merge m = merges[un.merge];
+    const int j = un.query + threadIdx.x / TPQ, nq = m.nrows * G, jj = min(j, nq - 1), np = m.pieces[0] + m.pieces[1];
+    auto record = [&](int p) {
+      const int x = p >= m.pieces[0], q = p - (x ? m.pieces[0] : 0);
+      return (size_t)m.rec[x] + (size_t)(q * hkv + g) * m.queries[x] + m.first[x] + jj;
+    };
+    const int r = m.row0 + jj / G, head = g * G + jj % G;
+    int lim = m.lim0 + jj / G;
     if (m.mode & ITEM_FLAT) lim = seq_len(A.c, A.seqs[r]);
-    float M = -INFINITY;
-    for (int x = 0; x < 2; x++)
-      for (int p = 0; p < m.pieces[x]; p++)
-        M = fmaxf(M, R.ml[(size_t)m.rec[x] + (size_t)(p * A.c.n_kv_heads + g) * m.queries[x] + m.first[x] + j].x);
-    float a[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
-    for (int x = 0; x < 2; x++)
-      for (int p = 0; p < m.pieces[x]; p++) {
-        const size_t at = (size_t)m.rec[x] + (size_t)(p * A.c.n_kv_heads + g) * m.queries[x] + m.first[x] + j;
-        const float2 ml = R.ml[at];
-        if (ml.y == 0.f) continue;  // no key of this row; a sum that is NaN goes on
-        const float f = __builtin_amdgcn_exp2f(ml.x - M);
-        const float4 o = *reinterpret_cast<const float4*>(R.o + at * DH + d);
-        L = fmaf(ml.y, f, L);
-        a[0] = fmaf(o.x, f, a[0]);
-        a[1] = fmaf(o.y, f, a[1]);
-        a[2] = fmaf(o.z, f, a[2]);
-        a[3] = fmaf(o.w, f, a[3]);
+    float M = -INFINITY, L = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = 0; p0 < np; p0 += TPQ) {  // a pass but for more pieces than lanes
+      const int p = p0 + lane;
+      const float2 ml = p < np ? R.ml[record(p)] : make_float2(-INFINITY, 0.f);
+      float mp = ml.x;
+#pragma unroll
+      for (int d = 1; d < TPQ; d <<= 1) mp = fmaxf(mp, __shfl_xor(mp, d, TPQ));
+      const float Mn = fmaxf(M, mp);
+      const float before = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - Mn);
+      // no key of this query in the piece: 0; a sum that is NaN goes on
+      const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - Mn);
+      float l = ml.y * f;
+#pragma unroll
+      for (int d = 1; d < TPQ; d <<= 1) l += __shfl_xor(l, d, TPQ);
+      M = Mn;
+      L = L * before + l;
+#pragma unroll
+      for (int e = 0; e < 4; e++) a[e] *= before;
+      const int here = min(TPQ, np - p0);
+      for (int b = 0; b < here; b += 8) {
+        float4 o[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) o[e] = *reinterpret_cast<const float4*>(R.o + record(min(p0 + b + e, np - 1)) * DH + 4 * lane);
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          const float w = __shfl(f, min(b + e, TPQ - 1), TPQ);
+          if (b + e >= here) continue;
+          a[0] = fmaf(o[e].x, w, a[0]);
+          a[1] = fmaf(o[e].y, w, a[1]);
+          a[2] = fmaf(o[e].z, w, a[2]);
+          a[3] = fmaf(o[e].w, w, a[3]);
+        }
       }
-    store4((T*)A.out + r * A.os + head * DH + d, a, lim > 0 ? 1.0f / L : 0.f);
+    }
+    if (j < nq) store4((T*)A.out + r * A.os + head * DH + 4 * lane, a, lim > 0 ? 1.0f / L : 0.f);
   }
 }
 
 // ------------------------------------------------------------------------------------------------------- launches
 // What a call takes: its tiles, and its workspace (the plan's lists, then the records).
 struct Request {
-  int rpt, wanted, jobs, tiles;
-  size_t items, merges, records;
-  size_t at_items, at_merges, at_tiles, at_ml, at_o, bytes;
+  int rpt, wanted, jobs, tiles, qpu;
+  bool merge;
+  size_t items, merges, units, records;
+  size_t at_items, at_merges, at_units, at_tiles, at_ml, at_o, bytes;
 };
 
-Request request(const spd_cache& c, int n_q_heads, int dtype, int nseqs, int rows, int ngroups, bool prefix) {
+Request request(const spd_cache& c, int n_q_heads, int nseqs, int rows, int ngroups, int max_len, bool prefix) {
   Request q{};
   const int hkv = c.n_kv_heads, G = n_q_heads / hkv;
-  q.rpt = 128 / G;
-  q.wanted = std::max(1, kWantedWGs / hkv);
-  if (prefix) {
-    q.tiles = ngroups > 0 ? nseqs / q.rpt + ngroups : 0;
-    q.jobs = q.tiles + nseqs;
-    q.merges = nseqs;
-  } else {
-    q.jobs = rows / q.rpt + nseqs;
-    q.merges = q.wanted;
-  }
-  // jobs over `chunk` >= keys / wanted: fewer than `wanted` of them, with fewer than 2 `wanted` pieces
+  q.rpt = (c.dtype == SPD_BF16 ? 256 : 128) / G;
+  q.qpu = c.head_dim == 128 ? merge_queries<128>() : merge_queries<64>();
+  // a job of at most kMinChunk keys is not split: then prompts have nothing to join
+  const bool split = max_len == 0 || max_len > kMinChunk;
+  q.wanted = split ? std::max(1, kWantedWGs / hkv) : 0;
+  q.merge = split || (prefix && ngroups > 0);
+  q.tiles = prefix && ngroups > 0 ? nseqs / q.rpt + ngroups : 0;
+  q.jobs = prefix ? q.tiles + nseqs : rows / q.rpt + nseqs;
+  // jobs of more than `chunk` >= keys / wanted: fewer than `wanted` of them, with fewer than 2 `wanted` pieces
   q.items = (size_t)q.jobs + 2 * q.wanted;
+  q.merges = prefix ? nseqs : q.wanted;
+  const int most = prefix ? G : std::min(q.rpt, rows) * G;  // queries of a merge
+  q.units = q.merges * ((most + q.qpu - 1) / q.qpu);
   q.records = 2 * (size_t)q.wanted * hkv * std::min(q.rpt, rows) * G;
-  if (prefix) q.records += 2 * (size_t)nseqs * n_q_heads;
+  if (prefix && ngroups > 0) q.records += 2 * (size_t)nseqs * n_q_heads;
   auto take = [&](size_t n) {
     const size_t at = q.bytes;
     q.bytes += (n + 255) / 256 * 256;
@@ -972,6 +1174,7 @@ Request request(const spd_cache& c, int n_q_heads, int dtype, int nseqs, int row
   take(64);  // counts
   q.at_items = take(q.items * sizeof(Item));
   q.at_merges = take(q.merges * sizeof(Merge));
+  q.at_units = take(q.units * sizeof(Unit));
   q.at_tiles = take((size_t)q.tiles * sizeof(int4));
   q.at_ml = take(q.records * sizeof(float2));
   q.at_o = take(q.records * c.head_dim * sizeof(float));
@@ -979,15 +1182,16 @@ Request request(const spd_cache& c, int n_q_heads, int dtype, int nseqs, int row
 }
 
 template <typename T, int DH>
-void launch_merge(const SeqArgs& a, const Request& q, const int* count, const Merge* merges, const Records& r, hipStream_t s) {
-  hipLaunchKernelGGL((k_merge<T, DH>), dim3(a.c.n_kv_heads, (unsigned)q.merges, kMergeZ), dim3(kWG), 0, s, a, count, merges, r);
-}
-
-template <typename T, int DH>
-void launch_bf16(const SeqArgs& a, const Request& q, const int* count, const Item* items, const Records& r, hipStream_t s) {
+void launch(const SeqArgs& a, const Request& q, const PlanArgs& p, const Records& r, hipStream_t s) {
   const dim3 grid(a.c.n_kv_heads, (unsigned)q.items);
-  const size_t shm = 2 * 2 * 64 * DH * 2;
-  hipLaunchKernelGGL((k_attend_bf16<T, DH>), grid, dim3(kWG), shm, s, a, count, items, r);
+  if (a.c.dtype == SPD_BF16) {
+    hipLaunchKernelGGL((k_attend_bf16<T, DH>), grid, dim3(kAttWG), 2 * 2 * 128 * DH * 2, s, a, p.count, p.items, r);
+  } else {
+    hipLaunchKernelGGL((k_attend_f32<DH>), grid, dim3(kWG), 2 * 2 * 32 * DH * 4, s, a, p.count, p.items, r);
+  }
+  if (q.merge)
+    hipLaunchKernelGGL((k_merge<T, DH>), dim3(a.c.n_kv_heads, (unsigned)std::min<size_t>(q.units, kMergeRows)), dim3(kWG), 0, s, a,
+                       p.count, p.units, p.merges, r);
 }
 
 // Plan, pieces, merge.
@@ -1004,33 +1208,25 @@ void run_attention(const SeqArgs& a, int dtype, const Request& q, bool prefix, v
   p.G = a.G;
   p.wanted = q.wanted;
   p.rpt = q.rpt;
+  p.tiles = q.tiles;
+  p.jobs = q.jobs;
+  p.qpu = q.qpu;
   p.records = q.records;
   p.count = (int*)ws;
   p.items = (Item*)(ws + q.at_items);
   p.merges = (Merge*)(ws + q.at_merges);
-  int4* tiles = (int4*)(ws + q.at_tiles);
+  p.units = (Unit*)(ws + q.at_units);
+  p.tile_rec = (int4*)(ws + q.at_tiles);
   const Records r{(float*)(ws + q.at_o), (float2*)(ws + q.at_ml)};
   if (prefix)
-    hipLaunchKernelGGL((k_plan_attention<true>), dim3(1), dim3(kPlanWG), 0, s, p, q.jobs, q.tiles, tiles);
+    hipLaunchKernelGGL((k_plan_attention<true>), dim3(1), dim3(kPlanWG), 0, s, p);
   else
-    hipLaunchKernelGGL((k_plan_attention<false>), dim3(1), dim3(kPlanWG), 0, s, p, q.jobs, q.tiles, tiles);
+    hipLaunchKernelGGL((k_plan_attention<false>), dim3(1), dim3(kPlanWG), 0, s, p);
   const bool wide = a.c.head_dim == 128;
-  if (a.c.dtype == SPD_F32) {
-    const dim3 grid(a.c.n_kv_heads, (unsigned)q.items);
-    const size_t shm = (size_t)2 * 2 * 32 * a.c.head_dim * 4;
-    if (wide)
-      hipLaunchKernelGGL(k_attend_f32<128>, grid, dim3(kWG), shm, s, a, p.count, p.items, r);
-    else
-      hipLaunchKernelGGL(k_attend_f32<64>, grid, dim3(kWG), shm, s, a, p.count, p.items, r);
-  } else if (dtype == SPD_BF16) {
-    wide ? launch_bf16<uint16_t, 128>(a, q, p.count, p.items, r, s) : launch_bf16<uint16_t, 64>(a, q, p.count, p.items, r, s);
-  } else {
-    wide ? launch_bf16<float, 128>(a, q, p.count, p.items, r, s) : launch_bf16<float, 64>(a, q, p.count, p.items, r, s);
-  }
   if (dtype == SPD_BF16)
-    wide ? launch_merge<uint16_t, 128>(a, q, p.count, p.merges, r, s) : launch_merge<uint16_t, 64>(a, q, p.count, p.merges, r, s);
+    wide ? launch<uint16_t, 128>(a, q, p, r, s) : launch<uint16_t, 64>(a, q, p, r, s);
   else
-    wide ? launch_merge<float, 128>(a, q, p.count, p.merges, r, s) : launch_merge<float, 64>(a, q, p.count, p.merges, r, s);
+    wide ? launch<float, 128>(a, q, p, r, s) : launch<float, 64>(a, q, p, r, s);
 }
 
 // What both attentions check of their sizes.
@@ -1084,7 +1280,7 @@ extern "C" spd_status spd_prompt_attention_workspace(const spd_cache* c, int32_t
   const spd_status st = check_sizes(call, c, n_q_heads, dtype, nseqs, max_len);
   if (st != SPD_OK) return st;
   if (!bytes || rows < 0) return invalid(call, "NULL pointer or negative rows");
-  *bytes = request(*c, n_q_heads, dtype, nseqs, rows, 0, false).bytes;
+  *bytes = request(*c, n_q_heads, nseqs, rows, 0, max_len, false).bytes;
   return SPD_OK;
 }
 
@@ -1105,7 +1301,7 @@ extern "C" spd_status spd_prompt_attention(const spd_cache* c, int32_t layer, co
   SeqArgs a = args_of(c, layer, q, q_stride, out, out_stride, n_q_heads, seqs, nseqs);
   a.cu = cu_rows;
   a.rows = rows;
-  run_attention(a, dtype, request(*c, n_q_heads, dtype, nseqs, rows, 0, false), false, workspace, (hipStream_t)stream);
+  run_attention(a, dtype, request(*c, n_q_heads, nseqs, rows, 0, max_len, false), false, workspace, (hipStream_t)stream);
   return check_launch(call);
 }
 
@@ -1116,7 +1312,7 @@ extern "C" spd_status spd_prefix_attention_workspace(const spd_cache* c, int32_t
   if (st != SPD_OK) return st;
   if (nseqs > 4096) return invalid(call, "nseqs must be at most 4096");
   if (!bytes || ngroups < 0 || ngroups > nseqs) return invalid(call, "NULL pointer, or ngroups outside [0, nseqs]");
-  *bytes = request(*c, n_q_heads, dtype, nseqs, nseqs, ngroups, true).bytes;
+  *bytes = request(*c, n_q_heads, nseqs, nseqs, ngroups, max_len, true).bytes;
   return SPD_OK;
 }
 
@@ -1138,6 +1334,6 @@ extern "C" spd_status spd_prefix_attention(const spd_cache* c, int32_t layer, co
   a.prefix = prefix_lens;
   a.ngroups = ngroups;
   a.rows = nseqs;
-  run_attention(a, dtype, request(*c, n_q_heads, dtype, nseqs, nseqs, ngroups, true), true, workspace, (hipStream_t)stream);
+  run_attention(a, dtype, request(*c, n_q_heads, nseqs, nseqs, ngroups, max_len, true), true, workspace, (hipStream_t)stream);
   return check_launch(call);
 }
