@@ -4,7 +4,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "spd_cachefn.h"
 
@@ -28,17 +27,17 @@ struct SeqArgs {
 };
 
 // A query over the keys [k0, k1) in plain fp32, by the whole workgroup, which a query, key or value that is not finite
-// needs: there 0 times a value behind the query's own keys, or a plane's 0 * inf, is NaN on matrix cores. Scores in passes of NTH keys, computed twice
+// needs: there 0 times a value behind the query's own keys, or a plane's 0 * inf, is NaN on matrix cores. Scores in passes of 256 keys, computed twice
 // rather than kept. M, L and a (dims 4 d4 .. + 3 of thread d4 = tid % (DH / 4)) are the maximum, the sum and the
-// output; true in the threads that hold them. lds: NTH * 6 floats.
-template <typename T, typename KVT, int DH, int NTH>
+// output; true in the threads that hold them. lds: kWG * 6 floats.
+template <typename T, typename KVT, int DH>
 __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* table, int g, const T* q, float scale, int k0,
                             int k1, float* lds, float& M, float& L, float (&a)[4]) {
-  constexpr int TPQ = DH / 4, NG = NTH / TPQ, NW = NTH / 64;
+  constexpr int TPQ = DH / 4, NG = kWG / TPQ, NW = kWG / 64;
   const int tid = threadIdx.x, d4 = tid % TPQ, grp = tid / TPQ;
   const size_t half = (size_t)c.n_kv_heads * kPage * DH;
   float* sp = lds;
-  float* sr = lds + NTH;
+  float* sr = lds + kWG;
   auto row = [&](int key) { return pool + page_to_read(c, table[key / kPage]) * 2 * half + (size_t)(g * kPage + key % kPage) * DH; };
   auto score = [&](int key) {
     const KVT* k = row(key);
@@ -55,7 +54,7 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
   };
   float m = -INFINITY;
   bool sound = true;
-  for (int key = k0 + tid; key < k1; key += NTH) {
+  for (int key = k0 + tid; key < k1; key += kWG) {
     const float s = score(key);
     m = fmaxf(m, s);
     sound = sound && s < INFINITY;
@@ -82,7 +81,7 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
     return grp == 0;
   }
   L = a[0] = a[1] = a[2] = a[3] = 0.f;
-  for (int base = k0; base < k1; base += NTH) {
+  for (int base = k0; base < k1; base += kWG) {
     float p = 0.f;
     if (base + tid < k1) {
       const float s = score(base + tid);
@@ -90,7 +89,7 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
     }
     sp[tid] = p;
     __syncthreads();
-    const int n = min(NTH, k1 - base);
+    const int n = min(kWG, k1 - base);
     for (int i = grp; i < n; i += NG) {
       const KVT* v = row(base + i) + half + 4 * d4;
       const float2 v0 = ld2<KVT>(v), v1 = ld2<KVT>(v + 2);
@@ -125,12 +124,6 @@ __device__ __forceinline__ void store4(uint16_t* p, const float (&a)[4], float f
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(a[0] * f, a[1] * f), pack_bf16(a[2] * f, a[3] * f));
 }
 
-// What a query's plain pass leaves in the place of its result in a piece: keys [k0, n) of the piece's.
-struct Item;
-struct Records;
-template <typename T, typename KVT, int DH, int NTH>
-__device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, int r, int head, int j, int nq, int n, float* lds);
-
 // --------------------------------------------------------------------------------------- pieces of the work
 // A call's work is cut on the device, by one workgroup, into pieces: some queries of a KV head (rows times its G
 // heads) over a run of keys. A prompt's tile of rows is a job over the keys up to its last row; a group's rows are jobs
@@ -147,7 +140,7 @@ struct Item {
   int lim0;         // causal: row row0 + i attends keys below lim0 + i
   int mode;
 };
-enum { ITEM_NARROW = 1, ITEM_FLAT = 2 };  // at most 64 queries; each row attends its sequence's keys
+enum { ITEM_FEW = 1, ITEM_FLAT = 2 };  // at most 16 queries; each row attends its sequence's keys
 
 // Rows whose pieces' records are to be joined: those of up to two jobs.
 struct Merge {
@@ -159,7 +152,7 @@ struct Merge {
 
 constexpr int kPlanWG = 1024;
 constexpr int kMinChunk = 256;
-constexpr int kWantedWGs = 256;
+constexpr int kWantedWGs = 512;
 constexpr int kBuckets = 256;
 
 // The sums of some queries: `query` of merge `merge` and those behind it, as many as a workgroup of the merge takes.
@@ -228,7 +221,7 @@ __device__ bool prompt_job(const PlanArgs& P, const Batch& B, int t, Job& j) {
   j.a = 0;
   j.lim0 = (int)max((long long)len - stop + j.row0 + 1, -(1ll << 30));
   j.b = max(0, j.lim0 + j.nrows - 1);
-  j.mode = j.nrows * P.G <= 64 ? ITEM_NARROW : 0;
+  j.mode = j.nrows * P.G <= 16 ? ITEM_FEW : 0;
   return true;
 }
 
@@ -256,7 +249,7 @@ __device__ bool prefix_job(const PlanArgs& P, const Batch& B, int t, Job& j, boo
     j.nrows = min(P.rpt, rows - (int)at);
     j.table = B.seq_at(first);
     j.b = n;
-    j.mode = ITEM_FLAT | (j.nrows * P.G <= 64 ? ITEM_NARROW : 0);
+    j.mode = ITEM_FLAT | (j.nrows * P.G <= 16 ? ITEM_FEW : 0);
     shared = true;
     return true;
   }
@@ -266,7 +259,7 @@ __device__ bool prefix_job(const PlanArgs& P, const Batch& B, int t, Job& j, boo
   j.nrows = 1;
   j.table = B.seq_at(r);
   j.b = len;
-  j.mode = ITEM_FLAT | ITEM_NARROW;
+  j.mode = ITEM_FLAT | ITEM_FEW;
   if (P.ngroups > 0) {
     const int g = B.last_at(P.ngroups, r, 1, 0), n = shared_prefix(P, B, g, first, rows);
     if (n > 0 && r >= first && r < first + rows) {
@@ -339,7 +332,7 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
   const int chunk = want >= (unsigned)s_max ? (s_max + 63) / 64 * 64 : max(kMinChunk, (int)((want + 63) / 64 * 64));
   const float per_key = (float)(kBuckets - 1) / (2.0f * (float)min(s_max, chunk));
   auto bucket = [&](int n, int mode) {  // the longest first; a key of a wide piece costs about twice a narrow one's
-    return kBuckets - 1 - min((int)((float)n * (mode & ITEM_NARROW ? 1.0f : 2.0f) * per_key), kBuckets - 1);
+    return kBuckets - 1 - min((int)((float)n * (mode & ITEM_FEW ? 1.0f : 2.0f) * per_key), kBuckets - 1);
   };
   // a job's pieces; 0: nothing to do (a row that ends with its prefix)
   auto pieces_of = [&](const Job& j, bool sh) { return j.b > j.a ? (j.b - j.a + chunk - 1) / chunk : sh ? 0 : 1; };
@@ -432,6 +425,7 @@ struct Records {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(1))) const char gbytes;
 typedef __attribute__((address_space(3))) char lbytes;
 typedef __attribute__((address_space(3))) bf16x4 lbf16x4;
@@ -448,6 +442,71 @@ __device__ __forceinline__ void planes3(float x, uint32_t& h, uint32_t& m, uint3
 
 constexpr float kLog2e = 1.44269504088896341f;
 
+// Two probabilities (finite, not negative) as planes of a product's operand: rounded to one bf16 each, or three that are exact.
+__device__ __forceinline__ void planes_of(float p0, float p1, uint32_t (&u)[1]) { u[0] = pack_bf16(p0, p1); }
+__device__ __forceinline__ void planes_of(float p0, float p1, uint32_t (&u)[3]) {
+  const uint32_t h0 = __float_as_uint(p0), h1 = __float_as_uint(p1);
+  const float r0 = p0 - __uint_as_float(h0 & 0xffff0000u), r1 = p1 - __uint_as_float(h1 & 0xffff0000u);
+  const uint32_t m0 = __float_as_uint(r0), m1 = __float_as_uint(r1);
+  const uint32_t l0 = __float_as_uint(r0 - __uint_as_float(m0 & 0xffff0000u));
+  const uint32_t l1 = __float_as_uint(r1 - __uint_as_float(m1 & 0xffff0000u));
+  u[0] = __builtin_amdgcn_perm(h1, h0, 0x07060302u);
+  u[1] = __builtin_amdgcn_perm(m1, m0, 0x07060302u);
+  u[2] = __builtin_amdgcn_perm(l1, l0, 0x07060302u);
+}
+
+// A lane's part of a query: 8 dims from q on, every `step`. bf16 as they are; fp32 times f, as planes.
+template <typename T, int KS, int STEP, int NP>
+__device__ __forceinline__ void load_query(bf16x8 (&qf)[NP][KS], const T* q, float f) {
+#pragma unroll
+  for (int s = 0; s < KS; s++) {
+    if constexpr (NP == 1) {
+      qf[0][s] = *reinterpret_cast<const bf16x8*>(q + s * STEP);
+    } else {
+      float x[8];
+      load8(q + s * STEP, x);
+      union { uint16_t u[8]; bf16x8 v; } t[3];
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        uint32_t a, b, c;
+        planes3(x[e] * f, a, b, c);
+        t[0].u[e] = (uint16_t)a;
+        t[1].u[e] = (uint16_t)b;
+        t[2].u[e] = (uint16_t)c;
+      }
+#pragma unroll
+      for (int p = 0; p < 3; p++) qf[p][s] = t[p].v;
+    }
+  }
+}
+
+// Keys that a row of a piece attends (of the whole sequence).
+__device__ __forceinline__ int row_limit(const SeqArgs& A, const Item& it, int row) {
+  if (!(it.mode & ITEM_FLAT)) return it.lim0 + row - it.row0;
+  const int s = A.seqs[row];
+  return (unsigned)s < (unsigned)A.c.max_seqs ? seq_len(A.c, s) : 0;
+}
+
+// Query j of a piece again, in plain arithmetic, in the place of its result.
+template <typename T, typename KVT, int DH>
+__device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, int j, float* lds) {
+  const int g = blockIdx.x, r = it.row0 + j / A.G, head = g * A.G + j % A.G, d = 4 * (threadIdx.x % (DH / 4));
+  const int n = min(row_limit(A, it, r), it.k1);
+  float a[4] = {0.f, 0.f, 0.f, 0.f}, M = -INFINITY, L = 0.f;
+  bool holds = threadIdx.x < DH / 4;
+  if (n > it.k0)
+    holds = plain_query<T, KVT, DH>(A.c, (const KVT*)A.kv, A.c.page_table + (size_t)it.table * A.c.max_pages, g,
+                                    (const T*)A.q + r * A.qs + head * DH, A.scale, it.k0, n, lds, M, L, a);
+  if (!holds) return;
+  if (it.rec < 0) {
+    store4((T*)A.out + r * A.os + head * DH + d, a, n > 0 ? 1.0f / L : 0.f);
+  } else {
+    const size_t at = (size_t)it.rec + (size_t)g * it.nrows * A.G + j;
+    store4(R.o + at * DH + d, a, 1.0f);
+    if (d == 0) R.ml[at] = make_float2(M * kLog2e, L);
+  }
+}
+
 // A piece of bf16 keys for 32 queries a wave. Query j of the tile is row row0 + j / G, head g * G + j % G.
 //   S^T = K Q^T (v_mfma_f32_32x32x16_bf16: lane l supplies 8 consecutive k of A row l % 32 and of B column l % 32, from
 //     k = 8 (l / 32); accumulator register v of lane l is row 8 (v / 4) + 4 (l / 32) + v % 4, column l % 32): lane l
@@ -460,30 +519,18 @@ constexpr float kLog2e = 1.44269504088896341f;
 // bf16 queries: q as it is, the scale in the exponent's FMA, p rounded to bf16 (half a step, 2^-8 of each p: as much as the
 // rounding of the output), l the sum of the rounded p. fp32 queries: q (scaled in fp32) and p as three exact planes, three products each.
 // K and V go to LDS by direct loads, the 16-byte chunks of a row permuted by its key so that neither kind of read
-// meets itself in a bank.
-//
-// Wide (256 queries, eight waves on 32 each): a wave's step has a matrix phase, the scores of the next tile and the
-// products of this one, and a vector phase, the next tile's softmax, each about 1000 cycles for 64 keys. The waves
-// of a SIMD, w and w + 4, take turns: barriers between the phases keep one in its matrix phase while the other is in its
-// vector phase. Slot 2 t is wave 0..3's matrix phase of step t and wave 4..7's vector phase of step t - 1. Tiles
-// K(t + 2) and V(t + 1) are requested at the start of slot 2 t, when the last reads of K(t) and V(t - 1) are
-// over, and waited for at the end of slot 2 t + 1.
-// Narrow (up to 64 queries): four waves share a tile's 128 keys, two the queries; what bounds it is the stream of keys,
-// two tiles deep.
-constexpr int kAttWG = 512;
-
-template <typename T, int DH, bool NARROW>
-__device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, char* lds) {
+// meets itself in a bank. A step reads its V fragments before it requests the next tile: the compiler lets every read of LDS
+// wait for the direct loads before it, and so the request has the softmax and the products to land in.
+// Two workgroups are on a CU, so that one's matrix work meets the other's vector work.
+template <typename T, int DH>
+__device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, char* lds) {
   constexpr int NP = sizeof(T) == 4 ? 3 : 1;
-  constexpr int WK = NARROW ? 4 : 1;
-  constexpr int KT = NARROW ? 128 : NP == 3 && DH == 128 ? 32 : 64;  // 32: three planes of q leave no registers for 64
-  constexpr int NT = DH / 32, KS = DH / 16, NCH = DH / 8;
-  constexpr int SB = NARROW ? 1 : KT / 32;  // 32-key blocks of a wave's step
-  constexpr int KBUF = KT * DH * 2, LPT = KT * NCH / kAttWG;
+  constexpr int KT = NP == 3 && DH == 128 ? 32 : 64;  // 32: three planes of q leave no registers for 64
+  constexpr int NT = DH / 32, KS = DH / 16, NCH = DH / 8, SB = KT / 32;
+  constexpr int KBUF = KT * DH * 2, LPT = KT * NCH / kWG;
   constexpr int KROT = DH == 128 ? 0 : 1;  // K: chunk c of key k sits at c ^ (k >> KROT) % NCH: 16 keys in 64 banks
   constexpr int VROT = DH == 128 ? 0 : 1;  // V: chunk c of key k sits at c ^ (k % 8 >> VROT) << 1
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
-  const int wk = WK == 1 ? 0 : w % WK, wq = WK == 1 ? w : w / WK;
   const int g = blockIdx.x, G = A.G, nq = it.nrows * G;
   const spd_cache& C = A.c;
   const int last = it.k1 - 1;
@@ -492,40 +539,13 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
   const uint16_t* pool = (const uint16_t*)A.kv + (size_t)g * kPage * DH;
   const int* table = C.page_table + (size_t)it.table * C.max_pages;
   const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;  // from scores to exponents
-  const bool active = wq * 32 < nq;
-  const int jq = wq * 32 + col, jj = min(jq, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
+  const bool active = w * 32 < nq;
+  const int jq = w * 32 + col, jj = min(jq, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
   const bool mine = jq < nq;
-  int lim = it.lim0 + jj / G;
-  if (it.mode & ITEM_FLAT) {
-    const int s = A.seqs[row];
-    lim = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
-  }
-  lim = min(lim, it.k1);
+  const int lim = min(row_limit(A, it, row), it.k1);
 
   bf16x8 qf[NP][KS];
-  {
-    const T* q = (const T*)A.q + row * A.qs + head * DH + h * 8;
-#pragma unroll
-    for (int s = 0; s < KS; s++) {
-      if constexpr (NP == 1) {
-        qf[0][s] = *reinterpret_cast<const bf16x8*>(q + s * 16);
-      } else {
-        float f[8];
-        load8(q + s * 16, f);
-        union { uint16_t u[8]; bf16x8 v; } t[3];
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          uint32_t x, y, z;
-          planes3(f[e] * (A.scale * kLog2e), x, y, z);
-          t[0].u[e] = (uint16_t)x;
-          t[1].u[e] = (uint16_t)y;
-          t[2].u[e] = (uint16_t)z;
-        }
-#pragma unroll
-        for (int p = 0; p < 3; p++) qf[p][s] = t[p].v;
-      }
-    }
-  }
+  load_query<T, KS, 16>(qf, (const T*)A.q + row * A.qs + head * DH + h * 8, A.scale * kLog2e);
   // keys below wmin are attended by every query of the wave, none at wmax and above by any
   int wmin = lim, wmax = lim;
 #pragma unroll
@@ -534,50 +554,42 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
     wmax = max(wmax, __shfl_xor(wmax, d, 64));
   }
   wmin = __builtin_amdgcn_readfirstlane(wmin);
-  wmax = __builtin_amdgcn_readfirstlane(wmax);
+  wmax = __builtin_amdgcn_readfirstlane(active ? wmax : 0);
 
   // The pages of a tile, one a lane (mod their number), are read a tile ahead of their use, and looked at only there: a look
   // at them here would wait for them and for the keys requested before them.
   auto pages = [&](int t) { return table[min(start / kPage + t * (KT / kPage) + (lane & (KT / kPage - 1)), last / kPage)]; };
-  // A thread's bytes of a page, load i: chunk ch % NCH of key ch / NCH. All loads of a thread are of the same key of a page,
-  // or of keys 16 apart, so one offset serves them.
+  // A thread's bytes of a page, load i: chunk lc of key lk, or of keys 16 apart.
   const int lk = tid / NCH, lc = tid % NCH;
-  static_assert(kAttWG / NCH % kPage == 0 && LPT >= 1, "a pass of the workgroup is whole pages");
+  static_assert(kWG / NCH % kPage == 0 && LPT >= 1, "a pass of the workgroup is whole pages");
   const uint32_t koff = (lc ^ (lk >> KROT) % NCH) << 4;
   const uint32_t voff = (lc ^ (lk & 7) >> VROT << 1) << 4;
   const size_t page_bytes = 2 * half * sizeof(uint16_t);
-  // The pages of a thread's loads, in scalar registers: looked at between loads, a lane's register would wait for those before it.
-  struct Pages {
-    int p[LPT];
-  };
-  auto own_pages = [&](int pg) {
-    Pages x;
+  // Tile t. Keys outside [k0, k1) are read as the nearest one inside: their probability is 0, and 0 times a value must be 0. The
+  // pages go to scalar registers first: looked at between loads, a lane's register would wait for those before it.
+  auto request = [&](int t, int pg) {
+    const int first = start + t * KT, to = (t & 1) * 2 * KBUF;
+    int page[LPT];
 #pragma unroll
-    for (int i = 0; i < LPT; i++) x.p[i] = page_to_read(C, __builtin_amdgcn_readlane(pg, (i * kAttWG + w * 64) / (NCH * kPage)));
-    return x;
-  };
-  // Tile t's keys or values to `to`. Keys outside [k0, k1) are read as the nearest one inside: their probability is 0, and 0
-  // times a value must be 0. (So is a tile behind the last one, which saves the loop a branch and is not used.)
-  auto load = [&](int to, int t, const Pages& pages, uint32_t off, size_t plane) {
-    const int first = start + t * KT;
+    for (int i = 0; i < LPT; i++) page[i] = page_to_read(C, __builtin_amdgcn_readlane(pg, (i * kWG + w * 64) / (NCH * kPage)));
 #pragma unroll
     for (int i = 0; i < LPT; i++) {
-      const uint32_t at = (uint32_t)(min(max(first + i * (kAttWG / NCH) + lk, it.k0), last) & (kPage - 1)) * (DH * 2) + off;
-      __builtin_amdgcn_global_load_lds((gbytes*)pool + (size_t)pages.p[i] * page_bytes + plane + at,
-                                       (lbytes*)(lds + to + (i * kAttWG + w * 64) * 16), 16, 0, 0);
+      const uint32_t at = (uint32_t)(min(max(first + i * (kWG / NCH) + lk, it.k0), last) & (kPage - 1)) * (DH * 2);
+      gbytes* p = (gbytes*)pool + (size_t)page[i] * page_bytes;
+      lbytes* l = (lbytes*)(lds + to + (i * kWG + w * 64) * 16);
+      __builtin_amdgcn_global_load_lds(p + (at + koff), l, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(p + half * sizeof(uint16_t) + (at + voff), l + KBUF, 16, 0, 0);
     }
   };
-  auto load_k = [&](int to, int t, const Pages& p) { load(to, t, p, koff, 0); };
-  auto load_v = [&](int to, int t, const Pages& p) { load(to, t, p, voff, half * sizeof(uint16_t)); };
   // A lane's bytes of a K or V tile.
   uint32_t ka[KS], va[NT];
 #pragma unroll
-  for (int k = 0; k < KS; k++) ka[k] = (WK == 1 ? 0 : wk * 32 * DH * 2) + col * DH * 2 + (((2 * k + h) ^ (col >> KROT) % NCH) << 4);
+  for (int k = 0; k < KS; k++) ka[k] = col * DH * 2 + (((2 * k + h) ^ (col >> KROT) % NCH) << 4);
 #pragma unroll
   for (int tt = 0; tt < NT; tt++) {
     // lane l % 16 of each 16: 8 bytes of row (l % 16) / 4 of its four keys; it gets dim l % 16 of all four
-    const int vk = (WK == 1 ? 0 : wk * 32) + h * 4 + (lane & 15) / 4, c = tt * 4 + (lane & 16) / 8 + (lane & 3) / 2;
-    va[tt] = vk * DH * 2 + ((c ^ (vk & 7) >> VROT << 1) << 4) + (lane & 1) * 8;
+    const int vk = h * 4 + (lane & 15) / 4, c = tt * 4 + (lane & 16) / 8 + (lane & 3) / 2;
+    va[tt] = KBUF + vk * DH * 2 + ((c ^ (vk & 7) >> VROT << 1) << 4) + (lane & 1) * 8;
   }
 
   f32x16 o[NT];
@@ -585,24 +597,66 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
   for (int t = 0; t < NT; t++) o[t] = (f32x16)(0.f);
   float m_run = -INFINITY, l_run = 0.f;
 
-  f32x16 s[SB];
-  union { uint32_t u[8]; bf16x8 f[2]; } pf[SB][NP];
-  // s = scores of the SB blocks at kt
-  auto scores = [&](const char* kt) {
+  int pg = 0;
+  if (tiles > 0) {
+    request(0, pages(0));
+    pg = pages(1);
+  }
+  for (int t = 0; t < tiles; t++) {
+    const char* tile = lds + (t & 1) * 2 * KBUF;
+    const int kb = start + t * KT;  // the tile's first key
+    // tile t has landed, every wave's part of it, and every wave is done with the one before
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (kb >= wmax) {
+      if (t + 1 < tiles) {
+        request(t + 1, pg);
+        pg = pages(t + 2);
+      }
+      continue;
+    }
+    f32x16 s[SB];
 #pragma unroll
     for (int x = 0; x < SB; x++)
 #pragma unroll
       for (int k = 0; k < KS; k++) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + ka[k] + x * 32 * DH * 2);
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + ka[k] + x * 32 * DH * 2);
 #pragma unroll
         for (int p = NP - 1; p >= 0; p--)
           s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[p][k], (p == NP - 1 && k == 0) ? (f32x16)(0.f) : s[x], 0, 0, 0);
       }
-  };
-  // p of the scores of the keys from kb on
-  auto softmax = [&](int kb) {
-    if (kb < it.k0 || kb + SB * 32 > wmin) {  // some key is not every query's
-      asm volatile("");                       // stays a branch: the masks cost as much as a third of the step's vector work
+    bf16x8 vf[SB][2][NT];
+#pragma unroll
+    for (int x = 0; x < SB; x++)
+#pragma unroll
+      for (int ks = 0; ks < 2; ks++)
+#pragma unroll
+        for (int tt = 0; tt < NT; tt++) {
+          union { bf16x4 q[2]; bf16x8 f; } u;
+#pragma unroll
+          for (int y = 0; y < 2; y++)
+            u.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lbf16x4*)(lbytes*)(tile + va[tt] + (x * 32 + ks * 16 + y * 8) * DH * 2));
+          vf[x][ks][tt] = u.f;
+        }
+    // the keys' fragments half a block ahead of their products, the values' among the last products
+    __builtin_amdgcn_sched_group_barrier(0x100, KS, 0);
+    if constexpr (SB > 1) {
+#pragma unroll
+      for (int k = 0; k < KS; k++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, NP, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < KS; k++) {
+      __builtin_amdgcn_sched_group_barrier(0x008, NP, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4 * NT * SB / KS, 0);
+    }
+    if (t + 1 < tiles) {
+      request(t + 1, pg);
+      pg = pages(t + 2);
+    }
+    if (kb < it.k0 || kb + KT > wmin) {  // some key is not every query's
+      asm volatile("");                  // stays a branch: the masks cost as much as a third of the step's vector work
 #pragma unroll
       for (int x = 0; x < SB; x++)
 #pragma unroll
@@ -630,282 +684,242 @@ __device__ void piece_bf16(const SeqArgs& A, const Item& it, const Records R, ch
     }
     const float off = m_run == -INFINITY ? 0.f : m_run;  // a query without a key yet: every p is 0
 #pragma unroll
-    for (int x = 0; x < SB; x++)
+    for (int x = 0; x < SB; x++) {
+      union { uint32_t u[8]; bf16x8 f[2]; } pf[NP];
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
         const float p0 = __builtin_amdgcn_exp2f(fmaf(s[x][e], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(s[x][e + 1], sc, -off));
         l_run += p0 + p1;
-        if constexpr (NP == 1) {
-          pf[x][0].u[e >> 1] = pack_bf16(p0, p1);
-        } else {
-          const uint32_t h0 = __float_as_uint(p0), h1 = __float_as_uint(p1);
-          const float r0 = p0 - __uint_as_float(h0 & 0xffff0000u), r1 = p1 - __uint_as_float(h1 & 0xffff0000u);
-          const uint32_t m0 = __float_as_uint(r0), m1 = __float_as_uint(r1);
-          const uint32_t l0 = __float_as_uint(r0 - __uint_as_float(m0 & 0xffff0000u));
-          const uint32_t l1 = __float_as_uint(r1 - __uint_as_float(m1 & 0xffff0000u));
-          pf[x][0].u[e >> 1] = __builtin_amdgcn_perm(h1, h0, 0x07060302u);
-          pf[x][1].u[e >> 1] = __builtin_amdgcn_perm(m1, m0, 0x07060302u);
-          pf[x][2].u[e >> 1] = __builtin_amdgcn_perm(l1, l0, 0x07060302u);
-        }
+        uint32_t pl[NP];
+        planes_of(p0, p1, pl);
+#pragma unroll
+        for (int p = 0; p < NP; p++) pf[p].u[e >> 1] = pl[p];
       }
-#pragma unroll
-    for (int x = 0; x < SB; x++)
-#pragma unroll
-      for (int p = 0; p < NP; p++) asm volatile("" : "+v"(pf[x][p].f[0]), "+v"(pf[x][p].f[1]));  // here, not behind a barrier
-  };
-  // o += p V of the blocks at vt
-  auto products = [&](const char* vt) {
-#pragma unroll
-    for (int x = 0; x < SB; x++)
 #pragma unroll
       for (int ks = 0; ks < 2; ks++)
 #pragma unroll
-        for (int tt = 0; tt < NT; tt++) {
-          union { bf16x4 q[2]; bf16x8 f; } vf;
-#pragma unroll
-          for (int y = 0; y < 2; y++)
-            vf.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lbf16x4*)(lbytes*)(vt + va[tt] + (x * 32 + ks * 16 + y * 8) * DH * 2));
+        for (int tt = 0; tt < NT; tt++)
 #pragma unroll
           for (int p = NP - 1; p >= 0; p--)
-            o[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.f, pf[x][p].f[ks], o[tt], 0, 0, 0);
-        }
-  };
-  // A wave comes to the barrier with its own LDS reads over, and landed all but its newest `outstanding` direct loads (-1: any).
-  auto barrier = [&](auto outstanding) {
-    constexpr int N = decltype(outstanding)::value;
-    __builtin_amdgcn_sched_barrier(0);
-    if constexpr (N >= 0)
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
-    else
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  using All = std::integral_constant<int, 0>;
-  using None = std::integral_constant<int, -1>;
-
-  if constexpr (NARROW) {
-    int pg = 0;
-    if (tiles > 0) {
-      const Pages p = own_pages(pages(0));
-      load_k(0, 0, p);
-      load_v(KBUF, 0, p);
-      pg = pages(1);
+            o[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x][ks][tt], pf[p].f[ks], o[tt], 0, 0, 0);
     }
-    for (int t = 0; t < tiles; t++) {
-      const int buf = (t & 1) * 2 * KBUF, next = (t & 1 ^ 1) * 2 * KBUF, kb = start + t * KT + wk * 32;
-      barrier(All{});
-      if (t + 1 < tiles) {
-        const Pages p = own_pages(pg);
-        pg = pages(t + 2);
-        load_k(next, t + 1, p);
-        load_v(next + KBUF, t + 1, p);
-      }
-      if (!active || kb >= wmax) continue;
-      scores(lds + buf);
-      softmax(kb);
-      products(lds + buf + KBUF);
-    }
-  } else if (tiles > 0) {
-    const bool late = w >= kAttWG / 128;
-    // K(t) is at t % 3 KBUF, V(t) at (3 + t % 3) KBUF: places of K(t + 1), V(t), K(t + 3) and V(t + 2)
-    int kat = 0, vat = 2 * KBUF;
-    auto turn = [&](int& at) { at = at == 2 * KBUF ? 0 : at + KBUF; };
-    Pages pk = own_pages(pages(0)), pv = pk;  // of K(t + 3) and V(t + 2)
-    int pg = pages(1);
-    load_k(0, 0, pk);
-    load_v(3 * KBUF, 0, pv);
-    pk = own_pages(pg);
-    load_k(KBUF, 1, pk);
-    pv = pk;
-    pg = pages(2);
-    // Behind a phase's LDS reads: the compiler lets a read of LDS wait for every direct load before it.
-    auto request = [&](int t) {
-      pk = own_pages(pg);
-      pg = pages(t + 4);
-      load_k(kat == 0 ? 2 * KBUF : kat - KBUF, t + 3, pk);
-      load_v(3 * KBUF + (vat == 0 ? 2 * KBUF : vat - KBUF), t + 2, pv);
-      pv = pk;
-      turn(kat);
-      turn(vat);
-    };
-    const int mine_tiles = active ? min(max((wmax - start + KT - 1) / KT, 0), tiles) : 0;  // tiles with keys of this wave's queries
-    barrier(All{});
-    if (late) barrier(None{});
-    if (mine_tiles > 0) scores(lds);
-    barrier(All{});
-    request(-1);
-    if (mine_tiles > 0) softmax(start);
-    barrier(None{});
-    int t;
-#pragma unroll 1
-    for (t = 0; t < mine_tiles - 1; t++) {
-      const char *kt = lds + kat, *vt = lds + 3 * KBUF + vat;
-      if constexpr (NP == 1) {
-        // fragments are read a batch ahead of the products that take them; p first: its registers are free when the scores come
-        bf16x8 f[2][2 * NT > KS ? 2 * NT : KS];
-        auto read_k = [&](bf16x8* f, int x) {
-#pragma unroll
-          for (int k = 0; k < KS; k++) f[k] = *reinterpret_cast<const bf16x8*>(kt + ka[k] + x * 32 * DH * 2);
-        };
-        auto read_v = [&](bf16x8* f, int x) {
-#pragma unroll
-          for (int i = 0; i < 2 * NT; i++) {
-            union { bf16x4 q[2]; bf16x8 f; } vf;
-#pragma unroll
-            for (int y = 0; y < 2; y++)
-              vf.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-                  (lbf16x4*)(lbytes*)(vt + va[i % NT] + (x * 32 + i / NT * 16 + y * 8) * DH * 2));
-            f[i] = vf.f;
-          }
-        };
-        read_v(f[0], 0);
-        read_v(f[1], 1);
-#pragma unroll
-        for (int x = 0; x < SB; x++)
-#pragma unroll
-          for (int i = 0; i < 2 * NT; i++)
-            o[i % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[x][i], pf[x][0].f[i / NT], o[i % NT], 0, 0, 0);
-        bf16x8 fk[2][KS];
-        read_k(fk[0], 0);
-        read_k(fk[1], 1);
-#pragma unroll
-        for (int x = 0; x < SB; x++)
-#pragma unroll
-          for (int k = 0; k < KS; k++) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[x][k], qf[0][k], k == 0 ? (f32x16)(0.f) : s[x], 0, 0, 0);
-        // reads of LDS a batch ahead of the products that take them
-        __builtin_amdgcn_sched_group_barrier(0x100, 4 * NT, 0);
-#pragma unroll
-        for (int i = 0; i < 2 * NT; i++) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 2 * KS; i++) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, 2 * NT, 0);
-      } else {
-        products(vt);
-        scores(kt);
-      }
-      barrier(All{});
-      request(t);
-      softmax(start + (t + 1) * KT);
-      barrier(None{});
-    }
-    if (mine_tiles > 0) {
-      products(lds + 3 * KBUF + vat);
-      barrier(All{});
-      request(t++);
-      barrier(None{});
-    }
-#pragma unroll 1
-    for (; t < tiles; t++) {
-      barrier(All{});
-      request(t);
-      barrier(None{});
-    }
-    if (!late) barrier(None{});
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the tiles behind the last one, before the memory has another use
   }
   l_run += __shfl_xor(l_run, 32, 64);
 
-  constexpr int NQB = kAttWG / 64 / WK;  // sets of 32 queries
-  __shared__ uint32_t s_bad[NQB];  // queries whose result here is not a number
-  if constexpr (WK > 1) {         // the waves of other keys hand their sums to the first
-    __syncthreads();
-    float* ox = (float*)lds + (size_t)wq * (WK - 1) * (NT * 16 + 2) * 64 + lane;
-    if (wk > 0 && active) {
-      float* mine_x = ox + (wk - 1) * (NT * 16 + 2) * 64;
-#pragma unroll
-      for (int tt = 0; tt < NT; tt++)
-#pragma unroll
-        for (int v = 0; v < 16; v++) mine_x[(tt * 16 + v) * 64] = o[tt][v];
-      mine_x[NT * 16 * 64] = m_run;
-      mine_x[(NT * 16 + 1) * 64] = l_run;
-    }
-    __syncthreads();
-    if (wk == 0 && active) {
-#pragma unroll 1
-      for (int x = 1; x < WK; x++, ox += (NT * 16 + 2) * 64) {
-        const float m1 = ox[NT * 16 * 64], l1 = ox[(NT * 16 + 1) * 64];
-        const float mn = fmaxf(m_run, m1);
-        const float f0 = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mn);
-        const float f1 = m1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1 - mn);
-        l_run = l_run * f0 + l1 * f1;
-        m_run = mn;
-#pragma unroll
-        for (int tt = 0; tt < NT; tt++)
-#pragma unroll
-          for (int v = 0; v < 16; v++) o[tt][v] = fmaf(ox[(tt * 16 + v) * 64], f1, o[tt][v] * f0);
-      }
-    }
-  }
-  if (tid < NQB) s_bad[tid] = 0u;
+  __shared__ uint32_t s_bad[kWG / 64];  // queries whose result here is not a number
+  if (tid < kWG / 64) s_bad[tid] = 0u;
   __syncthreads();
-  if (wk == 0 && active) {
+  if (active) {
     bool bad = !(l_run > 0.f) && lim > it.k0;  // NaN, or nothing but scores of -inf
 #pragma unroll
     for (int tt = 0; tt < NT; tt++)
 #pragma unroll
       for (int v = 0; v < 16; v++) bad = bad || o[tt][v] != o[tt][v];
     const unsigned long long bads = __ballot(bad && mine);
-    if (lane == 0) s_bad[wq] = (uint32_t)bads | (uint32_t)(bads >> 32);
+    if (lane == 0) s_bad[w] = (uint32_t)bads | (uint32_t)(bads >> 32);
     if (mine) {
-      if (it.rec < 0) {
-        const float inv = lim > 0 ? 1.0f / l_run : 0.f;
-        T* out = (T*)A.out + row * A.os + head * DH + 4 * h;
+      const size_t at = (size_t)max(it.rec, 0) + (size_t)g * nq + jq;
+      const float inv = lim > 0 ? 1.0f / l_run : 0.f;
 #pragma unroll
-        for (int tt = 0; tt < NT; tt++)
+      for (int tt = 0; tt < NT; tt++)
 #pragma unroll
-          for (int v = 0; v < 16; v += 4) {
-            const float x[4] = {o[tt][v], o[tt][v + 1], o[tt][v + 2], o[tt][v + 3]};
-            store4(out + tt * 32 + 2 * v, x, inv);
-          }
-      } else {
-        const size_t at = (size_t)it.rec + (size_t)g * nq + jq;
-        float* rec = R.o + at * DH + 4 * h;
-#pragma unroll
-        for (int tt = 0; tt < NT; tt++)
-#pragma unroll
-          for (int v = 0; v < 16; v += 4) {
-            const float x[4] = {o[tt][v], o[tt][v + 1], o[tt][v + 2], o[tt][v + 3]};
-            store4(rec + tt * 32 + 2 * v, x, 1.0f);
-          }
-        if (h == 0) R.ml[at] = make_float2(m_run, l_run);
-      }
+        for (int v = 0; v < 16; v += 4) {
+          const float x[4] = {o[tt][v], o[tt][v + 1], o[tt][v + 2], o[tt][v + 3]};
+          const int d = tt * 32 + 2 * v + 4 * h;
+          if (it.rec < 0)
+            store4((T*)A.out + row * A.os + head * DH + d, x, inv);
+          else
+            store4(R.o + at * DH + d, x, 1.0f);
+        }
+      if (it.rec >= 0 && h == 0) R.ml[at] = make_float2(m_run, l_run);
     }
   }
   __syncthreads();  // every result is stored, and the tiles are free
-  for (int i = 0; i < NQB; i++)
-    for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u) {
-      const int jb = i * 32 + __builtin_ctz(m), r = it.row0 + jb / G;
-      int n = it.lim0 + jb / G;
-      if (it.mode & ITEM_FLAT) {
-        const int s = A.seqs[r];
-        n = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
-      }
-      plain_piece<T, uint16_t, DH, kAttWG>(A, it, R, r, g * G + jb % G, jb, nq, min(n, it.k1), (float*)lds);
-    }
+  for (int i = 0; i < kWG / 64; i++)
+    for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u)
+      plain_piece<T, uint16_t, DH>(A, it, R, i * 32 + __builtin_ctz(m), (float*)lds);
 }
 
-template <typename T, typename KVT, int DH, int NTH>
-__device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, int r, int head, int j, int nq, int n, float* lds) {
-  const int g = head / A.G, d = 4 * (threadIdx.x % (DH / 4));
-  float a[4] = {0.f, 0.f, 0.f, 0.f}, M = -INFINITY, L = 0.f;
-  bool holds = threadIdx.x < DH / 4;
-  if (n > it.k0)
-    holds = plain_query<T, KVT, DH, NTH>(A.c, (const KVT*)A.kv, A.c.page_table + (size_t)it.table * A.c.max_pages, g,
-                                    (const T*)A.q + r * A.qs + head * DH, A.scale, it.k0, n, lds, M, L, a);
-  if (!holds) return;
-  if (it.rec < 0) {
-    store4((T*)A.out + r * A.os + head * DH + d, a, n > 0 ? 1.0f / L : 0.f);
-  } else {
-    const size_t at = (size_t)it.rec + (size_t)g * nq + j;
-    store4(R.o + at * DH + d, a, 1.0f);
-    if (d == 0) R.ml[at] = make_float2(M * kLog2e, L);
+// A piece of bf16 keys for up to 16 queries: each wave takes every fourth set of 32 keys by itself, with no barrier until
+// the end. What bounds it is the stream of keys, so a wave keeps the next 32 keys and values on the way (16 KB, 128 KB
+// a CU) while it works on these.
+//   S^T = K Q^T (v_mfma_f32_16x16x32_bf16: lane l supplies 8 consecutive k of A row l % 16 and of B column l % 16, from k =
+//     8 (l / 16); accumulator register v of lane l is row 4 (l / 16) + v, column l % 16).
+//   O^T += V^T P^T over the 32 keys at once: k = 8 q .. 8 q + 7 of lanes 16 q .. are the keys 4 q + 0..3 and 16 + 4 q + 0..3 whose
+//     probabilities they hold. K and V pass through a tile of LDS of the wave's own: loads take whole rows, operands 16 rows at once.
+template <typename T, int DH>
+__device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, char* lds) {
+  constexpr int NP = sizeof(T) == 4 ? 3 : 1;
+  constexpr int KT = 32, NW = kWG / 64, KS = DH / 32, NT = DH / 16, NCH = DH / 8, KPL = 64 / NCH;  // KPL: keys of a wave's load
+  constexpr int VL = KT / KPL;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, q4 = lane >> 4;
+  const int g = blockIdx.x, G = A.G, nq = it.nrows * G;
+  const spd_cache& C = A.c;
+  const int last = it.k1 - 1;
+  const int start = it.k0 & ~(kPage - 1), tiles = (it.k1 - start + KT - 1) / KT;
+  const size_t half = (size_t)C.n_kv_heads * kPage * DH;
+  const uint16_t* pool = (const uint16_t*)A.kv + (size_t)g * kPage * DH;
+  const int* table = C.page_table + (size_t)it.table * C.max_pages;
+  const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;
+  const int jj = min(col, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
+  const int lim = min(row_limit(A, it, row), it.k1);
+  bf16x8 qf[NP][KS];
+  load_query<T, KS, 32>(qf, (const T*)A.q + row * A.qs + head * DH + q4 * 8, A.scale * kLog2e);
+  int wmin = lim;
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) wmin = min(wmin, __shfl_xor(wmin, d, 64));
+  wmin = __builtin_amdgcn_readfirstlane(wmin);
+
+  // Keys outside [k0, k1) are read as the nearest one inside (see piece_wide).
+  auto pages = [&](int t) { return table[min(start / kPage + t * 2 + (lane & 1), last / kPage)]; };
+  auto in_page = [&](int key) { return (uint32_t)(min(max(key, it.k0), last) & (kPage - 1)) * DH; };
+  uint4 kr[VL], vr[VL];  // whole rows, so that a load takes whole lines
+  auto load = [&](int t, int pg) {
+    const uint16_t* p[2];
+#pragma unroll
+    for (int b = 0; b < 2; b++) p[b] = pool + (size_t)page_to_read(C, __builtin_amdgcn_readlane(pg, b)) * 2 * half;
+    const int first = start + t * KT;
+#pragma unroll
+    for (int i = 0; i < VL; i++) {
+      const uint16_t* at = p[i * KPL / 16] + in_page(first + i * KPL + lane / NCH) + lane % NCH * 8;
+      kr[i] = ldg16(at);  // read once
+      vr[i] = ldg16(at + half);
+    }
+  };
+  constexpr int KROT = DH == 128 ? 0 : 1, VROT = DH == 128 ? 0 : 1;  // as in piece_wide
+  char* kt = lds + w * 2 * KT * DH * 2;
+  char* vt = kt + KT * DH * 2;
+  uint32_t kw[VL], vw[VL], ka[KS], va[NT];
+#pragma unroll
+  for (int i = 0; i < VL; i++) {
+    const int k = i * KPL + lane / NCH;
+    kw[i] = k * DH * 2 + ((lane % NCH ^ (k >> KROT) % NCH) << 4);
+    vw[i] = k * DH * 2 + ((lane % NCH ^ (k & 7) >> VROT << 1) << 4);
   }
+#pragma unroll
+  for (int k = 0; k < KS; k++) ka[k] = col * DH * 2 + (((4 * k + q4) ^ (col >> KROT) % NCH) << 4);
+#pragma unroll
+  for (int tt = 0; tt < NT; tt++) {
+    const int k = q4 * 4 + col / 4, c = tt * 2 + (lane & 3) / 2;
+    va[tt] = k * DH * 2 + ((c ^ (k & 7) >> VROT << 1) << 4) + (lane & 1) * 8;
+  }
+  f32x4 o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; t++) o[t] = (f32x4)(0.f);
+  float m_run = -INFINITY, l_run = 0.f;
+  int pg = 0;
+  if (w < tiles) {
+    load(w, pages(w));
+    pg = pages(w + NW);
+  }
+  for (int t = w; t < tiles; t += NW) {
+    const int kb = start + t * KT;
+#pragma unroll
+    for (int i = 0; i < VL; i++) {
+      *reinterpret_cast<uint4*>(kt + kw[i]) = kr[i];
+      *reinterpret_cast<uint4*>(vt + vw[i]) = vr[i];
+    }
+    if (t + NW < tiles) {
+      load(t + NW, pg);
+      pg = pages(t + 2 * NW);
+    }
+    f32x4 s[2];
+#pragma unroll
+    for (int b = 0; b < 2; b++)
+#pragma unroll
+      for (int k = 0; k < KS; k++) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + ka[k] + b * 16 * DH * 2);
+#pragma unroll
+        for (int p = NP - 1; p >= 0; p--)
+          s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[p][k], (p == NP - 1 && k == 0) ? (f32x4)(0.f) : s[b], 0, 0, 0);
+      }
+    if (kb < it.k0 || kb + KT > wmin) {
+#pragma unroll
+      for (int b = 0; b < 2; b++)
+#pragma unroll
+        for (int v = 0; v < 4; v++) {
+          const int kk = kb + b * 16 + 4 * q4 + v;
+          s[b][v] = kk < lim && kk >= it.k0 ? s[b][v] : -INFINITY;
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int v = 1; v < 8; v++) mx = fmaxf(mx, s[v >> 2][v & 3]);
+    mx *= sc;
+    if (__any(mx > m_run + 8.0f)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float mn = fmaxf(m_run, mx);
+      const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - mn);
+      l_run *= al;
+#pragma unroll
+      for (int tt = 0; tt < NT; tt++) o[tt] *= al;
+      m_run = mn;
+    }
+    const float off = m_run == -INFINITY ? 0.f : m_run;
+    union { uint32_t u[4]; bf16x8 f; } pf[NP];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][(e & 3) + 1], sc, -off));
+      l_run += p0 + p1;
+      uint32_t pl[NP];
+      planes_of(p0, p1, pl);
+#pragma unroll
+      for (int p = 0; p < NP; p++) pf[p].u[e >> 1] = pl[p];
+    }
+#pragma unroll
+    for (int tt = 0; tt < NT; tt++) {
+      union { bf16x4 q[2]; bf16x8 f; } vf;
+#pragma unroll
+      for (int y = 0; y < 2; y++) vf.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lbf16x4*)(lbytes*)(vt + va[tt] + y * 16 * DH * 2));
+#pragma unroll
+      for (int p = NP - 1; p >= 0; p--) o[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.f, pf[p].f, o[tt], 0, 0, 0);
+    }
+  }
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+
+  // The waves' sums, in wave order.
+  __shared__ float2 s_ml[NW][16];
+  __shared__ uint32_t s_few_bad;
+  if (tid == 0) s_few_bad = 0u;
+  __syncthreads();  // every wave is done with its tile
+  float* ow = (float*)lds;  // [wave][query][dim]
+#pragma unroll
+  for (int tt = 0; tt < NT; tt++)
+    *reinterpret_cast<float4*>(ow + (w * 16 + col) * DH + tt * 16 + q4 * 4) = make_float4(o[tt][0], o[tt][1], o[tt][2], o[tt][3]);
+  if (q4 == 0) s_ml[w][col] = make_float2(m_run, l_run);
+  __syncthreads();
+  for (int i = tid; i < nq * (DH / 4); i += kWG) {
+    const int j = i / (DH / 4), d = i % (DH / 4) * 4, r = it.row0 + j / G, hd = g * G + j % G;
+    const int n = min(row_limit(A, it, r), it.k1);
+    float M = -INFINITY, L = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < NW; x++) M = fmaxf(M, s_ml[x][j].x);
+#pragma unroll
+    for (int x = 0; x < NW; x++) {
+      const float2 ml = s_ml[x][j];
+      const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+      const float4 v = *reinterpret_cast<const float4*>(ow + (x * 16 + j) * DH + d);
+      L = fmaf(ml.y, f, L);
+      a[0] = fmaf(v.x, f, a[0]);
+      a[1] = fmaf(v.y, f, a[1]);
+      a[2] = fmaf(v.z, f, a[2]);
+      a[3] = fmaf(v.w, f, a[3]);
+    }
+    if ((!(L > 0.f) && n > it.k0) || a[0] != a[0] || a[1] != a[1] || a[2] != a[2] || a[3] != a[3]) {
+      atomicOr(&s_few_bad, 1u << j);
+    } else if (it.rec < 0) {
+      store4((T*)A.out + r * A.os + hd * DH + d, a, n > 0 ? 1.0f / L : 0.f);
+    } else {
+      const size_t at = (size_t)it.rec + (size_t)g * nq + j;
+      store4(R.o + at * DH + d, a, 1.0f);
+      if (d == 0) R.ml[at] = make_float2(M, L);
+    }
+  }
+  __syncthreads();
+  for (uint32_t m = __builtin_amdgcn_readfirstlane(s_few_bad); m != 0u; m &= m - 1u)
+    plain_piece<T, uint16_t, DH>(A, it, R, __builtin_ctz(m), (float*)lds);
 }
 
 // The same over an fp32 cache, for 32 queries a wave, with v_mfma_f32_32x32x2_f32 (lane l supplies k = l / 32 of A row
@@ -926,12 +940,7 @@ __device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, cha
   const bool active = w * 32 < nq;
   const int j = w * 32 + col, jj = min(j, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
   const bool mine = j < nq;
-  int lim = it.lim0 + jj / G;
-  if (it.mode & ITEM_FLAT) {
-    const int s = A.seqs[row];
-    lim = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
-  }
-  lim = min(lim, it.k1);
+  const int lim = min(row_limit(A, it, row), it.k1);
   float4 qf[KS];
   {
     const float* q = (const float*)A.q + row * A.qs + head * DH + h * 4;
@@ -1049,27 +1058,20 @@ __device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, cha
   }
   __syncthreads();
   for (int i = 0; i < 4; i++)
-    for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u) {
-      const int jb = i * 32 + __builtin_ctz(m), r = it.row0 + jb / G;
-      int n = it.lim0 + jb / G;
-      if (it.mode & ITEM_FLAT) {
-        const int s = A.seqs[r];
-        n = (unsigned)s < (unsigned)C.max_seqs ? seq_len(C, s) : 0;
-      }
-      plain_piece<float, float, DH, kWG>(A, it, R, r, g * G + jb % G, jb, nq, min(n, it.k1), (float*)lds);
-    }
+    for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u)
+      plain_piece<float, float, DH>(A, it, R, i * 32 + __builtin_ctz(m), (float*)lds);
 }
 
 // Grid: x = KV head (with 8 of them a head's keys stay in one XCD's L2), y = piece.
 template <typename T, int DH>
-__global__ __launch_bounds__(kAttWG, 2) void k_attend_bf16(SeqArgs A, const int* count, const Item* items, Records R) {
+__global__ __launch_bounds__(kWG, 2) void k_attend_bf16(SeqArgs A, const int* count, const Item* items, Records R) {
   extern __shared__ __align__(16) char lds[];
   if ((int)blockIdx.y >= count[0]) return;
   const Item it = items[blockIdx.y];
-  if (it.mode & ITEM_NARROW)
-    piece_bf16<T, DH, true>(A, it, R, lds);
+  if (it.mode & ITEM_FEW)
+    piece_few<T, DH>(A, it, R, lds);
   else
-    piece_bf16<T, DH, false>(A, it, R, lds);
+    piece_wide<T, DH>(A, it, R, lds);
 }
 
 template <int DH>
@@ -1151,7 +1153,7 @@ struct Request {
 Request request(const spd_cache& c, int n_q_heads, int nseqs, int rows, int ngroups, int max_len, bool prefix) {
   Request q{};
   const int hkv = c.n_kv_heads, G = n_q_heads / hkv;
-  q.rpt = (c.dtype == SPD_BF16 ? 256 : 128) / G;
+  q.rpt = 128 / G;
   q.qpu = c.head_dim == 128 ? merge_queries<128>() : merge_queries<64>();
   // a job of at most kMinChunk keys is not split: then prompts have nothing to join
   const bool split = max_len == 0 || max_len > kMinChunk;
@@ -1185,7 +1187,7 @@ template <typename T, int DH>
 void launch(const SeqArgs& a, const Request& q, const PlanArgs& p, const Records& r, hipStream_t s) {
   const dim3 grid(a.c.n_kv_heads, (unsigned)q.items);
   if (a.c.dtype == SPD_BF16) {
-    hipLaunchKernelGGL((k_attend_bf16<T, DH>), grid, dim3(kAttWG), 2 * 2 * 128 * DH * 2, s, a, p.count, p.items, r);
+    hipLaunchKernelGGL((k_attend_bf16<T, DH>), grid, dim3(kWG), 2 * 2 * 64 * DH * 2, s, a, p.count, p.items, r);
   } else {
     hipLaunchKernelGGL((k_attend_f32<DH>), grid, dim3(kWG), 2 * 2 * 32 * DH * 4, s, a, p.count, p.items, r);
   }
