@@ -153,7 +153,7 @@ struct Merge {
 constexpr int kPlanWG = 1024;
 constexpr int kMinChunk = 256;
 constexpr int kWantedWGs = 512;
-constexpr int kBuckets = 256;
+constexpr int kBuckets = 64;  // a wave's lanes
 
 // The sums of some queries: `query` of merge `merge` and those behind it, as many as a workgroup of the merge takes.
 struct Unit {
@@ -183,37 +183,46 @@ struct Job {
 constexpr int kPlanSeqs = 4096;
 struct Batch {
   const int *cu, *seqs, *lens, *prefix;  // LDS: cu_rows or cu_groups, sequences, their lengths by row of the batch, prefix_lens
+  const int* base;                       // LDS: the number of a sequence's or group's first tile
   const PlanArgs* P;
   bool in_lds;
   __device__ __forceinline__ int cu_at(int i) const { return in_lds ? cu[i] : P->cu[i]; }
   __device__ __forceinline__ int seq_at(int i) const { return in_lds ? seqs[i] : P->seqs[i]; }
   __device__ __forceinline__ int prefix_at(int i) const { return in_lds ? prefix[i] : P->prefix[i]; }
+  // The tiles of entry i have the numbers cu[i] / rpt + i and up: enough of them, in order, without a sum over those before.
+  __device__ __forceinline__ int base_at(int i) const { return in_lds ? base[i] : P->cu[i] / P->rpt + i; }
   __device__ __forceinline__ int len_at(int i) const {  // -1: no such sequence
     if (in_lds) return lens[i];
     const int s = P->seqs[i];
     return (unsigned)s < (unsigned)P->c.max_seqs ? seq_len(P->c, s) : -1;
   }
-  // last i in [0, n) with cu[i] / d + i * step <= t (step 0 or 1; cu[0] = 0)
-  __device__ int last_at(int n, int t, int d, int step) const {
+  // last i in [0, n) with at(i) <= t, for at that ascends from at(0) <= t
+  template <typename F>
+  static __device__ __forceinline__ int last(int n, int t, F at) {
     int lo = 0, hi = n - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (cu_at(mid) / d + mid * step <= t)
+      if (at(mid) <= t)
         lo = mid;
       else
         hi = mid - 1;
     }
     return lo;
   }
+  __device__ __forceinline__ int of_tile(int n, int t) const {
+    return last(n, t, [&](int i) { return base_at(i); });
+  }
+  __device__ __forceinline__ int of_row(int n, int r) const {
+    return last(n, r, [&](int i) { return cu_at(i); });
+  }
 };
 
-// Job t of a prompt call. The tiles of sequence i have the numbers cu[i] / rpt + i and up: enough of them, in order,
-// without a sum over the sequences before.
+// Job t of a prompt call: a tile of a sequence's rows.
 __device__ bool prompt_job(const PlanArgs& P, const Batch& B, int t, Job& j) {
-  const int i = B.last_at(P.nseqs, t, P.rpt, 1);
+  const int i = B.of_tile(P.nseqs, t);
   const int begin = B.cu_at(i), stop = B.cu_at(i + 1), end = min(stop, P.rows), len = B.len_at(i);
   if (begin < 0 || begin >= end || len < 0) return false;
-  const long long row0 = begin + (long long)(t - begin / P.rpt - i) * P.rpt;
+  const long long row0 = begin + (long long)(t - B.base_at(i)) * P.rpt;
   if (row0 < begin || row0 >= end) return false;
   j.row0 = (int)row0;
   j.nrows = min(P.rpt, end - j.row0);
@@ -241,9 +250,9 @@ __device__ bool prefix_job(const PlanArgs& P, const Batch& B, int t, Job& j, boo
   j.lim0 = 0;
   j.a = 0;
   if (t < P.tiles) {
-    const int g = B.last_at(P.ngroups, t, P.rpt, 1), n = shared_prefix(P, B, g, first, rows);
+    const int g = B.of_tile(P.ngroups, t), n = shared_prefix(P, B, g, first, rows);
     if (n == 0) return false;
-    const long long at = (long long)(t - first / P.rpt - g) * P.rpt;
+    const long long at = (long long)(t - B.base_at(g)) * P.rpt;
     if (at < 0 || at >= rows) return false;
     j.row0 = first + (int)at;
     j.nrows = min(P.rpt, rows - (int)at);
@@ -261,38 +270,42 @@ __device__ bool prefix_job(const PlanArgs& P, const Batch& B, int t, Job& j, boo
   j.b = len;
   j.mode = ITEM_FLAT | ITEM_FEW;
   if (P.ngroups > 0) {
-    const int g = B.last_at(P.ngroups, r, 1, 0), n = shared_prefix(P, B, g, first, rows);
+    const int g = B.of_row(P.ngroups, r), n = shared_prefix(P, B, g, first, rows);
     if (n > 0 && r >= first && r < first + rows) {
       shared = true;
       j.a = min(n, len);
-      tile = first / P.rpt + g + (r - first) / P.rpt;
-      query = (r - first) % P.rpt * P.G;
+      const int in_group = (r - first) / P.rpt;
+      tile = B.base_at(g) + in_group;
+      query = (r - first - in_group * P.rpt) * P.G;
     }
   }
   return true;
 }
 
-// A prompt's merge is known with its job. A decode row's takes its own job's records and those of its tile, which the
-// tile's thread leaves in tile_rec.
+// Tiles whose records are kept in LDS for the rows that join them.
+constexpr int kPlanTiles = 1024;
+
 template <bool PREFIX>
 __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
-  __shared__ int s_cu[kPlanSeqs + 1], s_seqs[kPlanSeqs], s_lens[kPlanSeqs], s_prefix[PREFIX ? kPlanSeqs : 1];
+  __shared__ int s_cu[kPlanSeqs + 1], s_seqs[kPlanSeqs], s_lens[kPlanSeqs], s_base[kPlanSeqs], s_prefix[PREFIX ? kPlanSeqs : 1];
+  __shared__ int4 s_tile[PREFIX ? kPlanTiles : 1];
   __shared__ unsigned long long s_total, s_rec;
-  __shared__ int s_max, s_count[kBuckets], s_merges, s_units;
+  __shared__ int s_max, s_count[kBuckets], s_items, s_merges, s_units;
   const int tid = threadIdx.x;
-  const Batch B{s_cu, s_seqs, s_lens, s_prefix, &P, P.nseqs <= kPlanSeqs};
+  const Batch B{s_cu, s_seqs, s_lens, s_prefix, s_base, &P, P.nseqs <= kPlanSeqs};
   if (B.in_lds) {
+    const int n = PREFIX ? P.ngroups : P.nseqs;
     for (int i = tid; i < P.nseqs; i += kPlanWG) {
-      const int s = P.seqs[i];
+      const int s = P.seqs[i], c = i < n ? P.cu[i] : 0, x = PREFIX && i < n ? P.prefix[i] : 0;
       s_seqs[i] = s;
       s_lens[i] = (unsigned)s < (unsigned)P.c.max_seqs ? seq_len(P.c, s) : -1;
-    }
-    const int n = PREFIX ? P.ngroups : P.nseqs;
-    if (n > 0)
-      for (int i = tid; i <= n; i += kPlanWG) {
-        s_cu[i] = P.cu[i];
-        if (PREFIX && i < n) s_prefix[i] = P.prefix[i];
+      if (i < n) {
+        s_cu[i] = c;
+        s_base[i] = c / P.rpt + i;
+        if (PREFIX) s_prefix[i] = x;
       }
+    }
+    if (tid == 0 && n > 0) s_cu[n] = P.cu[n];
   }
   if (tid < kBuckets) s_count[tid] = 0;
   if (tid == 0) {
@@ -301,22 +314,38 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
     s_merges = s_units = 0;
   }
   __syncthreads();
-  auto job = [&](int t, Job& j, bool& shared, int& tile, int& query) {
-    if constexpr (PREFIX) return prefix_job(P, B, t, j, shared, tile, query);
-    shared = false;
-    return prompt_job(P, B, t, j);
+  // A thread's jobs are tid, tid + kPlanWG, ..: the first is kept.
+  struct Known {
+    Job j;
+    bool is, shared;
+    int tile, query;
   };
-  Job j;
-  bool sh;
-  int tile, query;
+  auto work_out = [&](int t, Known& k) {
+    if constexpr (PREFIX) {
+      k.is = prefix_job(P, B, t, k.j, k.shared, k.tile, k.query);
+    } else {
+      k.shared = false;
+      k.is = prompt_job(P, B, t, k.j);
+    }
+  };
+  Known mine;
+  mine.is = false;
+  if (tid < P.jobs) work_out(tid, mine);
+  auto each = [&](auto f) {
+    if (mine.is) f(tid, mine);
+    for (int t = tid + kPlanWG; t < P.jobs; t += kPlanWG) {
+      Known k;
+      work_out(t, k);
+      if (k.is) f(t, k);
+    }
+  };
   {
     unsigned long long sum = 0ull;
     int longest = 1;
-    for (int t = tid; t < P.jobs; t += kPlanWG) {
-      if (!job(t, j, sh, tile, query)) continue;
-      sum += (unsigned)(j.b - j.a);
-      longest = max(longest, j.b - j.a);
-    }
+    each([&](int, const Known& k) {
+      sum += (unsigned)(k.j.b - k.j.a);
+      longest = max(longest, k.j.b - k.j.a);
+    });
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       sum += __shfl_xor(sum, d, 64);
@@ -328,90 +357,103 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
     }
   }
   __syncthreads();
-  const unsigned long long want = P.wanted > 0 ? (s_total + P.wanted - 1) / P.wanted : ~0ull;
-  const int chunk = want >= (unsigned)s_max ? (s_max + 63) / 64 * 64 : max(kMinChunk, (int)((want + 63) / 64 * 64));
+  // Split where a job is longer than a CU's share, two workgroups being on one.
+  const bool split = P.wanted > 0 && (unsigned long long)s_max * (unsigned)max(P.wanted / 2, 1) > s_total;
+  const int chunk = split ? max(kMinChunk, (int)((s_total / P.wanted + 64) / 64 * 64)) : (s_max + 63) / 64 * 64;
   const float per_key = (float)(kBuckets - 1) / (2.0f * (float)min(s_max, chunk));
-  auto bucket = [&](int n, int mode) {  // the longest first; a key of a wide piece costs about twice a narrow one's
+  auto bucket = [&](int n, int mode) {  // the longest first; a key of a wide piece costs about twice another's
     return kBuckets - 1 - min((int)((float)n * (mode & ITEM_FEW ? 1.0f : 2.0f) * per_key), kBuckets - 1);
   };
   // a job's pieces; 0: nothing to do (a row that ends with its prefix)
-  auto pieces_of = [&](const Job& j, bool sh) { return j.b > j.a ? (j.b - j.a + chunk - 1) / chunk : sh ? 0 : 1; };
-  for (int t = tid; t < P.jobs; t += kPlanWG) {
-    if (!job(t, j, sh, tile, query)) continue;
-    const int n = pieces_of(j, sh);
-    for (int p = 0; p < n; p++) atomicAdd(&s_count[bucket(min(chunk, j.b - j.a - p * chunk), j.mode)], 1);
-  }
+  auto pieces_of = [&](const Known& k) { return k.j.b > k.j.a ? (k.j.b - k.j.a + chunk - 1) / chunk : k.shared ? 0 : 1; };
+  each([&](int, const Known& k) {
+    const int n = pieces_of(k);  // all but the last are whole
+    if (n > 1) atomicAdd(&s_count[bucket(chunk, k.j.mode)], n - 1);
+    if (n > 0) atomicAdd(&s_count[bucket(k.j.b - k.j.a - (n - 1) * chunk, k.j.mode)], 1);
+  });
+  if (PREFIX)
+    for (int t = tid; t < P.tiles; t += kPlanWG) {
+      if (t < kPlanTiles)
+        s_tile[t] = make_int4(0, 0, 0, 0);
+      else
+        P.tile_rec[t] = make_int4(0, 0, 0, 0);
+    }
   __syncthreads();
-  if (tid < 64) {  // bucket counts to their first places
-    int before = 0;
-    for (int b0 = 0; b0 < kBuckets; b0 += 64) {
-      const int v = s_count[b0 + tid];
-      int x = v;
+  if (tid < kBuckets) {  // bucket counts to their first places
+    const int v = s_count[tid];
+    int x = v;
 #pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(x, d, 64);
-        if (tid >= d) x += y;
-      }
-      s_count[b0 + tid] = before + x - v;
-      before += __shfl(x, 63, 64);
+    for (int d = 1; d < 64; d <<= 1) {
+      const int y = __shfl_up(x, d, 64);
+      if (tid >= d) x += y;
     }
-    if (tid == 0) P.count[0] = before;
+    s_count[tid] = x - v;
+    if (tid == kBuckets - 1) P.count[0] = s_items = x;
   }
   __syncthreads();
-  for (int t = tid; t < P.jobs; t += kPlanWG) {
-    if (!job(t, j, sh, tile, query)) {
-      if (PREFIX && t < P.tiles) P.tile_rec[t] = make_int4(0, 0, 0, 0);
-      continue;
-    }
-    int n = pieces_of(j, sh), rec = -1;
-    const int nq = j.nrows * P.G;
-    if (n > 1 || sh) {
-      const long long need = (long long)n * P.c.n_kv_heads * nq;
-      const unsigned long long at = atomicAdd(&s_rec, (unsigned long long)need);
-      rec = (int)at;
-      if (at + need > P.records) n = 0;  // only where cu_groups does not ascend
-      if (PREFIX && t < P.tiles) {
-        P.tile_rec[t] = make_int4(rec, n, nq, 0);
-      } else {
-        Merge m;
-        m.row0 = j.row0;
-        m.nrows = j.nrows;
-        m.rec[0] = m.pieces[0] = m.queries[0] = m.first[0] = 0;
-        m.rec[1] = rec;
-        m.pieces[1] = n;
-        m.queries[1] = nq;
-        m.first[1] = 0;
-        m.lim0 = j.lim0;
-        m.mode = j.mode;
-        if (PREFIX && sh) {
-          m.pieces[0] = -1;
-          m.queries[0] = tile;  // replaced below
-          m.first[0] = query;
-        }
-        const int at_merge = atomicAdd(&s_merges, 1);
-        P.merges[at_merge] = m;
-        const int units = (nq + P.qpu - 1) / P.qpu, at_unit = atomicAdd(&s_units, units);
-        for (int u = 0; u < units; u++) P.units[at_unit + u] = Unit{at_merge, u * P.qpu};
-      }
-    }
+  // Where all pieces are on the GPU at once, the second half comes in ascending order: a CU has a long one and a short one.
+  const int all = s_items, half = max(P.wanted / 2, 1);
+  auto place = [&](int at) { return at < half || all > 2 * half ? at : all - 1 - (at - half); };
+  auto room = [&](int n, int nq, int& rec) {  // for the records of a job; false: only where cu_groups does not ascend
+    const long long need = (long long)n * P.c.n_kv_heads * nq;
+    const unsigned long long at = atomicAdd(&s_rec, (unsigned long long)need);
+    rec = (int)at;
+    return at + need <= P.records;
+  };
+  auto put_items = [&](const Known& k, int n, int rec) {
+    if (n == 0) return;
+    const int nq = k.j.nrows * P.G, whole = n > 1 ? atomicAdd(&s_count[bucket(chunk, k.j.mode)], n - 1) : 0;
+    const int rest = atomicAdd(&s_count[bucket(k.j.b - k.j.a - (n - 1) * chunk, k.j.mode)], 1);
     for (int p = 0; p < n; p++) {
-      const int a = j.a + p * chunk, b = min(j.b, a + chunk);
-      const int at = atomicAdd(&s_count[bucket(b - a, j.mode)], 1);
-      P.items[at] = Item{j.row0, j.nrows, j.table, a, max(a, b), rec < 0 ? -1 : rec + p * P.c.n_kv_heads * nq, j.lim0, j.mode};
+      const int a = k.j.a + p * chunk;
+      P.items[place(p < n - 1 ? whole + p : rest)] = Item{k.j.row0, k.j.nrows, k.j.table, a, max(a, min(k.j.b, a + chunk)),
+                                                          rec < 0 ? -1 : rec + p * P.c.n_kv_heads * nq, k.j.lim0, k.j.mode};
     }
+  };
+  if (PREFIX) {  // the tiles' records first: rows join them
+    each([&](int t, const Known& k) {
+      if (t >= P.tiles) return;
+      int n = pieces_of(k), rec;
+      const int nq = k.j.nrows * P.G;
+      if (!room(n, nq, rec)) n = 0;
+      const int4 r = make_int4(rec, n, nq, 0);
+      if (t < kPlanTiles)
+        s_tile[t] = r;
+      else
+        P.tile_rec[t] = r;
+      put_items(k, n, rec);
+    });
+    __syncthreads();
   }
+  each([&](int t, const Known& k) {
+    if (PREFIX && t < P.tiles) return;
+    int n = pieces_of(k), rec = -1;
+    const int nq = k.j.nrows * P.G;
+    if (n > 1 || k.shared) {
+      if (!room(n, nq, rec)) n = 0;
+      int4 r = make_int4(0, 0, 0, 0);
+      if (PREFIX && k.shared) r = k.tile < kPlanTiles ? s_tile[k.tile] : P.tile_rec[k.tile];
+      Merge m;
+      m.row0 = k.j.row0;
+      m.nrows = k.j.nrows;
+      m.rec[0] = r.x;
+      m.pieces[0] = k.shared && k.query + nq <= r.z ? r.y : 0;
+      m.queries[0] = r.z;
+      m.first[0] = k.shared ? k.query : 0;
+      m.rec[1] = rec;
+      m.pieces[1] = n;
+      m.queries[1] = nq;
+      m.first[1] = 0;
+      m.lim0 = k.j.lim0;
+      m.mode = k.j.mode;
+      const int at_merge = atomicAdd(&s_merges, 1);
+      P.merges[at_merge] = m;
+      const int units = (nq + P.qpu - 1) / P.qpu, at_unit = atomicAdd(&s_units, units);
+      for (int u = 0; u < units; u++) P.units[at_unit + u] = Unit{at_merge, u * P.qpu};
+    }
+    put_items(k, n, rec);
+  });
   __syncthreads();
-  if (PREFIX) {
-    for (int i = tid; i < s_merges; i += kPlanWG) {
-      Merge& m = P.merges[i];
-      if (m.pieces[0] < 0) {
-        const int4 r = P.tile_rec[m.queries[0]];
-        m.rec[0] = r.x;
-        m.pieces[0] = m.first[0] + m.nrows * P.G <= r.z ? r.y : 0;
-        m.queries[0] = r.z;
-      }
-    }
-  }
   if (tid == 0) P.count[1] = s_units;
 }
 
