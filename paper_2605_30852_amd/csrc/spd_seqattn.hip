@@ -289,8 +289,8 @@ template <bool PREFIX>
 __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
   __shared__ int s_cu[kPlanSeqs + 1], s_seqs[kPlanSeqs], s_lens[kPlanSeqs], s_base[kPlanSeqs], s_prefix[PREFIX ? kPlanSeqs : 1];
   __shared__ int4 s_tile[PREFIX ? kPlanTiles : 1];
-  __shared__ unsigned long long s_total, s_rec;
-  __shared__ int s_max, s_count[kBuckets], s_items, s_merges, s_units;
+  __shared__ unsigned long long s_total, s_sums[kPlanWG / 64];
+  __shared__ int s_max, s_count[kBuckets], s_items;
   const int tid = threadIdx.x;
   const Batch B{s_cu, s_seqs, s_lens, s_prefix, s_base, &P, P.nseqs <= kPlanSeqs};
   if (B.in_lds) {
@@ -309,9 +309,8 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
   }
   if (tid < kBuckets) s_count[tid] = 0;
   if (tid == 0) {
-    s_total = s_rec = 0ull;
+    s_total = 0ull;
     s_max = 1;
-    s_merges = s_units = 0;
   }
   __syncthreads();
   // A thread's jobs are tid, tid + kPlanWG, ..: the first is kept.
@@ -371,13 +370,6 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
     if (n > 1) atomicAdd(&s_count[bucket(chunk, k.j.mode)], n - 1);
     if (n > 0) atomicAdd(&s_count[bucket(k.j.b - k.j.a - (n - 1) * chunk, k.j.mode)], 1);
   });
-  if (PREFIX)
-    for (int t = tid; t < P.tiles; t += kPlanWG) {
-      if (t < kPlanTiles)
-        s_tile[t] = make_int4(0, 0, 0, 0);
-      else
-        P.tile_rec[t] = make_int4(0, 0, 0, 0);
-    }
   __syncthreads();
   if (tid < kBuckets) {  // bucket counts to their first places
     const int v = s_count[tid];
@@ -394,43 +386,47 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
   // Where all pieces are on the GPU at once, the second half comes in ascending order: a CU has a long one and a short one.
   const int all = s_items, half = max(P.wanted / 2, 1);
   auto place = [&](int at) { return at < half || all > 2 * half ? at : all - 1 - (at - half); };
-  auto room = [&](int n, int nq, int& rec) {  // for the records of a job; false: only where cu_groups does not ascend
-    const long long need = (long long)n * P.c.n_kv_heads * nq;
-    const unsigned long long at = atomicAdd(&s_rec, (unsigned long long)need);
-    rec = (int)at;
-    return at + need <= P.records;
-  };
-  auto put_items = [&](const Known& k, int n, int rec) {
-    if (n == 0) return;
-    const int nq = k.j.nrows * P.G, whole = n > 1 ? atomicAdd(&s_count[bucket(chunk, k.j.mode)], n - 1) : 0;
-    const int rest = atomicAdd(&s_count[bucket(k.j.b - k.j.a - (n - 1) * chunk, k.j.mode)], 1);
-    for (int p = 0; p < n; p++) {
-      const int a = k.j.a + p * chunk;
-      P.items[place(p < n - 1 ? whole + p : rest)] = Item{k.j.row0, k.j.nrows, k.j.table, a, max(a, min(k.j.b, a + chunk)),
-                                                          rec < 0 ? -1 : rec + p * P.c.n_kv_heads * nq, k.j.lim0, k.j.mode};
+  // Places of records, merges and units come from a prefix sum over the jobs (64 lanes that add to one LDS word take about a
+  // microsecond), packed: records of a KV head above, then merges and units, which stay below 2^16.
+  unsigned long long before = 0ull;
+  for (int t0 = 0; t0 < P.jobs; t0 += kPlanWG) {
+    const int t = t0 + tid;
+    Known k = mine;
+    if (t0 > 0) {
+      k.is = false;
+      if (t < P.jobs) work_out(t, k);
     }
-  };
-  if (PREFIX) {  // the tiles' records first: rows join them
-    each([&](int t, const Known& k) {
-      if (t >= P.tiles) return;
-      int n = pieces_of(k), rec;
-      const int nq = k.j.nrows * P.G;
-      if (!room(n, nq, rec)) n = 0;
-      const int4 r = make_int4(rec, n, nq, 0);
+    const bool tile = PREFIX && t < P.tiles;
+    int n = k.is ? pieces_of(k) : 0;
+    const int nq = k.is ? k.j.nrows * P.G : 0, units = (nq + P.qpu - 1) / P.qpu;
+    const bool joins = k.is && (n > 1 || k.shared);
+    const unsigned long long v = joins ? (unsigned long long)(unsigned)(n * nq) << 32 | (tile ? 0 : 1u << 16 | units) : 0ull;
+    unsigned long long x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const unsigned long long y = __shfl_up(x, d, 64);
+      if ((tid & 63) >= d) x += y;
+    }
+    if ((tid & 63) == 63) s_sums[tid >> 6] = x;
+    __syncthreads();
+    unsigned long long at = before + x - v;
+#pragma unroll
+    for (int i = 0; i < kPlanWG / 64; i++) {
+      if (i < tid >> 6) at += s_sums[i];
+      before += s_sums[i];
+    }
+    const long long first = (long long)(at >> 32) * P.c.n_kv_heads;
+    if (joins && first + (long long)n * nq * P.c.n_kv_heads > (long long)P.records) n = 0;  // only where cu_groups does not ascend
+    const int rec = joins ? (int)first : -1;
+    if (tile) {
+      const int4 r = joins ? make_int4(rec, n, nq, 0) : make_int4(0, 0, 0, 0);
       if (t < kPlanTiles)
         s_tile[t] = r;
       else
         P.tile_rec[t] = r;
-      put_items(k, n, rec);
-    });
-    __syncthreads();
-  }
-  each([&](int t, const Known& k) {
-    if (PREFIX && t < P.tiles) return;
-    int n = pieces_of(k), rec = -1;
-    const int nq = k.j.nrows * P.G;
-    if (n > 1 || k.shared) {
-      if (!room(n, nq, rec)) n = 0;
+    }
+    __syncthreads();  // tiles come before the rows that join them; the sums are read
+    if (joins && !tile) {
       int4 r = make_int4(0, 0, 0, 0);
       if (PREFIX && k.shared) r = k.tile < kPlanTiles ? s_tile[k.tile] : P.tile_rec[k.tile];
       Merge m;
@@ -446,15 +442,21 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
       m.first[1] = 0;
       m.lim0 = k.j.lim0;
       m.mode = k.j.mode;
-      const int at_merge = atomicAdd(&s_merges, 1);
+      const int at_merge = (int)(at >> 16 & 0xffff), at_unit = (int)(at & 0xffff);
       P.merges[at_merge] = m;
-      const int units = (nq + P.qpu - 1) / P.qpu, at_unit = atomicAdd(&s_units, units);
       for (int u = 0; u < units; u++) P.units[at_unit + u] = Unit{at_merge, u * P.qpu};
     }
-    put_items(k, n, rec);
-  });
-  __syncthreads();
-  if (tid == 0) P.count[1] = s_units;
+    if (n > 0) {
+      const int whole = n > 1 ? atomicAdd(&s_count[bucket(chunk, k.j.mode)], n - 1) : 0;
+      const int rest = atomicAdd(&s_count[bucket(k.j.b - k.j.a - (n - 1) * chunk, k.j.mode)], 1);
+      for (int p = 0; p < n; p++) {
+        const int a = k.j.a + p * chunk;
+        P.items[place(p < n - 1 ? whole + p : rest)] = Item{k.j.row0, k.j.nrows, k.j.table, a, max(a, min(k.j.b, a + chunk)),
+                                                            rec < 0 ? -1 : rec + p * P.c.n_kv_heads * nq, k.j.lim0, k.j.mode};
+      }
+    }
+  }
+  if (tid == 0) P.count[1] = (int)(before & 0xffff);
 }
 
 // Records: o, then (m, l) with m in units of log2.
