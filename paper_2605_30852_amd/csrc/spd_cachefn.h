@@ -49,6 +49,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(fp32x2{a, b}, bf16x2));
 }
 
+// 16-byte store past the caches.
+__device__ __forceinline__ void stg16(void* p, const uint4& u) {
+  const v4u v = {u.x, u.y, u.z, u.w};
+  __builtin_nontemporal_store(v, (__attribute__((address_space(1))) v4u*)(p));
+}
+
 // Eight elements (16-byte aligned) as floats, and back.
 __device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
   const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
