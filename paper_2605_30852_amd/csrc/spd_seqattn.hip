@@ -166,6 +166,7 @@ struct PlanArgs {
   int nseqs, rows, ngroups, G, wanted;  // wanted: pieces of a KV head; 0: no job is split
   int rpt;                              // rows of a tile
   int tiles, jobs;
+  int wide_cost;                        // of a key of a wide piece; 1: of one of few queries
   int qpu;                              // queries of a merge's workgroup
   unsigned long long records;           // room for them
   int* count;                           // items, units
@@ -289,8 +290,8 @@ template <bool PREFIX>
 __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
   __shared__ int s_cu[kPlanSeqs + 1], s_seqs[kPlanSeqs], s_lens[kPlanSeqs], s_base[kPlanSeqs], s_prefix[PREFIX ? kPlanSeqs : 1];
   __shared__ int4 s_tile[PREFIX ? kPlanTiles : 1];
-  __shared__ unsigned long long s_total, s_sums[kPlanWG / 64];
-  __shared__ int s_max, s_count[kBuckets], s_items;
+  __shared__ unsigned long long s_total, s_max, s_sums[kPlanWG / 64];
+  __shared__ int s_count[kBuckets], s_items;
   const int tid = threadIdx.x;
   const Batch B{s_cu, s_seqs, s_lens, s_prefix, s_base, &P, P.nseqs <= kPlanSeqs};
   if (B.in_lds) {
@@ -310,7 +311,7 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
   if (tid < kBuckets) s_count[tid] = 0;
   if (tid == 0) {
     s_total = 0ull;
-    s_max = 1;
+    s_max = 1ull;
   }
   __syncthreads();
   // A thread's jobs are tid, tid + kPlanWG, ..: the first is kept.
@@ -338,12 +339,13 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
       if (k.is) f(t, k);
     }
   };
+  auto cost = [&](int keys, int mode) { return (unsigned long long)keys * (mode & ITEM_FEW ? 1 : P.wide_cost); };
   {
-    unsigned long long sum = 0ull;
-    int longest = 1;
+    unsigned long long sum = 0ull, longest = 1ull;
     each([&](int, const Known& k) {
-      sum += (unsigned)(k.j.b - k.j.a);
-      longest = max(longest, k.j.b - k.j.a);
+      const unsigned long long c = cost(k.j.b - k.j.a, k.j.mode);
+      sum += c;
+      longest = max(longest, c);
     });
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -357,16 +359,22 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
   }
   __syncthreads();
   // Split where a job is longer than a CU's share, two workgroups being on one.
-  const bool split = P.wanted > 0 && (unsigned long long)s_max * (unsigned)max(P.wanted / 2, 1) > s_total;
-  const int chunk = split ? max(kMinChunk, (int)((s_total / P.wanted + 64) / 64 * 64)) : (s_max + 63) / 64 * 64;
-  const float per_key = (float)(kBuckets - 1) / (2.0f * (float)min(s_max, chunk));
-  auto bucket = [&](int n, int mode) {  // the longest first; a key of a wide piece costs about twice another's
-    return kBuckets - 1 - min((int)((float)n * (mode & ITEM_FEW ? 1.0f : 2.0f) * per_key), kBuckets - 1);
+  const bool split = P.wanted > 0 && s_max * (unsigned)max(P.wanted / 2, 1) > s_total;
+  const unsigned long long share = split ? min((s_total + P.wanted - 1) / P.wanted, s_max) : s_max;
+  const int chunk_few = max(kMinChunk, (int)((min(share, 1ull << 30) + 63) / 64 * 64));
+  const int chunk_wide = max(kMinChunk / 2, (int)((min(share / P.wide_cost, 1ull << 30) + 64) / 64 * 64));
+  auto chunk_of = [&](const Known& k) { return k.j.mode & ITEM_FEW ? chunk_few : chunk_wide; };
+  const float per_cost = (float)(kBuckets - 1) / (float)max(cost(chunk_few, ITEM_FEW), cost(chunk_wide, 0));
+  auto bucket = [&](int keys, int mode) {  // the costliest first
+    return kBuckets - 1 - min((int)((float)cost(keys, mode) * per_cost), kBuckets - 1);
   };
   // a job's pieces; 0: nothing to do (a row that ends with its prefix)
-  auto pieces_of = [&](const Known& k) { return k.j.b > k.j.a ? (k.j.b - k.j.a + chunk - 1) / chunk : k.shared ? 0 : 1; };
+  auto pieces_of = [&](const Known& k) {
+    const int chunk = chunk_of(k);
+    return k.j.b > k.j.a ? (k.j.b - k.j.a + chunk - 1) / chunk : k.shared ? 0 : 1;
+  };
   each([&](int, const Known& k) {
-    const int n = pieces_of(k);  // all but the last are whole
+    const int n = pieces_of(k), chunk = chunk_of(k);  // all but the last are whole
     if (n > 1) atomicAdd(&s_count[bucket(chunk, k.j.mode)], n - 1);
     if (n > 0) atomicAdd(&s_count[bucket(k.j.b - k.j.a - (n - 1) * chunk, k.j.mode)], 1);
   });
@@ -447,6 +455,7 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
       for (int u = 0; u < units; u++) P.units[at_unit + u] = Unit{at_merge, u * P.qpu};
     }
     if (n > 0) {
+      const int chunk = chunk_of(k);
       const int whole = n > 1 ? atomicAdd(&s_count[bucket(chunk, k.j.mode)], n - 1) : 0;
       const int rest = atomicAdd(&s_count[bucket(k.j.b - k.j.a - (n - 1) * chunk, k.j.mode)], 1);
       for (int p = 0; p < n; p++) {
@@ -582,6 +591,11 @@ __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, ch
   const size_t half = (size_t)C.n_kv_heads * kPage * DH;
   const uint16_t* pool = (const uint16_t*)A.kv + (size_t)g * kPage * DH;
   const int* table = C.page_table + (size_t)it.table * C.max_pages;
+  // The pages of a tile, one a lane (mod their number), are read a tile ahead of their use, and looked at only there: a look
+  // at them here would wait for them and for the keys requested before them.
+  auto pages = [&](int t) { return table[min(start / kPage + t * (KT / kPage) + (lane & (KT / kPage - 1)), last / kPage)]; };
+  const int pg0 = tiles > 0 ? pages(0) : 0;
+  int pg = tiles > 0 ? pages(1) : 0;
   const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;  // from scores to exponents
   const bool active = w * 32 < nq;
   const int jq = w * 32 + col, jj = min(jq, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
@@ -591,18 +605,18 @@ __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, ch
   bf16x8 qf[NP][KS];
   load_query<T, KS, 16>(qf, (const T*)A.q + row * A.qs + head * DH + h * 8, A.scale * kLog2e);
   // keys below wmin are attended by every query of the wave, none at wmax and above by any
-  int wmin = lim, wmax = lim;
+  int wmin = it.lim0 + w * 32 / G, wmax = it.lim0 + min(w * 32 + 31, nq - 1) / G;
+  if (it.mode & ITEM_FLAT) {
+    wmin = wmax = lim;
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    wmin = min(wmin, __shfl_xor(wmin, d, 64));
-    wmax = max(wmax, __shfl_xor(wmax, d, 64));
+    for (int d = 1; d < 32; d <<= 1) {
+      wmin = min(wmin, __shfl_xor(wmin, d, 64));
+      wmax = max(wmax, __shfl_xor(wmax, d, 64));
+    }
   }
-  wmin = __builtin_amdgcn_readfirstlane(wmin);
-  wmax = __builtin_amdgcn_readfirstlane(active ? wmax : 0);
+  wmin = __builtin_amdgcn_readfirstlane(min(wmin, it.k1));
+  wmax = __builtin_amdgcn_readfirstlane(active ? min(wmax, it.k1) : 0);
 
-  // The pages of a tile, one a lane (mod their number), are read a tile ahead of their use, and looked at only there: a look
-  // at them here would wait for them and for the keys requested before them.
-  auto pages = [&](int t) { return table[min(start / kPage + t * (KT / kPage) + (lane & (KT / kPage - 1)), last / kPage)]; };
   // A thread's bytes of a page, load i: chunk lc of key lk, or of keys 16 apart.
   const int lk = tid / NCH, lc = tid % NCH;
   static_assert(kWG / NCH % kPage == 0 && LPT >= 1, "a pass of the workgroup is whole pages");
@@ -641,11 +655,7 @@ __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, ch
   for (int t = 0; t < NT; t++) o[t] = (f32x16)(0.f);
   float m_run = -INFINITY, l_run = 0.f;
 
-  int pg = 0;
-  if (tiles > 0) {
-    request(0, pages(0));
-    pg = pages(1);
-  }
+  if (tiles > 0) request(0, pg0);
   for (int t = 0; t < tiles; t++) {
     const char* tile = lds + (t & 1) * 2 * KBUF;
     const int kb = start + t * KT;  // the tile's first key
@@ -804,6 +814,9 @@ __device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, cha
   const size_t half = (size_t)C.n_kv_heads * kPage * DH;
   const uint16_t* pool = (const uint16_t*)A.kv + (size_t)g * kPage * DH;
   const int* table = C.page_table + (size_t)it.table * C.max_pages;
+  auto pages = [&](int t) { return table[min(start / kPage + t * 2 + (lane & 1), last / kPage)]; };
+  const int pg0 = w < tiles ? pages(w) : 0;
+  int pg = w < tiles ? pages(w + NW) : 0;
   const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;
   const int jj = min(col, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
   const int lim = min(row_limit(A, it, row), it.k1);
@@ -815,7 +828,6 @@ __device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, cha
   wmin = __builtin_amdgcn_readfirstlane(wmin);
 
   // Keys outside [k0, k1) are read as the nearest one inside (see piece_wide).
-  auto pages = [&](int t) { return table[min(start / kPage + t * 2 + (lane & 1), last / kPage)]; };
   auto in_page = [&](int key) { return (uint32_t)(min(max(key, it.k0), last) & (kPage - 1)) * DH; };
   uint4 kr[VL], vr[VL];  // whole rows, so that a load takes whole lines
   auto load = [&](int t, int pg) {
@@ -851,11 +863,7 @@ __device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, cha
 #pragma unroll
   for (int t = 0; t < NT; t++) o[t] = (f32x4)(0.f);
   float m_run = -INFINITY, l_run = 0.f;
-  int pg = 0;
-  if (w < tiles) {
-    load(w, pages(w));
-    pg = pages(w + NW);
-  }
+  if (w < tiles) load(w, pg0);
   for (int t = w; t < tiles; t += NW) {
     const int kb = start + t * KT;
 #pragma unroll
@@ -1110,8 +1118,8 @@ __device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, cha
 template <typename T, int DH>
 __global__ __launch_bounds__(kWG, 2) void k_attend_bf16(SeqArgs A, const int* count, const Item* items, Records R) {
   extern __shared__ __align__(16) char lds[];
+  const Item it = items[blockIdx.y];  // beside the count, not behind it: the list has an entry for every workgroup
   if ((int)blockIdx.y >= count[0]) return;
-  const Item it = items[blockIdx.y];
   if (it.mode & ITEM_FEW)
     piece_few<T, DH>(A, it, R, lds);
   else
@@ -1199,13 +1207,13 @@ Request request(const spd_cache& c, int n_q_heads, int nseqs, int rows, int ngro
   const int hkv = c.n_kv_heads, G = n_q_heads / hkv;
   q.rpt = 128 / G;
   q.qpu = c.head_dim == 128 ? merge_queries<128>() : merge_queries<64>();
-  // a job of at most kMinChunk keys is not split: then prompts have nothing to join
-  const bool split = max_len == 0 || max_len > kMinChunk;
+  // a job of at most kMinChunk / 2 keys is not split: then prompts have nothing to join
+  const bool split = max_len == 0 || max_len > kMinChunk / 2;
   q.wanted = split ? std::max(1, kWantedWGs / hkv) : 0;
   q.merge = split || (prefix && ngroups > 0);
   q.tiles = prefix && ngroups > 0 ? nseqs / q.rpt + ngroups : 0;
   q.jobs = prefix ? q.tiles + nseqs : rows / q.rpt + nseqs;
-  // jobs of more than `chunk` >= keys / wanted: fewer than `wanted` of them, with fewer than 2 `wanted` pieces
+  // jobs that cost more than a share (all costs / wanted): fewer than `wanted` of them, with fewer than 2 `wanted` pieces
   q.items = (size_t)q.jobs + 2 * q.wanted;
   q.merges = prefix ? nseqs : q.wanted;
   const int most = prefix ? G : std::min(q.rpt, rows) * G;  // queries of a merge
@@ -1256,6 +1264,7 @@ void run_attention(const SeqArgs& a, int dtype, const Request& q, bool prefix, v
   p.rpt = q.rpt;
   p.tiles = q.tiles;
   p.jobs = q.jobs;
+  p.wide_cost = dtype == SPD_BF16 ? 1 : 4;
   p.qpu = q.qpu;
   p.records = q.records;
   p.count = (int*)ws;
