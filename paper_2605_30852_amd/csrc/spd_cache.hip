@@ -547,7 +547,7 @@ extern "C" spd_status spd_cache_append(const spd_cache* c, int32_t layer, const 
   if (layer < 0 || layer >= c->n_layers) return invalid(call, "no such layer");
   if (!seqs || !cu_rows || misaligned(seqs, 4) || misaligned(cu_rows, 4)) return invalid(call, "NULL or misaligned pointer");
   if (nseqs < 1 || nseqs > c->max_seqs) return invalid(call, "nseqs must be in [1, max_seqs]");
-  if (rows < 0) return invalid(call, "rows must not be negative");
+  if (rows < 0 || rows >= 1 << 24) return invalid(call, "rows must be in [0, 2^24)");
   if ((st = check_rows(call, k, k_stride, c->n_kv_heads, c->head_dim, dtype)) != SPD_OK) return st;
   if ((st = check_rows(call, v, v_stride, c->n_kv_heads, c->head_dim, dtype)) != SPD_OK) return st;
   if (n_q_heads < 0 || n_q_heads > 16384 || (n_q_heads == 0) != (q == nullptr) || (q == nullptr) != (q_out == nullptr))

@@ -6,14 +6,15 @@
 
 namespace spd {
 
-// Last i in [0, n) with at[i] <= r, for ascending at with at[0] <= r; by a whole wave, 64 probes a round (two rounds
+// Last i in [0, n) with at(i) <= r, for at that ascends from at(0) <= r; by a whole wave, 64 probes a round (two rounds
 // up to 4096 entries, where a binary search waits for twelve loads one after the other).
-__device__ __forceinline__ int find_last(const int* at, int n, int r) {
+template <typename F>
+__device__ __forceinline__ int find_last(int n, int r, F at) {
   const int lane = threadIdx.x & 63;
   int lo = 0;
   while (n > 1) {
     const int step = (n + 63) / 64;
-    const bool le = lane * step < n && at[lo + lane * step] <= r;
+    const bool le = lane * step < n && at(lo + lane * step) <= r;
     const int k = max(__popcll(__ballot(le)) - 1, 0);
     lo += k * step;
     n = min(step, n - k * step);
@@ -29,7 +30,7 @@ struct RowAt {
 };
 
 __device__ __forceinline__ RowAt row_at(const spd_cache& c, const int* seqs, const int* cu_rows, int nseqs, int r) {
-  const int i = find_last(cu_rows, nseqs, r);
+  const int i = find_last(nseqs, r, [&](int k) { return cu_rows[k]; });
   const int begin = cu_rows[i], end = cu_rows[i + 1], s = seqs[i];
   RowAt a{-1, -1};
   if (begin > r || r >= end || begin < 0 || (unsigned)s >= (unsigned)c.max_seqs) return a;

@@ -22,7 +22,7 @@ struct SeqArgs {
   const int* seqs;
   const int* cu;      // prompts: cu_rows; decode rows: cu_groups
   const int* prefix;  // decode rows: prefix_lens
-  int hq, G, nseqs, rows, ngroups;
+  int hq, G, nseqs, rows, ngroups, rpt;
   float scale;
 };
 
@@ -153,6 +153,7 @@ struct Merge {
 constexpr int kPlanWG = 1024;
 constexpr int kMinChunk = 256;
 constexpr int kWantedWGs = 512;
+constexpr size_t kMaxWGs = (1 << 24) - 1;  // of 256 threads: a launch's threads are below 2^32
 constexpr int kBuckets = 64;  // a wave's lanes
 
 // The sums of some queries: `query` of merge `merge` and those behind it, as many as a workgroup of the merge takes.
@@ -542,8 +543,8 @@ __device__ __forceinline__ int row_limit(const SeqArgs& A, const Item& it, int r
 
 // Query j of a piece again, in plain arithmetic, in the place of its result.
 template <typename T, typename KVT, int DH>
-__device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, int j, float* lds) {
-  const int g = blockIdx.x, r = it.row0 + j / A.G, head = g * A.G + j % A.G, d = 4 * (threadIdx.x % (DH / 4));
+__device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, int g, int j, float* lds) {
+  const int r = it.row0 + j / A.G, head = g * A.G + j % A.G, d = 4 * (threadIdx.x % (DH / 4));
   const int n = min(row_limit(A, it, r), it.k1);
   float a[4] = {0.f, 0.f, 0.f, 0.f}, M = -INFINITY, L = 0.f;
   bool holds = threadIdx.x < DH / 4;
@@ -576,7 +577,7 @@ __device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, 
 // wait for the direct loads before it, and so the request has the softmax and the products to land in.
 // Two workgroups are on a CU, so that one's matrix work meets the other's vector work.
 template <typename T, int DH>
-__device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, char* lds) {
+__device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, int g, char* lds) {
   constexpr int NP = sizeof(T) == 4 ? 3 : 1;
   constexpr int KT = NP == 3 && DH == 128 ? 32 : 64;  // 32: three planes of q leave no registers for 64
   constexpr int NT = DH / 32, KS = DH / 16, NCH = DH / 8, SB = KT / 32;
@@ -584,7 +585,7 @@ __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, ch
   constexpr int KROT = DH == 128 ? 0 : 1;  // K: chunk c of key k sits at c ^ (k >> KROT) % NCH: 16 keys in 64 banks
   constexpr int VROT = DH == 128 ? 0 : 1;  // V: chunk c of key k sits at c ^ (k % 8 >> VROT) << 1
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
-  const int g = blockIdx.x, G = A.G, nq = it.nrows * G;
+  const int G = A.G, nq = it.nrows * G;
   const spd_cache& C = A.c;
   const int last = it.k1 - 1;
   const int start = it.k0 & ~(kPage - 1), tiles = (it.k1 - start + KT - 1) / KT;
@@ -791,7 +792,61 @@ __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, ch
   __syncthreads();  // every result is stored, and the tiles are free
   for (int i = 0; i < kWG / 64; i++)
     for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u)
-      plain_piece<T, uint16_t, DH>(A, it, R, i * 32 + __builtin_ctz(m), (float*)lds);
+      plain_piece<T, uint16_t, DH>(A, it, R, g, i * 32 + __builtin_ctz(m), (float*)lds);
+}
+
+// The end of a piece of few queries: lane l holds dims 16 t + 4 (l / 16) .. + 3 of query l % 16, over its wave's keys. The waves' sums
+// are joined in wave order and written.
+template <typename T, typename KVT, int DH>
+__device__ void finish_few(const SeqArgs& A, const Item& it, const Records R, int g, const f32x4 (&o)[DH / 16], float m_run,
+                           float l_run, char* lds) {
+  constexpr int NW = kWG / 64, NT = DH / 16;
+  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, col = lane & 15, q4 = lane >> 4;
+  const int G = A.G, nq = it.nrows * G;
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+
+  // The waves' sums, in wave order.
+  __shared__ float2 s_ml[NW][16];
+  __shared__ uint32_t s_few_bad;
+  if (tid == 0) s_few_bad = 0u;
+  __syncthreads();  // every wave is done with its tile
+  float* ow = (float*)lds;  // [wave][query][dim]
+#pragma unroll
+  for (int tt = 0; tt < NT; tt++)
+    *reinterpret_cast<float4*>(ow + (w * 16 + col) * DH + tt * 16 + q4 * 4) = make_float4(o[tt][0], o[tt][1], o[tt][2], o[tt][3]);
+  if (q4 == 0) s_ml[w][col] = make_float2(m_run, l_run);
+  __syncthreads();
+  for (int i = tid; i < nq * (DH / 4); i += kWG) {
+    const int j = i / (DH / 4), d = i % (DH / 4) * 4, r = it.row0 + j / G, hd = g * G + j % G;
+    const int n = min(row_limit(A, it, r), it.k1);
+    float M = -INFINITY, L = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < NW; x++) M = fmaxf(M, s_ml[x][j].x);
+#pragma unroll
+    for (int x = 0; x < NW; x++) {
+      const float2 ml = s_ml[x][j];
+      const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+      const float4 v = *reinterpret_cast<const float4*>(ow + (x * 16 + j) * DH + d);
+      L = fmaf(ml.y, f, L);
+      a[0] = fmaf(v.x, f, a[0]);
+      a[1] = fmaf(v.y, f, a[1]);
+      a[2] = fmaf(v.z, f, a[2]);
+      a[3] = fmaf(v.w, f, a[3]);
+    }
+    if ((!(L > 0.f) && n > it.k0) || a[0] != a[0] || a[1] != a[1] || a[2] != a[2] || a[3] != a[3]) {
+      atomicOr(&s_few_bad, 1u << j);
+    } else if (it.rec < 0) {
+      store4((T*)A.out + r * A.os + hd * DH + d, a, n > 0 ? 1.0f / L : 0.f);
+    } else {
+      const size_t at = (size_t)it.rec + (size_t)g * nq + j;
+      store4(R.o + at * DH + d, a, 1.0f);
+      if (d == 0) R.ml[at] = make_float2(M, L);
+    }
+  }
+  __syncthreads();
+  for (uint32_t m = __builtin_amdgcn_readfirstlane(s_few_bad); m != 0u; m &= m - 1u)
+    plain_piece<T, KVT, DH>(A, it, R, g, __builtin_ctz(m), (float*)lds);
 }
 
 // A piece of bf16 keys for up to 16 queries: each wave takes every fourth set of 32 keys by itself, with no barrier until
@@ -802,12 +857,12 @@ __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, ch
 //   O^T += V^T P^T over the 32 keys at once: k = 8 q .. 8 q + 7 of lanes 16 q .. are the keys 4 q + 0..3 and 16 + 4 q + 0..3 whose
 //     probabilities they hold. K and V pass through a tile of LDS of the wave's own: loads take whole rows, operands 16 rows at once.
 template <typename T, int DH>
-__device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, char* lds) {
+__device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, int g, char* lds) {
   constexpr int NP = sizeof(T) == 4 ? 3 : 1;
   constexpr int KT = 32, NW = kWG / 64, KS = DH / 32, NT = DH / 16, NCH = DH / 8, KPL = 64 / NCH;  // KPL: keys of a wave's load
   constexpr int VL = KT / KPL;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, q4 = lane >> 4;
-  const int g = blockIdx.x, G = A.G, nq = it.nrows * G;
+  const int G = A.G, nq = it.nrows * G;
   const spd_cache& C = A.c;
   const int last = it.k1 - 1;
   const int start = it.k0 & ~(kPage - 1), tiles = (it.k1 - start + KT - 1) / KT;
@@ -928,61 +983,120 @@ __device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, cha
       for (int p = NP - 1; p >= 0; p--) o[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.f, pf[p].f, o[tt], 0, 0, 0);
     }
   }
-  l_run += __shfl_xor(l_run, 16, 64);
-  l_run += __shfl_xor(l_run, 32, 64);
+  finish_few<T, uint16_t, DH>(A, it, R, g, o, m_run, l_run, lds);
+}
 
-  // The waves' sums, in wave order.
-  __shared__ float2 s_ml[NW][16];
-  __shared__ uint32_t s_few_bad;
-  if (tid == 0) s_few_bad = 0u;
-  __syncthreads();  // every wave is done with its tile
-  float* ow = (float*)lds;  // [wave][query][dim]
+// The same over an fp32 cache, 16 keys at a time, with v_mfma_f32_16x16x4_f32 (lane l supplies k = l / 16 of A row and B column
+// l % 16): a lane's four dims of a chunk are four steps; p is used as it is, register v of lanes 16 q .. being key 4 q + v.
+template <int DH>
+__device__ void piece_few_f32(const SeqArgs& A, const Item& it, const Records R, int g, char* lds) {
+  constexpr int KT = 16, NW = kWG / 64, KS = DH / 16, NT = DH / 16, NCH = DH / 4, KPL = 64 / NCH, VL = KT / KPL;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, q4 = lane >> 4;
+  const int G = A.G, nq = it.nrows * G;
+  const spd_cache& C = A.c;
+  const int last = it.k1 - 1;
+  const int start = it.k0 & ~(kPage - 1), tiles = (it.k1 - start + KT - 1) / KT;  // a tile is a page
+  const size_t half = (size_t)C.n_kv_heads * kPage * DH;
+  const float* pool = (const float*)A.kv + (size_t)g * kPage * DH;
+  const int* table = C.page_table + (size_t)it.table * C.max_pages;
+  auto page_at = [&](int t) { return table[min(start / kPage + t, last / kPage)]; };
+  const int pg0 = w < tiles ? page_at(w) : 0;
+  int pg = w < tiles ? page_at(w + NW) : 0;
+  const int jj = min(col, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
+  const int lim = min(row_limit(A, it, row), it.k1);
+  float4 qf[KS];
+  {
+    const float* q = (const float*)A.q + row * A.qs + head * DH + q4 * 4;
+    const float f = A.scale * kLog2e;
 #pragma unroll
-  for (int tt = 0; tt < NT; tt++)
-    *reinterpret_cast<float4*>(ow + (w * 16 + col) * DH + tt * 16 + q4 * 4) = make_float4(o[tt][0], o[tt][1], o[tt][2], o[tt][3]);
-  if (q4 == 0) s_ml[w][col] = make_float2(m_run, l_run);
-  __syncthreads();
-  for (int i = tid; i < nq * (DH / 4); i += kWG) {
-    const int j = i / (DH / 4), d = i % (DH / 4) * 4, r = it.row0 + j / G, hd = g * G + j % G;
-    const int n = min(row_limit(A, it, r), it.k1);
-    float M = -INFINITY, L = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int x = 0; x < NW; x++) M = fmaxf(M, s_ml[x][j].x);
-#pragma unroll
-    for (int x = 0; x < NW; x++) {
-      const float2 ml = s_ml[x][j];
-      const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-      const float4 v = *reinterpret_cast<const float4*>(ow + (x * 16 + j) * DH + d);
-      L = fmaf(ml.y, f, L);
-      a[0] = fmaf(v.x, f, a[0]);
-      a[1] = fmaf(v.y, f, a[1]);
-      a[2] = fmaf(v.z, f, a[2]);
-      a[3] = fmaf(v.w, f, a[3]);
-    }
-    if ((!(L > 0.f) && n > it.k0) || a[0] != a[0] || a[1] != a[1] || a[2] != a[2] || a[3] != a[3]) {
-      atomicOr(&s_few_bad, 1u << j);
-    } else if (it.rec < 0) {
-      store4((T*)A.out + r * A.os + hd * DH + d, a, n > 0 ? 1.0f / L : 0.f);
-    } else {
-      const size_t at = (size_t)it.rec + (size_t)g * nq + j;
-      store4(R.o + at * DH + d, a, 1.0f);
-      if (d == 0) R.ml[at] = make_float2(M, L);
+    for (int s = 0; s < KS; s++) {
+      const float4 x = *reinterpret_cast<const float4*>(q + s * 16);
+      qf[s] = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
     }
   }
-  __syncthreads();
-  for (uint32_t m = __builtin_amdgcn_readfirstlane(s_few_bad); m != 0u; m &= m - 1u)
-    plain_piece<T, uint16_t, DH>(A, it, R, __builtin_ctz(m), (float*)lds);
+  uint4 kr[VL], vr[VL];
+  auto load = [&](int t, int pg) {
+    const float* p = pool + (size_t)page_to_read(C, __builtin_amdgcn_readfirstlane(pg)) * 2 * half;
+    const int first = start + t * KT;
+#pragma unroll
+    for (int i = 0; i < VL; i++) {
+      const float* at = p + (uint32_t)(min(max(first + i * KPL + lane / NCH, it.k0), last) & (kPage - 1)) * DH + lane % NCH * 4;
+      kr[i] = ldg16(at);
+      vr[i] = ldg16(at + half);
+    }
+  };
+  // K: chunk c of key k sits at c ^ k; V: at c ^ (k / 4) << 2, so that the four keys of a read are in different banks
+  char* kt = lds + w * 2 * KT * DH * 4;
+  char* vt = kt + KT * DH * 4;
+  f32x4 o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; t++) o[t] = (f32x4)(0.f);
+  float m_run = -INFINITY, l_run = 0.f;
+  if (w < tiles) load(w, pg0);
+  for (int t = w; t < tiles; t += NW) {
+    const int kb = start + t * KT;
+#pragma unroll
+    for (int i = 0; i < VL; i++) {
+      const int k = i * KPL + lane / NCH, c = lane % NCH;
+      *reinterpret_cast<uint4*>(kt + k * DH * 4 + ((c ^ k) << 4)) = kr[i];
+      *reinterpret_cast<uint4*>(vt + k * DH * 4 + ((c ^ (k >> 2) << 2) << 4)) = vr[i];
+    }
+    if (t + NW < tiles) {
+      load(t + NW, pg);
+      pg = page_at(t + 2 * NW);
+    }
+    f32x4 s = (f32x4)(0.f);
+#pragma unroll
+    for (int k = 0; k < KS; k++) {
+      const float4 kf = *reinterpret_cast<const float4*>(kt + col * DH * 4 + (((4 * k + q4) ^ col) << 4));
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.x, qf[k].x, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.y, qf[k].y, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.z, qf[k].z, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.w, qf[k].w, s, 0, 0, 0);
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < 4; v++) {
+      const int kk = kb + 4 * q4 + v;
+      s[v] = kk < lim && kk >= it.k0 ? s[v] : -INFINITY;
+      mx = fmaxf(mx, s[v]);
+    }
+    if (__any(mx > m_run + 8.0f)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float mn = fmaxf(m_run, mx);
+      const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - mn);
+      l_run *= al;
+#pragma unroll
+      for (int tt = 0; tt < NT; tt++) o[tt] *= al;
+      m_run = mn;
+    }
+    const float off = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+    for (int v = 0; v < 4; v++) {
+      s[v] = __builtin_amdgcn_exp2f(s[v] - off);
+      l_run += s[v];
+    }
+#pragma unroll
+    for (int v = 0; v < 4; v++)
+#pragma unroll
+      for (int tt = 0; tt < NT; tt++) {
+        const float vf = *reinterpret_cast<const float*>(vt + (4 * q4 + v) * DH * 4 + (((tt * 4 + col / 4) ^ q4 << 2) << 4) + (col & 3) * 4);
+        o[tt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf, s[v], o[tt], 0, 0, 0);
+      }
+  }
+  finish_few<float, float, DH>(A, it, R, g, o, m_run, l_run, lds);
 }
 
 // The same over an fp32 cache, for 32 queries a wave, with v_mfma_f32_32x32x2_f32 (lane l supplies k = l / 32 of A row
 // and B column l % 32; accumulators as above): a lane's four dims of a chunk are four steps, so the halves take chunks in
 // turn. P is used as it is. Tiles of 32 keys.
 template <int DH>
-__device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, char* lds) {
+__device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, int g, char* lds) {
   constexpr int KT = 32, NT = DH / 32, KS = DH / 8, NCH = DH / 4;
   constexpr int KBUF = KT * DH * 4, BUF = 2 * KBUF, LPT = KT * NCH / kWG;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
-  const int g = blockIdx.x, G = A.G, nq = it.nrows * G;
+  const int G = A.G, nq = it.nrows * G;
   const spd_cache& C = A.c;
   const int last = it.k1 - 1;
   const int start = it.k0 & ~(kPage - 1), tiles = (it.k1 - start + KT - 1) / KT;
@@ -1111,26 +1225,72 @@ __device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, cha
   __syncthreads();
   for (int i = 0; i < 4; i++)
     for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u)
-      plain_piece<float, float, DH>(A, it, R, i * 32 + __builtin_ctz(m), (float*)lds);
+      plain_piece<float, float, DH>(A, it, R, g, i * 32 + __builtin_ctz(m), (float*)lds);
 }
 
-// Grid: x = KV head (with 8 of them a head's keys stay in one XCD's L2), y = piece.
+// The piece of a call without a plan: a tile of at most 16 queries, or a decode row, over all its keys.
+__device__ __forceinline__ bool direct_item(const SeqArgs& A, int y, Item& it) {
+  it.k0 = 0;
+  it.rec = -1;
+  if (A.cu == nullptr) {
+    it.table = A.seqs[y];
+    if ((unsigned)it.table >= (unsigned)A.c.max_seqs) return false;
+    it.row0 = y;
+    it.nrows = 1;
+    it.k1 = seq_len(A.c, it.table);
+    it.lim0 = 0;
+    it.mode = ITEM_FLAT | ITEM_FEW;
+    return true;
+  }
+  const int i = find_last(A.nseqs, y, [&](int k) { return A.cu[k] / A.rpt + k; });
+  const int begin = A.cu[i], stop = A.cu[i + 1], end = min(stop, A.rows);
+  it.table = A.seqs[i];
+  if (begin < 0 || begin >= end || (unsigned)it.table >= (unsigned)A.c.max_seqs) return false;
+  const long long row0 = begin + (long long)(y - (begin / A.rpt + i)) * A.rpt;
+  if (row0 < begin || row0 >= end) return false;
+  it.row0 = (int)row0;
+  it.nrows = min(A.rpt, end - it.row0);
+  it.lim0 = (int)max((long long)seq_len(A.c, it.table) - stop + it.row0 + 1, -(1ll << 30));
+  it.k1 = max(0, it.lim0 + it.nrows - 1);
+  it.mode = ITEM_FEW;
+  return true;
+}
+
+// Grid: a piece's KV heads one after the other (with 8 of them a head's keys stay in one XCD's L2).
 template <typename T, int DH>
 __global__ __launch_bounds__(kWG, 2) void k_attend_bf16(SeqArgs A, const int* count, const Item* items, Records R) {
   extern __shared__ __align__(16) char lds[];
-  const Item it = items[blockIdx.y];  // beside the count, not behind it: the list has an entry for every workgroup
-  if ((int)blockIdx.y >= count[0]) return;
+  const int g = blockIdx.x % A.c.n_kv_heads, y = blockIdx.x / A.c.n_kv_heads;
+  const Item it = items[y];  // beside the count, not behind it: the list has an entry for every workgroup
+  if (y >= count[0]) return;
   if (it.mode & ITEM_FEW)
-    piece_few<T, DH>(A, it, R, lds);
+    piece_few<T, DH>(A, it, R, g, lds);
   else
-    piece_wide<T, DH>(A, it, R, lds);
+    piece_wide<T, DH>(A, it, R, g, lds);
 }
 
 template <int DH>
 __global__ __launch_bounds__(kWG, 2) void k_attend_f32(SeqArgs A, const int* count, const Item* items, Records R) {
   extern __shared__ __align__(16) char lds[];
-  if ((int)blockIdx.y >= count[0]) return;
-  piece_f32<DH>(A, items[blockIdx.y], R, lds);
+  const int g = blockIdx.x % A.c.n_kv_heads, y = blockIdx.x / A.c.n_kv_heads;
+  const Item it = items[y];
+  if (y >= count[0]) return;
+  if (it.mode & ITEM_FEW)
+    piece_few_f32<DH>(A, it, R, g, lds);
+  else
+    piece_f32<DH>(A, it, R, g, lds);
+}
+
+template <typename T, typename KVT, int DH>
+__global__ __launch_bounds__(kWG, 2) void k_attend_direct(SeqArgs A) {
+  extern __shared__ __align__(16) char lds[];
+  Item it;
+  const int g = blockIdx.x % A.c.n_kv_heads;
+  if (!direct_item(A, blockIdx.x / A.c.n_kv_heads, it)) return;
+  if constexpr (sizeof(KVT) == 2)
+    piece_few<T, DH>(A, it, Records{}, g, lds);
+  else
+    piece_few_f32<DH>(A, it, Records{}, g, lds);
 }
 
 // Records to outputs. Grid: x = KV head, y = units (strided). The DH / 4 lanes of a query first hold a piece's (m, l) each,
@@ -1197,7 +1357,7 @@ __global__ __launch_bounds__(kWG) void k_merge(SeqArgs A, const int* count, cons
 // What a call takes: its tiles, and its workspace (the plan's lists, then the records).
 struct Request {
   int rpt, wanted, jobs, tiles, qpu;
-  bool merge;
+  bool direct, merge;
   size_t items, merges, units, records;
   size_t at_items, at_merges, at_units, at_tiles, at_ml, at_o, bytes;
 };
@@ -1205,6 +1365,16 @@ struct Request {
 Request request(const spd_cache& c, int n_q_heads, int nseqs, int rows, int ngroups, int max_len, bool prefix) {
   Request q{};
   const int hkv = c.n_kv_heads, G = n_q_heads / hkv;
+  // Short calls that the GPU holds at once go without a plan, one launch: prompts whose tiles of 16 queries are at most two a
+  // CU, decode rows that share nothing. 63 fp32 rows of up to 65 keys: 9.0 us against 17.4 with plan and tiles of 128
+  // queries; 64 bf16 rows of 512 keys each: 14 us against 19. Longer ones need the splits, larger ones the wide tiles.
+  const bool fits = max_len > 0 && max_len <= 512;
+  q.rpt = 16 / G;
+  q.direct = fits && (prefix ? ngroups == 0 && nseqs * hkv <= 2048 : ((long long)rows / q.rpt + nseqs) * hkv <= 512);
+  if (q.direct) {
+    q.jobs = prefix ? nseqs : rows / q.rpt + nseqs;
+    return q;
+  }
   q.rpt = 128 / G;
   q.qpu = c.head_dim == 128 ? merge_queries<128>() : merge_queries<64>();
   // a job of at most kMinChunk / 2 keys is not split: then prompts have nothing to join
@@ -1237,19 +1407,30 @@ Request request(const spd_cache& c, int n_q_heads, int nseqs, int rows, int ngro
 
 template <typename T, int DH>
 void launch(const SeqArgs& a, const Request& q, const PlanArgs& p, const Records& r, hipStream_t s) {
-  const dim3 grid(a.c.n_kv_heads, (unsigned)q.items);
-  if (a.c.dtype == SPD_BF16) {
-    hipLaunchKernelGGL((k_attend_bf16<T, DH>), grid, dim3(kWG), 2 * 2 * 64 * DH * 2, s, a, p.count, p.items, r);
+  const bool bf16 = a.c.dtype == SPD_BF16;
+  const size_t shm = 2 * 2 * 32 * DH * 4;  // either kind: two tiles of K and V, or a wave's own
+  if (q.direct) {
+    const dim3 grid((unsigned)(a.c.n_kv_heads * q.jobs));
+    if (bf16)
+      hipLaunchKernelGGL((k_attend_direct<T, uint16_t, DH>), grid, dim3(kWG), shm, s, a);
+    else
+      hipLaunchKernelGGL((k_attend_direct<float, float, DH>), grid, dim3(kWG), shm, s, a);
+    return;
+  }
+  const dim3 grid((unsigned)(a.c.n_kv_heads * q.items));
+  if (bf16) {
+    hipLaunchKernelGGL((k_attend_bf16<T, DH>), grid, dim3(kWG), shm, s, a, p.count, p.items, r);
   } else {
-    hipLaunchKernelGGL((k_attend_f32<DH>), grid, dim3(kWG), 2 * 2 * 32 * DH * 4, s, a, p.count, p.items, r);
+    hipLaunchKernelGGL((k_attend_f32<DH>), grid, dim3(kWG), shm, s, a, p.count, p.items, r);
   }
   if (q.merge)
     hipLaunchKernelGGL((k_merge<T, DH>), dim3(a.c.n_kv_heads, (unsigned)std::min<size_t>(q.units, kMergeRows)), dim3(kWG), 0, s, a,
                        p.count, p.units, p.merges, r);
 }
 
-// Plan, pieces, merge.
-void run_attention(const SeqArgs& a, int dtype, const Request& q, bool prefix, void* workspace, hipStream_t s) {
+// Plan, pieces, merge; or the pieces alone.
+void run_attention(SeqArgs a, int dtype, const Request& q, bool prefix, void* workspace, hipStream_t s) {
+  a.rpt = q.rpt;
   char* ws = (char*)workspace;
   PlanArgs p{};
   p.c = a.c;
@@ -1267,16 +1448,19 @@ void run_attention(const SeqArgs& a, int dtype, const Request& q, bool prefix, v
   p.wide_cost = dtype == SPD_BF16 ? 1 : 4;
   p.qpu = q.qpu;
   p.records = q.records;
-  p.count = (int*)ws;
-  p.items = (Item*)(ws + q.at_items);
-  p.merges = (Merge*)(ws + q.at_merges);
-  p.units = (Unit*)(ws + q.at_units);
-  p.tile_rec = (int4*)(ws + q.at_tiles);
-  const Records r{(float*)(ws + q.at_o), (float2*)(ws + q.at_ml)};
-  if (prefix)
-    hipLaunchKernelGGL((k_plan_attention<true>), dim3(1), dim3(kPlanWG), 0, s, p);
-  else
-    hipLaunchKernelGGL((k_plan_attention<false>), dim3(1), dim3(kPlanWG), 0, s, p);
+  Records r{};
+  if (!q.direct) {
+    p.count = (int*)ws;
+    p.items = (Item*)(ws + q.at_items);
+    p.merges = (Merge*)(ws + q.at_merges);
+    p.units = (Unit*)(ws + q.at_units);
+    p.tile_rec = (int4*)(ws + q.at_tiles);
+    r = Records{(float*)(ws + q.at_o), (float2*)(ws + q.at_ml)};
+    if (prefix)
+      hipLaunchKernelGGL((k_plan_attention<true>), dim3(1), dim3(kPlanWG), 0, s, p);
+    else
+      hipLaunchKernelGGL((k_plan_attention<false>), dim3(1), dim3(kPlanWG), 0, s, p);
+  }
   const bool wide = a.c.head_dim == 128;
   if (dtype == SPD_BF16)
     wide ? launch<uint16_t, 128>(a, q, p, r, s) : launch<uint16_t, 64>(a, q, p, r, s);
@@ -1335,7 +1519,9 @@ extern "C" spd_status spd_prompt_attention_workspace(const spd_cache* c, int32_t
   const spd_status st = check_sizes(call, c, n_q_heads, dtype, nseqs, max_len);
   if (st != SPD_OK) return st;
   if (!bytes || rows < 0) return invalid(call, "NULL pointer or negative rows");
-  *bytes = request(*c, n_q_heads, nseqs, rows, 0, max_len, false).bytes;
+  const Request q = request(*c, n_q_heads, nseqs, rows, 0, max_len, false);
+  if (q.items * c->n_kv_heads > kMaxWGs) return invalid(call, "more rows than one launch takes (2^24 tiles of 128 queries, with all KV heads)");
+  *bytes = q.bytes;
   return SPD_OK;
 }
 
