@@ -89,12 +89,7 @@ __device__ __forceinline__ int pages_of(int keys) { return (keys + kPage - 1) / 
 // Exclusive prefix sum of v over the workgroup, and the total; sums: kPlanWaves + 1 entries of LDS.
 __device__ __forceinline__ long long plan_scan(long long v, long long* sums, long long* total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  long long x = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const long long y = __shfl_up(x, d, 64);
-    if (lane >= d) x += y;
-  }
+  const long long x = (long long)wave_scan((unsigned long long)v);
   __syncthreads();  // the last tile's sums are read
   if (lane == 63) sums[w] = x;
   __syncthreads();

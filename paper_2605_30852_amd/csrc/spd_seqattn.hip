@@ -348,12 +348,9 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
       sum += c;
       longest = max(longest, c);
     });
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      sum += __shfl_xor(sum, d, 64);
-      longest = max(longest, __shfl_xor(longest, d, 64));
-    }
-    if ((tid & 63) == 0) {
+    sum = wave_scan(sum);
+    longest = wave_top(longest);
+    if ((tid & 63) == 63) {
       atomicAdd(&s_total, sum);
       atomicMax(&s_max, longest);
     }
@@ -381,13 +378,7 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
   });
   __syncthreads();
   if (tid < kBuckets) {  // bucket counts to their first places
-    const int v = s_count[tid];
-    int x = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int y = __shfl_up(x, d, 64);
-      if (tid >= d) x += y;
-    }
+    const int v = s_count[tid], x = (int)wave_scan((unsigned)v);
     s_count[tid] = x - v;
     if (tid == kBuckets - 1) P.count[0] = s_items = x;
   }
@@ -410,12 +401,7 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
     const int nq = k.is ? k.j.nrows * P.G : 0, units = (nq + P.qpu - 1) / P.qpu;
     const bool joins = k.is && (n > 1 || k.shared);
     const unsigned long long v = joins ? (unsigned long long)(unsigned)(n * nq) << 32 | (tile ? 0 : 1u << 16 | units) : 0ull;
-    unsigned long long x = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const unsigned long long y = __shfl_up(x, d, 64);
-      if ((tid & 63) >= d) x += y;
-    }
+    const unsigned long long x = wave_scan(v);
     if ((tid & 63) == 63) s_sums[tid >> 6] = x;
     __syncthreads();
     unsigned long long at = before + x - v;
@@ -508,6 +494,12 @@ __device__ __forceinline__ void planes_of(float p0, float p1, uint32_t (&u)[3]) 
   u[1] = __builtin_amdgcn_perm(m1, m0, 0x07060302u);
   u[2] = __builtin_amdgcn_perm(l1, l0, 0x07060302u);
 }
+
+// l plus what was made of the two: the rounded values in one instruction (1% of a long prompt's time), or the values.
+__device__ __forceinline__ float add_planes(float l, float, float, const uint32_t (&u)[1]) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, u[0]), __builtin_bit_cast(bf16x2, 0x3f803f80u), l, false);
+}
+__device__ __forceinline__ float add_planes(float l, float p0, float p1, const uint32_t (&)[3]) { return l + (p0 + p1); }
 
 // A lane's part of a query: 8 dims from q on, every `step`. bf16 as they are; fp32 times f, as planes.
 template <typename T, int KS, int STEP, int NP>
@@ -744,9 +736,9 @@ __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, in
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
         const float p0 = __builtin_amdgcn_exp2f(fmaf(s[x][e], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(s[x][e + 1], sc, -off));
-        l_run += p0 + p1;
         uint32_t pl[NP];
         planes_of(p0, p1, pl);
+        l_run = add_planes(l_run, p0, p1, pl);
 #pragma unroll
         for (int p = 0; p < NP; p++) pf[p].u[e >> 1] = pl[p];
       }
@@ -968,9 +960,9 @@ __device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, int
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
       const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][(e & 3) + 1], sc, -off));
-      l_run += p0 + p1;
       uint32_t pl[NP];
       planes_of(p0, p1, pl);
+      l_run = add_planes(l_run, p0, p1, pl);
 #pragma unroll
       for (int p = 0; p < NP; p++) pf[p].u[e >> 1] = pl[p];
     }
