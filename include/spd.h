@@ -463,8 +463,9 @@ spd_status spd_prompt_attention(const spd_cache* c, int32_t layer, const void* q
 /* Decode attention of a batch in which groups of sequences share a prefix, read once for all of a group. Row i of q
  * (its query at key lens[seqs[i]] - 1) attends keys 0 .. lens[seqs[i]] - 1 of sequence seqs[i]; a sequence without
  * keys gets zeros. Group j is rows cu_groups[j] .. cu_groups[j + 1] - 1 (device int32[ngroups + 1], ascending, from 0 to
- * nseqs); its rows' sequences agree in their first prefix_lens[j] keys (device int32[ngroups]), as forked ones do, which
- * are read through the pages of the group's first sequence. A row shorter than its group's prefix attends the
+ * nseqs); its rows' sequences agree in their first prefix_lens[j] keys (device int32[ngroups]), as forked ones do. Those are
+ * read through the pages of the group's first sequence, once for 128 queries, or, in short calls, by every row through
+ * its own pages, which it has to hold. A row shorter than its group's prefix attends the
  * keys it has; the first row's sequence must hold the prefix. With ngroups 0 (both arrays NULL) no row shares
  * anything. q, out, max_len and the workspace as in spd_prompt_attention; nseqs at most 4096. */
 spd_status spd_prefix_attention_workspace(const spd_cache* c, int32_t n_q_heads, int32_t dtype, int32_t nseqs,

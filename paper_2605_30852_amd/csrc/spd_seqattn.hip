@@ -27,17 +27,17 @@ struct SeqArgs {
 };
 
 // A query over the keys [k0, k1) in plain fp32, by the whole workgroup, which a query, key or value that is not finite
-// needs: there 0 times a value behind the query's own keys, or a plane's 0 * inf, is NaN on matrix cores. Scores in passes of 256 keys, computed twice
+// needs: there 0 times a value behind the query's own keys, or a plane's 0 * inf, is NaN on matrix cores. Scores in passes of a key a thread, computed twice
 // rather than kept. M, L and a (dims 4 d4 .. + 3 of thread d4 = tid % (DH / 4)) are the maximum, the sum and the
-// output; true in the threads that hold them. lds: kWG * 6 floats.
-template <typename T, typename KVT, int DH>
+// output; true in the threads that hold them. lds: NTH * 6 floats.
+template <typename T, typename KVT, int DH, int NTH>
 __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* table, int g, const T* q, float scale, int k0,
                             int k1, float* lds, float& M, float& L, float (&a)[4]) {
-  constexpr int TPQ = DH / 4, NG = kWG / TPQ, NW = kWG / 64;
+  constexpr int TPQ = DH / 4, NG = NTH / TPQ, NW = NTH / 64;
   const int tid = threadIdx.x, d4 = tid % TPQ, grp = tid / TPQ;
   const size_t half = (size_t)c.n_kv_heads * kPage * DH;
   float* sp = lds;
-  float* sr = lds + kWG;
+  float* sr = lds + NTH;
   auto row = [&](int key) { return pool + page_to_read(c, table[key / kPage]) * 2 * half + (size_t)(g * kPage + key % kPage) * DH; };
   auto score = [&](int key) {
     const KVT* k = row(key);
@@ -54,7 +54,7 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
   };
   float m = -INFINITY;
   bool sound = true;
-  for (int key = k0 + tid; key < k1; key += kWG) {
+  for (int key = k0 + tid; key < k1; key += NTH) {
     const float s = score(key);
     m = fmaxf(m, s);
     sound = sound && s < INFINITY;
@@ -81,7 +81,7 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
     return grp == 0;
   }
   L = a[0] = a[1] = a[2] = a[3] = 0.f;
-  for (int base = k0; base < k1; base += kWG) {
+  for (int base = k0; base < k1; base += NTH) {
     float p = 0.f;
     if (base + tid < k1) {
       const float s = score(base + tid);
@@ -89,7 +89,7 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
     }
     sp[tid] = p;
     __syncthreads();
-    const int n = min(kWG, k1 - base);
+    const int n = min(NTH, k1 - base);
     for (int i = grp; i < n; i += NG) {
       const KVT* v = row(base + i) + half + 4 * d4;
       const float2 v0 = ld2<KVT>(v), v1 = ld2<KVT>(v + 2);
@@ -534,14 +534,14 @@ __device__ __forceinline__ int row_limit(const SeqArgs& A, const Item& it, int r
 }
 
 // Query j of a piece again, in plain arithmetic, in the place of its result.
-template <typename T, typename KVT, int DH>
+template <typename T, typename KVT, int DH, int NTH = kWG>
 __device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, int g, int j, float* lds) {
   const int r = it.row0 + j / A.G, head = g * A.G + j % A.G, d = 4 * (threadIdx.x % (DH / 4));
   const int n = min(row_limit(A, it, r), it.k1);
   float a[4] = {0.f, 0.f, 0.f, 0.f}, M = -INFINITY, L = 0.f;
   bool holds = threadIdx.x < DH / 4;
   if (n > it.k0)
-    holds = plain_query<T, KVT, DH>(A.c, (const KVT*)A.kv, A.c.page_table + (size_t)it.table * A.c.max_pages, g,
+    holds = plain_query<T, KVT, DH, NTH>(A.c, (const KVT*)A.kv, A.c.page_table + (size_t)it.table * A.c.max_pages, g,
                                     (const T*)A.q + r * A.qs + head * DH, A.scale, it.k0, n, lds, M, L, a);
   if (!holds) return;
   if (it.rec < 0) {
@@ -551,6 +551,51 @@ __device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, 
     store4(R.o + at * DH + d, a, 1.0f);
     if (d == 0) R.ml[at] = make_float2(M * kLog2e, L);
   }
+}
+
+// The end of a piece of 32 queries a wave: registers 4 v .. + 3 of tile t are dims 32 t + 8 v + 4 h .. + 3 of the lane's query, which
+// attends keys below lim.
+template <typename T, typename KVT, int DH, int NTH>
+__device__ void finish_wide(const SeqArgs& A, const Item& it, const Records R, int g, const f32x16 (&o)[DH / 32], float m_run,
+                            float l_run, int lim, char* lds) {
+  constexpr int NT = DH / 32;
+  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, col = lane & 31, h = lane >> 5;
+  const int G = A.G, nq = it.nrows * G, jq = w * 32 + col, jj = min(jq, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
+  const bool active = w * 32 < nq, mine = jq < nq;
+  l_run += __shfl_xor(l_run, 32, 64);
+
+  __shared__ uint32_t s_bad[NTH / 64];  // queries whose result here is not a number
+  if (tid < NTH / 64) s_bad[tid] = 0u;
+  __syncthreads();
+  if (active) {
+    bool bad = !(l_run > 0.f) && lim > it.k0;  // NaN, or nothing but scores of -inf
+#pragma unroll
+    for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) bad = bad || o[tt][v] != o[tt][v];
+    const unsigned long long bads = __ballot(bad && mine);
+    if (lane == 0) s_bad[w] = (uint32_t)bads | (uint32_t)(bads >> 32);
+    if (mine) {
+      const size_t at = (size_t)max(it.rec, 0) + (size_t)g * nq + jq;
+      const float inv = lim > 0 ? 1.0f / l_run : 0.f;
+#pragma unroll
+      for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4) {
+          const float x[4] = {o[tt][v], o[tt][v + 1], o[tt][v + 2], o[tt][v + 3]};
+          const int d = tt * 32 + 2 * v + 4 * h;
+          if (it.rec < 0)
+            store4((T*)A.out + row * A.os + head * DH + d, x, inv);
+          else
+            store4(R.o + at * DH + d, x, 1.0f);
+        }
+      if (it.rec >= 0 && h == 0) R.ml[at] = make_float2(m_run, l_run);
+    }
+  }
+  __syncthreads();  // every result is stored, and the tiles are free
+  for (int i = 0; i < NTH / 64; i++)
+    for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u)
+      plain_piece<T, KVT, DH, NTH>(A, it, R, g, i * 32 + __builtin_ctz(m), (float*)lds);
 }
 
 // A piece of bf16 keys for 32 queries a wave. Query j of the tile is row row0 + j / G, head g * G + j % G.
@@ -592,7 +637,6 @@ __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, in
   const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;  // from scores to exponents
   const bool active = w * 32 < nq;
   const int jq = w * 32 + col, jj = min(jq, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
-  const bool mine = jq < nq;
   const int lim = min(row_limit(A, it, row), it.k1);
 
   bf16x8 qf[NP][KS];
@@ -751,40 +795,7 @@ __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, in
             o[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x][ks][tt], pf[p].f[ks], o[tt], 0, 0, 0);
     }
   }
-  l_run += __shfl_xor(l_run, 32, 64);
-
-  __shared__ uint32_t s_bad[kWG / 64];  // queries whose result here is not a number
-  if (tid < kWG / 64) s_bad[tid] = 0u;
-  __syncthreads();
-  if (active) {
-    bool bad = !(l_run > 0.f) && lim > it.k0;  // NaN, or nothing but scores of -inf
-#pragma unroll
-    for (int tt = 0; tt < NT; tt++)
-#pragma unroll
-      for (int v = 0; v < 16; v++) bad = bad || o[tt][v] != o[tt][v];
-    const unsigned long long bads = __ballot(bad && mine);
-    if (lane == 0) s_bad[w] = (uint32_t)bads | (uint32_t)(bads >> 32);
-    if (mine) {
-      const size_t at = (size_t)max(it.rec, 0) + (size_t)g * nq + jq;
-      const float inv = lim > 0 ? 1.0f / l_run : 0.f;
-#pragma unroll
-      for (int tt = 0; tt < NT; tt++)
-#pragma unroll
-        for (int v = 0; v < 16; v += 4) {
-          const float x[4] = {o[tt][v], o[tt][v + 1], o[tt][v + 2], o[tt][v + 3]};
-          const int d = tt * 32 + 2 * v + 4 * h;
-          if (it.rec < 0)
-            store4((T*)A.out + row * A.os + head * DH + d, x, inv);
-          else
-            store4(R.o + at * DH + d, x, 1.0f);
-        }
-      if (it.rec >= 0 && h == 0) R.ml[at] = make_float2(m_run, l_run);
-    }
-  }
-  __syncthreads();  // every result is stored, and the tiles are free
-  for (int i = 0; i < kWG / 64; i++)
-    for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u)
-      plain_piece<T, uint16_t, DH>(A, it, R, g, i * 32 + __builtin_ctz(m), (float*)lds);
+  finish_wide<T, uint16_t, DH, kWG>(A, it, R, g, o, m_run, l_run, lim, lds);
 }
 
 // The end of a piece of few queries: lane l holds dims 16 t + 4 (l / 16) .. + 3 of query l % 16, over its wave's keys. The waves' sums
@@ -1097,7 +1108,6 @@ __device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, int
   const int* table = C.page_table + (size_t)it.table * C.max_pages;
   const bool active = w * 32 < nq;
   const int j = w * 32 + col, jj = min(j, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
-  const bool mine = j < nq;
   const int lim = min(row_limit(A, it, row), it.k1);
   float4 qf[KS];
   {
@@ -1188,39 +1198,10 @@ __device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, int
       }
     }
   }
-  l_run += __shfl_xor(l_run, 32, 64);
-  __shared__ uint32_t s_bad[4];
-  if (tid < 4) s_bad[tid] = 0u;
-  __syncthreads();
-  if (active) {
-    bool bad = !(l_run > 0.f) && lim > it.k0;
-#pragma unroll
-    for (int tt = 0; tt < NT; tt++)
-#pragma unroll
-      for (int v = 0; v < 16; v++) bad = bad || o[tt][v] != o[tt][v];
-    const unsigned long long bads = __ballot(bad && mine);
-    if (lane == 0) s_bad[w] = (uint32_t)bads | (uint32_t)(bads >> 32);
-    if (mine) {
-      const size_t at = (size_t)it.rec + (size_t)g * nq + j;
-      float* to = it.rec < 0 ? (float*)A.out + row * A.os + head * DH + 4 * h : R.o + at * DH + 4 * h;
-      const float f = it.rec >= 0 ? 1.0f : lim > 0 ? 1.0f / l_run : 0.f;
-#pragma unroll
-      for (int tt = 0; tt < NT; tt++)
-#pragma unroll
-        for (int v = 0; v < 16; v += 4) {
-          const float x[4] = {o[tt][v], o[tt][v + 1], o[tt][v + 2], o[tt][v + 3]};
-          store4(to + tt * 32 + 2 * v, x, f);
-        }
-      if (it.rec >= 0 && h == 0) R.ml[at] = make_float2(m_run, l_run);
-    }
-  }
-  __syncthreads();
-  for (int i = 0; i < 4; i++)
-    for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u)
-      plain_piece<float, float, DH>(A, it, R, g, i * 32 + __builtin_ctz(m), (float*)lds);
+  finish_wide<float, float, DH, kWG>(A, it, R, g, o, m_run, l_run, lim, lds);
 }
 
-// The piece of a call without a plan: a tile of at most 16 queries, or a decode row, over all its keys.
+// The piece of a call without a plan: a tile of at most 16 queries, or (no cu) a decode row, over all its keys.
 __device__ __forceinline__ bool direct_item(const SeqArgs& A, int y, Item& it) {
   it.k0 = 0;
   it.rec = -1;
@@ -1357,12 +1338,13 @@ struct Request {
 Request request(const spd_cache& c, int n_q_heads, int nseqs, int rows, int ngroups, int max_len, bool prefix) {
   Request q{};
   const int hkv = c.n_kv_heads, G = n_q_heads / hkv;
-  // Short calls that the GPU holds at once go without a plan, one launch: prompts whose tiles of 16 queries are at most two a
-  // CU, decode rows that share nothing. 63 fp32 rows of up to 65 keys: 9.0 us against 17.4 with plan and tiles of 128
-  // queries; 64 bf16 rows of 512 keys each: 14 us against 19. Longer ones need the splits, larger ones the wide tiles.
+  // Short calls go without a plan, one launch, every piece of at most 16 queries over all its keys: prompts whose tiles are at
+  // most two a CU, decode rows (a shared prefix of so few keys is in the L2 for all of a group that the GPU holds at once). Planned and
+  // so: 3 fp32 prompts of 21 rows 13.7 and 5.1 us, 4 bf16 prompts of 16 rows behind 300 keys 16.7 and 9.2, decode rows of
+  // 300 keys 16.8 and 8.2, 256 of 512 keys 90 and 84. Longer calls need the splits, larger prompts the wide tiles.
   const bool fits = max_len > 0 && max_len <= 512;
   q.rpt = 16 / G;
-  q.direct = fits && (prefix ? ngroups == 0 && nseqs * hkv <= 2048 : ((long long)rows / q.rpt + nseqs) * hkv <= 512);
+  q.direct = fits && (prefix ? nseqs * hkv <= (ngroups > 0 ? 512 : 2048) : ((long long)rows / q.rpt + nseqs) * hkv <= 512);
   if (q.direct) {
     q.jobs = prefix ? nseqs : rows / q.rpt + nseqs;
     return q;
@@ -1423,6 +1405,7 @@ void launch(const SeqArgs& a, const Request& q, const PlanArgs& p, const Records
 // Plan, pieces, merge; or the pieces alone.
 void run_attention(SeqArgs a, int dtype, const Request& q, bool prefix, void* workspace, hipStream_t s) {
   a.rpt = q.rpt;
+  if (q.direct && prefix) a.cu = nullptr;
   char* ws = (char*)workspace;
   PlanArgs p{};
   p.c = a.c;

@@ -109,6 +109,13 @@ def filled(lens, hkv, dh, dtype, seed, layers=1, spare=3, extra_pages=0, stale=f
     return PagedCache(kv.cuda(), table.cuda(), i32(list(lens)), refs.cuda()), rows
 
 
+def agree(cache, first, other, n):
+    """The first n keys and values of sequence `other` become those of `first`."""
+    j = torch.arange(n, device="cuda")
+    a, b = cache.page_table[first, j // PAGE].long(), cache.page_table[other, j // PAGE].long()
+    cache.kv[:, b, :, :, j % PAGE] = cache.kv[:, a, :, :, j % PAGE]
+
+
 def attend(q, k, v, limits):
     """q [n][heads][dh] over k, v [KV heads][len][dh], row i the first limits[i] keys: outputs in 64 bits, and
     sum p |v|, which scales the error of rounded probabilities."""

@@ -94,14 +94,17 @@ def test_batches_of_many_rows(heads, rows, cached):
 
 
 def run_prefix(groups, prefix, lens, heads, types, seed=0, max_len=0, pad=0, use_groups=True):
-    """Groups of rows that agree in their first prefix keys (in pages of their own: only the first row's are read)."""
-    from tests.seqcache import attend, check, filled, i32
+    """Groups of rows that agree in their first prefix keys, in pages of their own."""
+    from tests.seqcache import agree, attend, check, filled, i32
     hq, hkv, dh = heads
     n = len(lens)
     cache, kv = filled(lens, hkv, dh, dt(types[1]), seed)
     cu = [0]
     for r in groups:
         cu.append(cu[-1] + r)
+    for j in range(len(groups)):
+        for i in range(cu[j] + 1, cu[j + 1]):
+            agree(cache, cu[j], i, min(prefix[j], lens[cu[j]], lens[i]))
     g = torch.Generator().manual_seed(seed + 1)
     wide = (1.5 * torch.randn(n, hq * dh + pad, generator=g)).to(dt(types[0])).cuda()
     q = wide[:, :hq * dh].unflatten(1, (hq, dh))
@@ -137,6 +140,13 @@ def test_rows_without_keys_and_prefixes_of_any_length(types):
 def test_long_prefix(types, max_len):
     run_prefix([21, 40], [2500, 777], [2500 + 7 * i for i in range(21)] + [777 + 13 * i for i in range(40)], (8, 2, 128), types,
                seed=5, max_len=max_len)
+
+
+@pytest.mark.parametrize("types", TYPES, ids="-".join)
+@pytest.mark.parametrize("heads", [(8, 2, 128), (4, 4, 64)], ids=str)
+def test_short_shared_prefixes(heads, types):
+    for max_len in (100, 512):
+        run_prefix([3, 1, 2], [37, 9, 64], [40, 99, 37, 20, 70, 65], heads, types, seed=9, max_len=max_len)
 
 
 @pytest.mark.parametrize("types", TYPES, ids="-".join)

@@ -73,11 +73,13 @@ def test_more_sequences_than_the_plan_keeps():
 
 def test_more_groups_than_the_plan_keeps():
     """2048 groups of two rows: more tiles than the 1024 whose records the plan holds in LDS."""
-    from tests.seqcache import attend, check, i32
+    from tests.seqcache import agree, attend, check, i32
     n, hq, hkv, dh = 4096, 2, 1, 64
     cache, lens = small_cache(n, 60, hkv, dh, 5)
     rng = random.Random(6)
     prefix = [rng.choice([0, 1, 16, 20, 48, 70]) for _ in range(n // 2)]
+    for j, p in enumerate(prefix):
+        agree(cache, 2 * j, 2 * j + 1, min(p, lens[2 * j], lens[2 * j + 1]))
     q = (1.5 * torch.randn(n, hq, dh, device="cuda")).bfloat16()
     out = cache.prefix_attention(0, q, i32(list(range(n))), i32(list(range(0, n + 1, 2))), i32(prefix))
     assert torch.isfinite(out).all()
