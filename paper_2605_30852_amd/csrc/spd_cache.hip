@@ -289,8 +289,10 @@ __global__ __launch_bounds__(kWG) void k_apply_fork(spd_cache c, const int* src,
   if (threadIdx.x == 0) c.lens[dst[i]] = keep[i];
 }
 
-// Grid: x = sequence. What refuses the call is in its arguments, which nothing changes, so every workgroup checks them all
-// and no launch has to come before.
+// Grid: x = sequence (strided). What refuses the call is in its arguments, which nothing changes, so every workgroup checks
+// them all and no launch has to come before. That is n entries a workgroup, so there are at most kTruncateWGs of them: 4096
+// sequences take 15.6, 13.7 and 19.3 us with 256, 512 and 1024, 65536 sequences 0.18 ms with 512 and 14 ms with one each.
+constexpr int kTruncateWGs = 512;
 __global__ __launch_bounds__(kWG) void k_truncate(spd_cache c, const int* seqs, const int* keep, int n, int* status) {
   __shared__ uint32_t bits[kMaxSeqs / 32];
   __shared__ int s_status;
@@ -298,6 +300,7 @@ __global__ __launch_bounds__(kWG) void k_truncate(spd_cache c, const int* seqs, 
   if (threadIdx.x == 0) s_status = SPD_CACHE_DONE;
   __syncthreads();
   const Named named{bits};
+#pragma unroll 4
   for (int i = threadIdx.x; i < n; i += kWG) {
     const int s = seqs[i];
     const int bad = (unsigned)s >= (unsigned)c.max_seqs || !named.first(s) ? SPD_CACHE_BAD_SEQ : keep[i] < 0 ? SPD_CACHE_BAD_LEN : 0;
@@ -306,16 +309,18 @@ __global__ __launch_bounds__(kWG) void k_truncate(spd_cache c, const int* seqs, 
   __syncthreads();
   if (blockIdx.x == 0 && threadIdx.x == 0) *status = s_status;
   if (s_status != SPD_CACHE_DONE) return;
-  const int s = seqs[blockIdx.x], len = seq_len(c, s), k = min(keep[blockIdx.x], len), end = pages_of(len);
-  int* row = c.page_table + (size_t)s * c.max_pages;
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int s = seqs[i], len = seq_len(c, s), k = min(keep[i], len), end = pages_of(len);
+    int* row = c.page_table + (size_t)s * c.max_pages;
 #pragma unroll 4
-  for (int j = pages_of(k) + threadIdx.x; j < end; j += kWG) {
-    const int p = row[j];
-    row[j] = -1;
-    if ((unsigned)p < (unsigned)c.num_pages) atomicSub(&c.refs[p], 1);
+    for (int j = pages_of(k) + threadIdx.x; j < end; j += kWG) {
+      const int p = row[j];
+      row[j] = -1;
+      if ((unsigned)p < (unsigned)c.num_pages) atomicSub(&c.refs[p], 1);
+    }
+    __syncthreads();  // every wave has read the length
+    if (threadIdx.x == 0) c.lens[s] = k;
   }
-  __syncthreads();  // every wave has read the length
-  if (threadIdx.x == 0) c.lens[s] = k;
 }
 
 // Held pages are counted (n), then those at n and above and the holes below n are listed, in order: as many of each.
@@ -516,7 +521,7 @@ extern "C" spd_status spd_cache_truncate(const spd_cache* c, const int32_t* seqs
                                          int32_t* status, void* workspace, size_t ws_bytes, void* stream) {
   const spd_status st = check_change("cache truncate", c, {seqs, keep, status}, n, workspace, ws_bytes);
   if (st != SPD_OK) return st;
-  hipLaunchKernelGGL(k_truncate, dim3(n), dim3(kWG), 0, (hipStream_t)stream, *c, seqs, keep, n, status);
+  hipLaunchKernelGGL(k_truncate, dim3(std::min(n, kTruncateWGs)), dim3(kWG), 0, (hipStream_t)stream, *c, seqs, keep, n, status);
   return check_launch("cache truncate");
 }
 
