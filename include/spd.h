@@ -379,7 +379,7 @@ spd_status spd_decode_attention_noalloc(const float* q, const void* kv, const in
  * SPD_E_HIP if the launch fails; spd_last_error(NULL) has the message). What only the device knows is kept in
  * bounds there: a length counts as at most 16 * max_pages and at least 0, a page id outside [0, num_pages) is read as
  * page 0 and never written to, and a sequence index outside [0, max_seqs) has no rows.
- * The workspaces of calls that may run at the same time must differ. */
+ * The workspaces of calls that may run at the same time must differ, and no array of a call overlaps the cache's. */
 typedef struct spd_cache {
   void* kv;              /* device, [n_layers][num_pages][K, V][n_kv_heads][16 keys][head_dim], 16-byte aligned */
   int32_t* page_table;   /* device [max_seqs][max_pages] */
@@ -448,7 +448,8 @@ spd_status spd_cache_append(const spd_cache* c, int32_t layer, const void* k, in
  * the row of key p attends keys 0 .. p of its sequence, query head h reads KV head h / (n_q_heads / n_kv_heads),
  * scores are scaled by 1 / sqrt(head_dim). A row that would stand for a key before the first attends nothing: zeros.
  *   q, out: device [rows] of n_q_heads * head_dim elements of dtype, rows q_stride and out_stride elements apart
- *     (16-byte aligned, strides multiples of 16 bytes). dtype SPD_F32 with any cache, SPD_BF16 with a bf16 cache.
+ *     (16-byte aligned, strides multiples of 16 bytes; no element of out is one of q). dtype SPD_F32 with any cache,
+ *     SPD_BF16 with a bf16 cache.
  *   max_len (host): the keys of the longest sequence, for the choice of key splits (0: 16 * max_pages). The result
  *     is right for any value, if not always in the same order of sums.
  *   workspace: device, 256-byte aligned, of spd_prompt_attention_workspace(the same sizes).

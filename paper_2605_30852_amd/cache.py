@@ -128,7 +128,8 @@ class PagedCache:
             if cu_groups is None or prefix_lens is None:
                 raise ValueError("cu_groups and prefix_lens come together")
             ng = self._batch(prefix_lens, cu_groups)
-            cg, pl = cu_groups.data_ptr(), prefix_lens.data_ptr()
+            if ng:
+                cg, pl = cu_groups.data_ptr(), prefix_lens.data_ptr()
         dt = _DTYPES[q.dtype]
         wb = self._bytes(("prefix", hq, dt, n, ng, max_len), B.spd_prefix_attention_workspace)
         ws, wp = self._workspace(wb)
@@ -164,7 +165,7 @@ class PagedCache:
                 dtype not in _DTYPES or t.device != self.device:
             raise ValueError(f"{name} must be [{rows} rows][{heads} heads][{dh}] of {dtype} (float32 or bfloat16) on the "
                              "cache's device, the heads of a row one after the other")
-        return st[0] if rows > 1 else max(st[0], heads * dh)
+        return st[0] if rows > 1 else heads * dh
 
     def _query(self, q: torch.Tensor, rows: int, out: Optional[torch.Tensor]):
         hq = q.shape[1] if q.dim() == 3 else 0

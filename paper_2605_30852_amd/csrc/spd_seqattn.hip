@@ -22,22 +22,22 @@ struct SeqArgs {
   const int* seqs;
   const int* cu;      // prompts: cu_rows; decode rows: cu_groups
   const int* prefix;  // decode rows: prefix_lens
-  int hq, G, nseqs, rows, ngroups, rpt;
+  int G, nseqs, rows, ngroups, rpt;
   float scale;
 };
 
 // A query over the keys [k0, k1) in plain fp32, by the whole workgroup, which a query, key or value that is not finite
-// needs: there 0 times a value behind the query's own keys, or a plane's 0 * inf, is NaN on matrix cores. Scores in passes of a key a thread, computed twice
-// rather than kept. M, L and a (dims 4 d4 .. + 3 of thread d4 = tid % (DH / 4)) are the maximum, the sum and the
-// output; true in the threads that hold them. lds: NTH * 6 floats.
-template <typename T, typename KVT, int DH, int NTH>
+// needs: there 0 times a value behind the query's own keys, or a plane's 0 * inf, is NaN on matrix cores. Scores in passes of
+// a key a thread, computed twice rather than kept. M, L and a (dims 4 d4 .. + 3 of thread d4 = tid % (DH / 4)) are the
+// maximum, the sum and the output; true in the threads that hold them. lds: 6 * kWG floats.
+template <typename T, typename KVT, int DH>
 __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* table, int g, const T* q, float scale, int k0,
                             int k1, float* lds, float& M, float& L, float (&a)[4]) {
-  constexpr int TPQ = DH / 4, NG = NTH / TPQ, NW = NTH / 64;
+  constexpr int TPQ = DH / 4, NG = kWG / TPQ, NW = kWG / 64;
   const int tid = threadIdx.x, d4 = tid % TPQ, grp = tid / TPQ;
   const size_t half = (size_t)c.n_kv_heads * kPage * DH;
   float* sp = lds;
-  float* sr = lds + NTH;
+  float* sr = lds + kWG;
   auto row = [&](int key) { return pool + page_to_read(c, table[key / kPage]) * 2 * half + (size_t)(g * kPage + key % kPage) * DH; };
   auto score = [&](int key) {
     const KVT* k = row(key);
@@ -54,7 +54,7 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
   };
   float m = -INFINITY;
   bool sound = true;
-  for (int key = k0 + tid; key < k1; key += NTH) {
+  for (int key = k0 + tid; key < k1; key += kWG) {
     const float s = score(key);
     m = fmaxf(m, s);
     sound = sound && s < INFINITY;
@@ -81,7 +81,7 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
     return grp == 0;
   }
   L = a[0] = a[1] = a[2] = a[3] = 0.f;
-  for (int base = k0; base < k1; base += NTH) {
+  for (int base = k0; base < k1; base += kWG) {
     float p = 0.f;
     if (base + tid < k1) {
       const float s = score(base + tid);
@@ -89,7 +89,7 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
     }
     sp[tid] = p;
     __syncthreads();
-    const int n = min(NTH, k1 - base);
+    const int n = min(kWG, k1 - base);
     for (int i = grp; i < n; i += NG) {
       const KVT* v = row(base + i) + half + 4 * d4;
       const float2 v0 = ld2<KVT>(v), v1 = ld2<KVT>(v + 2);
@@ -534,14 +534,14 @@ __device__ __forceinline__ int row_limit(const SeqArgs& A, const Item& it, int r
 }
 
 // Query j of a piece again, in plain arithmetic, in the place of its result.
-template <typename T, typename KVT, int DH, int NTH = kWG>
+template <typename T, typename KVT, int DH>
 __device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, int g, int j, float* lds) {
   const int r = it.row0 + j / A.G, head = g * A.G + j % A.G, d = 4 * (threadIdx.x % (DH / 4));
   const int n = min(row_limit(A, it, r), it.k1);
   float a[4] = {0.f, 0.f, 0.f, 0.f}, M = -INFINITY, L = 0.f;
   bool holds = threadIdx.x < DH / 4;
   if (n > it.k0)
-    holds = plain_query<T, KVT, DH, NTH>(A.c, (const KVT*)A.kv, A.c.page_table + (size_t)it.table * A.c.max_pages, g,
+    holds = plain_query<T, KVT, DH>(A.c, (const KVT*)A.kv, A.c.page_table + (size_t)it.table * A.c.max_pages, g,
                                     (const T*)A.q + r * A.qs + head * DH, A.scale, it.k0, n, lds, M, L, a);
   if (!holds) return;
   if (it.rec < 0) {
@@ -555,7 +555,7 @@ __device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, 
 
 // The end of a piece of 32 queries a wave: registers 4 v .. + 3 of tile t are dims 32 t + 8 v + 4 h .. + 3 of the lane's query, which
 // attends keys below lim.
-template <typename T, typename KVT, int DH, int NTH>
+template <typename T, typename KVT, int DH>
 __device__ void finish_wide(const SeqArgs& A, const Item& it, const Records R, int g, const f32x16 (&o)[DH / 32], float m_run,
                             float l_run, int lim, char* lds) {
   constexpr int NT = DH / 32;
@@ -564,8 +564,8 @@ __device__ void finish_wide(const SeqArgs& A, const Item& it, const Records R, i
   const bool active = w * 32 < nq, mine = jq < nq;
   l_run += __shfl_xor(l_run, 32, 64);
 
-  __shared__ uint32_t s_bad[NTH / 64];  // queries whose result here is not a number
-  if (tid < NTH / 64) s_bad[tid] = 0u;
+  __shared__ uint32_t s_bad[kWG / 64];  // queries whose result here is not a number
+  if (tid < kWG / 64) s_bad[tid] = 0u;
   __syncthreads();
   if (active) {
     bool bad = !(l_run > 0.f) && lim > it.k0;  // NaN, or nothing but scores of -inf
@@ -593,9 +593,9 @@ __device__ void finish_wide(const SeqArgs& A, const Item& it, const Records R, i
     }
   }
   __syncthreads();  // every result is stored, and the tiles are free
-  for (int i = 0; i < NTH / 64; i++)
+  for (int i = 0; i < kWG / 64; i++)
     for (uint32_t m = __builtin_amdgcn_readfirstlane(s_bad[i]); m != 0u; m &= m - 1u)
-      plain_piece<T, KVT, DH, NTH>(A, it, R, g, i * 32 + __builtin_ctz(m), (float*)lds);
+      plain_piece<T, KVT, DH>(A, it, R, g, i * 32 + __builtin_ctz(m), (float*)lds);
 }
 
 // A piece of bf16 keys for 32 queries a wave. Query j of the tile is row row0 + j / G, head g * G + j % G.
@@ -795,7 +795,7 @@ __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, in
             o[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x][ks][tt], pf[p].f[ks], o[tt], 0, 0, 0);
     }
   }
-  finish_wide<T, uint16_t, DH, kWG>(A, it, R, g, o, m_run, l_run, lim, lds);
+  finish_wide<T, uint16_t, DH>(A, it, R, g, o, m_run, l_run, lim, lds);
 }
 
 // The end of a piece of few queries: lane l holds dims 16 t + 4 (l / 16) .. + 3 of query l % 16, over its wave's keys. The waves' sums
@@ -1198,7 +1198,7 @@ __device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, int
       }
     }
   }
-  finish_wide<float, float, DH, kWG>(A, it, R, g, o, m_run, l_run, lim, lds);
+  finish_wide<float, float, DH>(A, it, R, g, o, m_run, l_run, lim, lds);
 }
 
 // The piece of a call without a plan: a tile of at most 16 queries, or (no cu) a decode row, over all its keys.
@@ -1461,6 +1461,7 @@ spd_status check_call(const char* call, const spd_cache* c, int layer, const voi
   spd_status st = check_rows(call, q, q_stride, n_q_heads, c->head_dim, dtype);
   if (st == SPD_OK) st = check_rows(call, out, out_stride, n_q_heads, c->head_dim, dtype);
   if (st != SPD_OK) return st;
+  if (q == out) return invalid(call, "out must not be q");
   if (layer < 0 || layer >= c->n_layers) return invalid(call, "no such layer");
   if (!seqs || misaligned(seqs, 4)) return invalid(call, "NULL or misaligned pointer");
   return SPD_OK;
@@ -1476,7 +1477,6 @@ SeqArgs args_of(const spd_cache* c, int layer, const void* q, int64_t q_stride, 
   a.qs = q_stride;
   a.os = out_stride;
   a.seqs = seqs;
-  a.hq = n_q_heads;
   a.G = n_q_heads / c->n_kv_heads;
   a.nseqs = nseqs;
   a.scale = (float)(1.0 / std::sqrt((double)c->head_dim));

@@ -129,3 +129,8 @@ def test_null_outputs():
     assert B.lib().spd_prompt_attention_workspace(ct.byref(c), 8, B.SPD_BF16, 1, 1, 0, None) == B.SPD_E_INVAL
     assert B.lib().spd_prefix_attention_workspace(ct.byref(c), 8, B.SPD_BF16, 1, 0, 0, None) == B.SPD_E_INVAL
     assert B.lib().spd_cache_reserve(None, 4, 8, 1, 12, 256, BIG, 0) == B.SPD_E_INVAL
+
+
+def test_attention_in_place():
+    for call in (prompt, prefix):
+        refused(call, q=32, out=32)

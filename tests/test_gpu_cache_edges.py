@@ -25,3 +25,56 @@ def test_truncate_of_more_sequences_than_workgroups():
     bad = keep[:-1] + [-1]
     same(c, m, kv0, c.truncate(i32(seqs), i32(bad)), m.truncate(seqs, bad), "a length")
     same(c, m, kv0, c.truncate(i32(seqs), i32(keep)), m.truncate(seqs, keep), "cut")
+
+
+def test_an_empty_list_of_groups():
+    from tests.seqcache import filled, i32
+    c, _ = filled([40, 7], 2, 64, torch.bfloat16, 1)
+    q = torch.randn(2, 4, 64, device="cuda").bfloat16()
+    for max_len in (0, 40):
+        want = c.prefix_attention(0, q, i32([0, 1]), max_len=max_len)
+        got = c.prefix_attention(0, q, i32([0, 1]), i32([0]), i32([]), max_len=max_len)
+        assert torch.equal(got, want)
+
+
+def test_one_row_of_any_stride():
+    from tests.seqcache import filled, i32
+    c, _ = filled([40], 2, 64, torch.bfloat16, 1)
+    q = torch.randn(4 * 64, device="cuda").bfloat16()
+    want = c.prompt_attention(0, q.view(1, 4, 64), i32([0]), i32([0, 1]))
+    for stride in (1, 4 * 64 + 1):
+        got = c.prompt_attention(0, q.as_strided((1, 4, 64), (stride, 64, 1)), i32([0]), i32([0, 1]))
+        assert torch.equal(got, want)
+
+
+def test_the_output_is_not_the_input():
+    from paper_2605_30852_amd import binding as B
+    from tests.seqcache import filled, i32
+    c, _ = filled([40], 2, 64, torch.bfloat16, 1)
+    q = torch.randn(1, 4, 64, device="cuda").bfloat16()
+    keep = q.clone()
+    for max_len in (0, 40):
+        with pytest.raises(B.SPDError, match="out must not be q"):
+            c.prompt_attention(0, q, i32([0]), i32([0, 1]), out=q, max_len=max_len)
+        with pytest.raises(B.SPDError, match="out must not be q"):
+            c.prefix_attention(0, q, i32([0]), out=q, max_len=max_len)
+    assert torch.equal(q, keep)
+
+
+@pytest.mark.parametrize("max_len", [0, 300])
+def test_a_sequence_named_twice_is_read_twice(max_len):
+    from tests.seqcache import filled, i32
+    c, _ = filled([300, 20], 2, 128, torch.float32, 2)
+    q = torch.randn(33, 6, 128, device="cuda")
+    out = c.prompt_attention(0, torch.cat((q, q[:5], q)), i32([0, 1, 0]), i32([0, 33, 38, 71]), max_len=max_len)
+    assert torch.equal(out[:33], out[38:])
+    rows = c.prefix_attention(0, torch.cat((q[:1], q[:1], q[:1])), i32([0, 0, 0]), i32([0, 3]), i32([300]), max_len=max_len)
+    assert torch.equal(rows[0], rows[1]) and torch.equal(rows[0], rows[2])
+
+
+@pytest.mark.parametrize("types", [("bf16", "bf16"), ("f32", "f32")], ids="-".join)
+def test_hundreds_of_kv_heads(types):
+    from tests.test_gpu_seq_attention import run_prefix, run_prompt
+    heads = (600, 600, 64)
+    run_prompt([3, 20], [300, 1], heads, types, seed=6)
+    run_prefix([3, 1], [290, 0], [300, 291, 310, 5], heads, types, seed=6)
