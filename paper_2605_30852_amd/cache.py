@@ -29,6 +29,7 @@ class PagedCache:
             raise ValueError("kv must be contiguous, on a GPU")
         self.kv, self.page_table, self.lens, self.refs = kv, page_table, lens, refs
         self.device = kv.device
+        self._gpu = kv.get_device()
         self.n_layers, self.num_pages, _, self.n_kv_heads, _, self.head_dim = kv.shape
         self._index("page_table", page_table, 2)
         self.max_seqs, self.max_pages = page_table.shape
@@ -84,18 +85,19 @@ class PagedCache:
             hq = q.shape[1] if q.dim() == 3 else 0
             qs = self._rows("q", q, rows, k.dtype, hq)
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            os_ = self._rows("q_out", q_out, rows, k.dtype, hq)
+                q_out, os_ = torch.empty(q.shape, dtype=q.dtype, device=self.device), hq * self.head_dim
+            else:
+                os_ = self._rows("q_out", q_out, rows, k.dtype, hq)
             qp, op = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             raise ValueError("q_out without q")
         cos = sin = places = 0
         if rope is not None:
+            places, half = rope[0].shape[0], self.head_dim // 2
             for x in rope:
-                if x.dtype != torch.float32 or x.device != self.device or not x.is_contiguous() or x.shape != rope[0].shape \
-                        or x.dim() != 2 or x.shape[1] != self.head_dim // 2:
+                if x.dtype is not torch.float32 or x.shape != (places, half) or x.get_device() != self._gpu or not x.is_contiguous():
                     raise ValueError("rope must be two contiguous float32 tensors [positions][head_dim / 2] on the cache's device")
-            cos, sin, places = rope[0].data_ptr(), rope[1].data_ptr(), rope[0].shape[0]
+            cos, sin = rope[0].data_ptr(), rope[1].data_ptr()
         if rows:
             self._on_device(lambda s: B.spd_cache_append(self.c, layer, k.data_ptr(), ks, v.data_ptr(), vs, qp, qs, op, os_, hq,
                                                          _DTYPES[k.dtype], cos, sin, places, seqs.data_ptr(), cu_rows.data_ptr(),
@@ -139,7 +141,7 @@ class PagedCache:
 
     # ------------------------------------------------------------------------------------------------ marshalling
     def _index(self, name: str, t: torch.Tensor, dim: int = 1, size: Optional[int] = None) -> None:
-        if t.dtype is not torch.int32 or t.dim() != dim or t.device != self.device or not t.is_contiguous() or \
+        if t.dtype is not torch.int32 or t.get_device() != self._gpu or t.dim() != dim or not t.is_contiguous() or \
                 (size is not None and t.shape[0] != size):
             raise ValueError(f"{name} must be a contiguous int32 tensor of {dim} dimension(s)"
                              + (f" and {size} entries" if size is not None else "") + " on the cache's device")
@@ -160,9 +162,11 @@ class PagedCache:
     def _rows(self, name: str, t: torch.Tensor, rows: int, dtype: torch.dtype, heads: int) -> int:
         """The stride between the rows of [rows][heads][head_dim]."""
         dh = self.head_dim
-        st = t.stride()
-        if t.shape != (rows, heads, dh) or (heads > 1 and st[1] != dh) or st[2] != 1 or t.dtype is not dtype or \
-                dtype not in _DTYPES or t.device != self.device:
+        if t.dtype is not dtype or t.shape != (rows, heads, dh) or t.get_device() != self._gpu or dtype not in _DTYPES:
+            st = None
+        else:
+            st = t.stride()
+        if st is None or st[2] != 1 or (heads > 1 and st[1] != dh):
             raise ValueError(f"{name} must be [{rows} rows][{heads} heads][{dh}] of {dtype} (float32 or bfloat16) on the "
                              "cache's device, the heads of a row one after the other")
         return st[0] if rows > 1 else heads * dh
@@ -185,6 +189,8 @@ class PagedCache:
     def _workspace(self, nbytes: int):
         """Of the current stream's pool, whose blocks are 512-byte aligned; free again when the call has returned, as the stream orders
         its next user behind it."""
+        if nbytes == 0:
+            return None, 0
         ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         return ws, ws.data_ptr()
 
@@ -198,7 +204,7 @@ class PagedCache:
     def _on_device(self, call) -> None:
         """call(stream) with the cache's device current: the library launches on the current one. (The raw stream is
         torch.cuda.current_stream().cuda_stream without the object, 2 us less a call.)"""
-        i = self.device.index
+        i = self._gpu
         if torch._C._cuda_getDevice() == i:
             call(torch._C._cuda_getCurrentRawStream(i))
         else:
