@@ -140,7 +140,7 @@ struct Item {
   int lim0;         // causal: row row0 + i attends keys below lim0 + i
   int mode;
 };
-enum { ITEM_FEW = 1, ITEM_FLAT = 2 };  // at most 16 queries; each row attends its sequence's keys
+enum { ITEM_FEW = 1, ITEM_PAIR = 2, ITEM_FLAT = 4 };  // at most 16 queries; at most 32 (of an fp32 cache); each row attends its sequence's keys
 
 // Rows whose pieces' records are to be joined: those of up to two jobs.
 struct Merge {
@@ -167,7 +167,8 @@ struct PlanArgs {
   int nseqs, rows, ngroups, G, wanted;  // wanted: pieces of a KV head; 0: no job is split
   int rpt;                              // rows of a tile
   int tiles, jobs;
-  int wide_cost;                        // of a key of a wide piece; 1: of one of few queries
+  int pair;                             // an fp32 cache: pieces of up to 32 queries
+  int wide_cost;                        // of a key of a wide piece; 1: of one of few queries, 2: of a pair
   int qpu;                              // queries of a merge's workgroup
   unsigned long long records;           // room for them
   int* count;                           // items, units
@@ -219,6 +220,10 @@ struct Batch {
   }
 };
 
+__device__ __forceinline__ int size_mode(const PlanArgs& P, int nq) {
+  return nq <= 16 ? ITEM_FEW : P.pair && nq <= 32 ? ITEM_PAIR : 0;
+}
+
 // Job t of a prompt call: a tile of a sequence's rows.
 __device__ bool prompt_job(const PlanArgs& P, const Batch& B, int t, Job& j) {
   const int i = B.of_tile(P.nseqs, t);
@@ -232,7 +237,7 @@ __device__ bool prompt_job(const PlanArgs& P, const Batch& B, int t, Job& j) {
   j.a = 0;
   j.lim0 = (int)max((long long)len - stop + j.row0 + 1, -(1ll << 30));
   j.b = max(0, j.lim0 + j.nrows - 1);
-  j.mode = j.nrows * P.G <= 16 ? ITEM_FEW : 0;
+  j.mode = size_mode(P, j.nrows * P.G);
   return true;
 }
 
@@ -260,7 +265,7 @@ __device__ bool prefix_job(const PlanArgs& P, const Batch& B, int t, Job& j, boo
     j.nrows = min(P.rpt, rows - (int)at);
     j.table = B.seq_at(first);
     j.b = n;
-    j.mode = ITEM_FLAT | (j.nrows * P.G <= 16 ? ITEM_FEW : 0);
+    j.mode = ITEM_FLAT | size_mode(P, j.nrows * P.G);
     shared = true;
     return true;
   }
@@ -340,7 +345,7 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
       if (k.is) f(t, k);
     }
   };
-  auto cost = [&](int keys, int mode) { return (unsigned long long)keys * (mode & ITEM_FEW ? 1 : P.wide_cost); };
+  auto cost = [&](int keys, int mode) { return (unsigned long long)keys * (mode & ITEM_FEW ? 1 : mode & ITEM_PAIR ? 2 : P.wide_cost); };
   {
     unsigned long long sum = 0ull, longest = 1ull;
     each([&](int, const Known& k) {
@@ -360,9 +365,10 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
   const bool split = P.wanted > 0 && s_max * (unsigned)max(P.wanted / 2, 1) > s_total;
   const unsigned long long share = split ? min((s_total + P.wanted - 1) / P.wanted, s_max) : s_max;
   const int chunk_few = max(kMinChunk, (int)((min(share, 1ull << 30) + 63) / 64 * 64));
+  const int chunk_pair = max(kMinChunk / 2, (int)((min(share / 2, 1ull << 30) + 64) / 64 * 64));
   const int chunk_wide = max(kMinChunk / 2, (int)((min(share / P.wide_cost, 1ull << 30) + 64) / 64 * 64));
-  auto chunk_of = [&](const Known& k) { return k.j.mode & ITEM_FEW ? chunk_few : chunk_wide; };
-  const float per_cost = (float)(kBuckets - 1) / (float)max(cost(chunk_few, ITEM_FEW), cost(chunk_wide, 0));
+  auto chunk_of = [&](const Known& k) { return k.j.mode & ITEM_FEW ? chunk_few : k.j.mode & ITEM_PAIR ? chunk_pair : chunk_wide; };
+  const float per_cost = (float)(kBuckets - 1) / (float)max(max(cost(chunk_few, ITEM_FEW), cost(chunk_pair, ITEM_PAIR)), cost(chunk_wide, 0));
   auto bucket = [&](int keys, int mode) {  // the costliest first
     return kBuckets - 1 - min((int)((float)cost(keys, mode) * per_cost), kBuckets - 1);
   };
@@ -798,27 +804,30 @@ __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, in
   finish_wide<T, uint16_t, DH>(A, it, R, g, o, m_run, l_run, lim, lds);
 }
 
-// The end of a piece of few queries: lane l holds dims 16 t + 4 (l / 16) .. + 3 of query l % 16, over its wave's keys. The waves' sums
-// are joined in wave order and written.
-template <typename T, typename KVT, int DH>
-__device__ void finish_few(const SeqArgs& A, const Item& it, const Records R, int g, const f32x4 (&o)[DH / 16], float m_run,
-                           float l_run, char* lds) {
-  constexpr int NW = kWG / 64, NT = DH / 16;
+// The end of a piece of few queries: lane l holds dims 16 t + 4 (l / 16) .. + 3 of queries l % 16 + 16 x, over its wave's keys. The
+// waves' sums are joined in wave order and written.
+template <typename T, typename KVT, int DH, int QS>
+__device__ void finish_few(const SeqArgs& A, const Item& it, const Records R, int g, const f32x4 (&o)[QS][DH / 16],
+                           const float (&m_run)[QS], const float (&l_run)[QS], char* lds) {
+  constexpr int NW = kWG / 64, NT = DH / 16, NQ = 16 * QS;
   const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, col = lane & 15, q4 = lane >> 4;
   const int G = A.G, nq = it.nrows * G;
-  l_run += __shfl_xor(l_run, 16, 64);
-  l_run += __shfl_xor(l_run, 32, 64);
-
-  // The waves' sums, in wave order.
-  __shared__ float2 s_ml[NW][16];
+  __shared__ float2 s_ml[NW][NQ];
   __shared__ uint32_t s_few_bad;
   if (tid == 0) s_few_bad = 0u;
   __syncthreads();  // every wave is done with its tile
   float* ow = (float*)lds;  // [wave][query][dim]
 #pragma unroll
-  for (int tt = 0; tt < NT; tt++)
-    *reinterpret_cast<float4*>(ow + (w * 16 + col) * DH + tt * 16 + q4 * 4) = make_float4(o[tt][0], o[tt][1], o[tt][2], o[tt][3]);
-  if (q4 == 0) s_ml[w][col] = make_float2(m_run, l_run);
+  for (int x = 0; x < QS; x++) {
+    float l = l_run[x];
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+#pragma unroll
+    for (int tt = 0; tt < NT; tt++)
+      *reinterpret_cast<float4*>(ow + (w * NQ + x * 16 + col) * DH + tt * 16 + q4 * 4) =
+          make_float4(o[x][tt][0], o[x][tt][1], o[x][tt][2], o[x][tt][3]);
+    if (q4 == 0) s_ml[w][x * 16 + col] = make_float2(m_run[x], l);
+  }
   __syncthreads();
   for (int i = tid; i < nq * (DH / 4); i += kWG) {
     const int j = i / (DH / 4), d = i % (DH / 4) * 4, r = it.row0 + j / G, hd = g * G + j % G;
@@ -830,7 +839,7 @@ __device__ void finish_few(const SeqArgs& A, const Item& it, const Records R, in
     for (int x = 0; x < NW; x++) {
       const float2 ml = s_ml[x][j];
       const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-      const float4 v = *reinterpret_cast<const float4*>(ow + (x * 16 + j) * DH + d);
+      const float4 v = *reinterpret_cast<const float4*>(ow + (x * NQ + j) * DH + d);
       L = fmaf(ml.y, f, L);
       a[0] = fmaf(v.x, f, a[0]);
       a[1] = fmaf(v.y, f, a[1]);
@@ -917,10 +926,10 @@ __device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, int
     const int k = q4 * 4 + col / 4, c = tt * 2 + (lane & 3) / 2;
     va[tt] = k * DH * 2 + ((c ^ (k & 7) >> VROT << 1) << 4) + (lane & 1) * 8;
   }
-  f32x4 o[NT];
+  f32x4 o[1][NT];
 #pragma unroll
-  for (int t = 0; t < NT; t++) o[t] = (f32x4)(0.f);
-  float m_run = -INFINITY, l_run = 0.f;
+  for (int t = 0; t < NT; t++) o[0][t] = (f32x4)(0.f);
+  float m_run[1] = {-INFINITY}, l_run[1] = {0.f};
   if (w < tiles) load(w, pg0);
   for (int t = w; t < tiles; t += NW) {
     const int kb = start + t * KT;
@@ -956,24 +965,24 @@ __device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, int
 #pragma unroll
     for (int v = 1; v < 8; v++) mx = fmaxf(mx, s[v >> 2][v & 3]);
     mx *= sc;
-    if (__any(mx > m_run + 8.0f)) {
+    if (__any(mx > m_run[0] + 8.0f)) {
       mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float mn = fmaxf(m_run, mx);
-      const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - mn);
-      l_run *= al;
+      const float mn = fmaxf(m_run[0], mx);
+      const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[0] - mn);
+      l_run[0] *= al;
 #pragma unroll
-      for (int tt = 0; tt < NT; tt++) o[tt] *= al;
-      m_run = mn;
+      for (int tt = 0; tt < NT; tt++) o[0][tt] *= al;
+      m_run[0] = mn;
     }
-    const float off = m_run == -INFINITY ? 0.f : m_run;
+    const float off = m_run[0] == -INFINITY ? 0.f : m_run[0];
     union { uint32_t u[4]; bf16x8 f; } pf[NP];
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
       const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][(e & 3) + 1], sc, -off));
       uint32_t pl[NP];
       planes_of(p0, p1, pl);
-      l_run = add_planes(l_run, p0, p1, pl);
+      l_run[0] = add_planes(l_run[0], p0, p1, pl);
 #pragma unroll
       for (int p = 0; p < NP; p++) pf[p].u[e >> 1] = pl[p];
     }
@@ -983,15 +992,17 @@ __device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, int
 #pragma unroll
       for (int y = 0; y < 2; y++) vf.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lbf16x4*)(lbytes*)(vt + va[tt] + y * 16 * DH * 2));
 #pragma unroll
-      for (int p = NP - 1; p >= 0; p--) o[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.f, pf[p].f, o[tt], 0, 0, 0);
+      for (int p = NP - 1; p >= 0; p--) o[0][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.f, pf[p].f, o[0][tt], 0, 0, 0);
     }
   }
-  finish_few<T, uint16_t, DH>(A, it, R, g, o, m_run, l_run, lds);
+  finish_few<T, uint16_t, DH, 1>(A, it, R, g, o, m_run, l_run, lds);
 }
 
-// The same over an fp32 cache, 16 keys at a time, with v_mfma_f32_16x16x4_f32 (lane l supplies k = l / 16 of A row and B column
-// l % 16): a lane's four dims of a chunk are four steps; p is used as it is, register v of lanes 16 q .. being key 4 q + v.
-template <int DH>
+// The same over an fp32 cache, for up to 16 QS queries, 16 keys at a time, with v_mfma_f32_16x16x4_f32 (lane l supplies k = l / 16 of
+// A row and B column l % 16): a lane's four dims of a chunk are four steps; p is used as it is, register v of lanes 16 q .. being
+// key 4 q + v. One set of queries is bound by the stream of keys (64 sequences of 4096 keys, 8 KV heads of 128: 336 us, 6.4 TB/s), two
+// by the products behind it (461 us; 669 with 32 queries in one wave of piece_f32).
+template <int DH, int QS>
 __device__ void piece_few_f32(const SeqArgs& A, const Item& it, const Records R, int g, char* lds) {
   constexpr int KT = 16, NW = kWG / 64, KS = DH / 16, NT = DH / 16, NCH = DH / 4, KPL = 64 / NCH, VL = KT / KPL;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, q4 = lane >> 4;
@@ -1005,16 +1016,18 @@ __device__ void piece_few_f32(const SeqArgs& A, const Item& it, const Records R,
   auto page_at = [&](int t) { return table[min(start / kPage + t, last / kPage)]; };
   const int pg0 = w < tiles ? page_at(w) : 0;
   int pg = w < tiles ? page_at(w + NW) : 0;
-  const int jj = min(col, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
-  const int lim = min(row_limit(A, it, row), it.k1);
-  float4 qf[KS];
-  {
+  int lim[QS];
+  float4 qf[QS][KS];
+#pragma unroll
+  for (int x = 0; x < QS; x++) {
+    const int jj = min(x * 16 + col, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
+    lim[x] = min(row_limit(A, it, row), it.k1);
     const float* q = (const float*)A.q + row * A.qs + head * DH + q4 * 4;
     const float f = A.scale * kLog2e;
 #pragma unroll
     for (int s = 0; s < KS; s++) {
-      const float4 x = *reinterpret_cast<const float4*>(q + s * 16);
-      qf[s] = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
+      const float4 v = *reinterpret_cast<const float4*>(q + s * 16);
+      qf[x][s] = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
     }
   }
   uint4 kr[VL], vr[VL];
@@ -1031,10 +1044,15 @@ __device__ void piece_few_f32(const SeqArgs& A, const Item& it, const Records R,
   // K: chunk c of key k sits at c ^ k; V: at c ^ (k / 4) << 2, so that the four keys of a read are in different banks
   char* kt = lds + w * 2 * KT * DH * 4;
   char* vt = kt + KT * DH * 4;
-  f32x4 o[NT];
+  f32x4 o[QS][NT];
+  float m_run[QS], l_run[QS];
 #pragma unroll
-  for (int t = 0; t < NT; t++) o[t] = (f32x4)(0.f);
-  float m_run = -INFINITY, l_run = 0.f;
+  for (int x = 0; x < QS; x++) {
+#pragma unroll
+    for (int t = 0; t < NT; t++) o[x][t] = (f32x4)(0.f);
+    m_run[x] = -INFINITY;
+    l_run[x] = 0.f;
+  }
   if (w < tiles) load(w, pg0);
   for (int t = w; t < tiles; t += NW) {
     const int kb = start + t * KT;
@@ -1048,47 +1066,66 @@ __device__ void piece_few_f32(const SeqArgs& A, const Item& it, const Records R,
       load(t + NW, pg);
       pg = page_at(t + 2 * NW);
     }
-    f32x4 s = (f32x4)(0.f);
+    f32x4 s[QS];
+#pragma unroll
+    for (int x = 0; x < QS; x++) s[x] = (f32x4)(0.f);
 #pragma unroll
     for (int k = 0; k < KS; k++) {
       const float4 kf = *reinterpret_cast<const float4*>(kt + col * DH * 4 + (((4 * k + q4) ^ col) << 4));
-      s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.x, qf[k].x, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.y, qf[k].y, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.z, qf[k].z, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.w, qf[k].w, s, 0, 0, 0);
-    }
-    float mx = -INFINITY;
 #pragma unroll
-    for (int v = 0; v < 4; v++) {
-      const int kk = kb + 4 * q4 + v;
-      s[v] = kk < lim && kk >= it.k0 ? s[v] : -INFINITY;
-      mx = fmaxf(mx, s[v]);
-    }
-    if (__any(mx > m_run + 8.0f)) {
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float mn = fmaxf(m_run, mx);
-      const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - mn);
-      l_run *= al;
+      for (int x = 0; x < QS; x++) s[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.x, qf[x][k].x, s[x], 0, 0, 0);
 #pragma unroll
-      for (int tt = 0; tt < NT; tt++) o[tt] *= al;
-      m_run = mn;
-    }
-    const float off = m_run == -INFINITY ? 0.f : m_run;
+      for (int x = 0; x < QS; x++) s[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.y, qf[x][k].y, s[x], 0, 0, 0);
 #pragma unroll
-    for (int v = 0; v < 4; v++) {
-      s[v] = __builtin_amdgcn_exp2f(s[v] - off);
-      l_run += s[v];
+      for (int x = 0; x < QS; x++) s[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.z, qf[x][k].z, s[x], 0, 0, 0);
+#pragma unroll
+      for (int x = 0; x < QS; x++) s[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.w, qf[x][k].w, s[x], 0, 0, 0);
+    }
+    float mx[QS];
+    bool renew = false;
+#pragma unroll
+    for (int x = 0; x < QS; x++) {
+      mx[x] = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < 4; v++) {
+        const int kk = kb + 4 * q4 + v;
+        s[x][v] = kk < lim[x] && kk >= it.k0 ? s[x][v] : -INFINITY;
+        mx[x] = fmaxf(mx[x], s[x][v]);
+      }
+      renew = renew || mx[x] > m_run[x] + 8.0f;
+    }
+    if (__any(renew)) {
+#pragma unroll
+      for (int x = 0; x < QS; x++) {
+        float m = fmaxf(mx[x], __shfl_xor(mx[x], 16, 64));
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        const float mn = fmaxf(m_run[x], m);
+        const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[x] - mn);
+        l_run[x] *= al;
+#pragma unroll
+        for (int tt = 0; tt < NT; tt++) o[x][tt] *= al;
+        m_run[x] = mn;
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < QS; x++) {
+      const float off = m_run[x] == -INFINITY ? 0.f : m_run[x];
+#pragma unroll
+      for (int v = 0; v < 4; v++) {
+        s[x][v] = __builtin_amdgcn_exp2f(s[x][v] - off);
+        l_run[x] += s[x][v];
+      }
     }
 #pragma unroll
     for (int v = 0; v < 4; v++)
 #pragma unroll
       for (int tt = 0; tt < NT; tt++) {
         const float vf = *reinterpret_cast<const float*>(vt + (4 * q4 + v) * DH * 4 + (((tt * 4 + col / 4) ^ q4 << 2) << 4) + (col & 3) * 4);
-        o[tt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf, s[v], o[tt], 0, 0, 0);
+#pragma unroll
+        for (int x = 0; x < QS; x++) o[x][tt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf, s[x][v], o[x][tt], 0, 0, 0);
       }
   }
-  finish_few<float, float, DH>(A, it, R, g, o, m_run, l_run, lds);
+  finish_few<float, float, DH, QS>(A, it, R, g, o, m_run, l_run, lds);
 }
 
 // The same over an fp32 cache, for 32 queries a wave, with v_mfma_f32_32x32x2_f32 (lane l supplies k = l / 32 of A row
@@ -1249,7 +1286,9 @@ __global__ __launch_bounds__(kWG, 2) void k_attend_f32(SeqArgs A, const int* cou
   const Item it = items[y];
   if (y >= count[0]) return;
   if (it.mode & ITEM_FEW)
-    piece_few_f32<DH>(A, it, R, g, lds);
+    piece_few_f32<DH, 1>(A, it, R, g, lds);
+  else if (it.mode & ITEM_PAIR)
+    piece_few_f32<DH, 2>(A, it, R, g, lds);
   else
     piece_f32<DH>(A, it, R, g, lds);
 }
@@ -1263,7 +1302,7 @@ __global__ __launch_bounds__(kWG, 2) void k_attend_direct(SeqArgs A) {
   if constexpr (sizeof(KVT) == 2)
     piece_few<T, DH>(A, it, Records{}, g, lds);
   else
-    piece_few_f32<DH>(A, it, Records{}, g, lds);
+    piece_few_f32<DH, 1>(A, it, Records{}, g, lds);
 }
 
 // Records to outputs. Grid: x = KV head, y = units (strided). The DH / 4 lanes of a query first hold a piece's (m, l) each,
@@ -1420,6 +1459,7 @@ void run_attention(SeqArgs a, int dtype, const Request& q, bool prefix, void* wo
   p.rpt = q.rpt;
   p.tiles = q.tiles;
   p.jobs = q.jobs;
+  p.pair = a.c.dtype == SPD_F32;
   p.wide_cost = dtype == SPD_BF16 ? 1 : 4;
   p.qpu = q.qpu;
   p.records = q.records;

@@ -78,3 +78,30 @@ def test_hundreds_of_kv_heads(types):
     heads = (600, 600, 64)
     run_prompt([3, 20], [300, 1], heads, types, seed=6)
     run_prefix([3, 1], [290, 0], [300, 291, 310, 5], heads, types, seed=6)
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128), (6, 2, 64), (16, 1, 128), (3, 3, 64)], ids=str)
+def test_seventeen_to_thirty_two_queries_of_an_fp32_cache(heads):
+    """Two sets of 16 queries a piece, split over long caches and not, with a prefix shared by as many."""
+    from tests.test_gpu_seq_attention import run_prefix, run_prompt
+    G = heads[0] // heads[1]
+    few, most = 16 // G + 1, 32 // G
+    for seed, cached in enumerate(([0, 3000, 17, 1200], [31, 255, 256, 700])):
+        run_prompt([few, most, most, few], cached, heads, ("f32", "f32"), seed=seed, tail=1, pad=4)
+    lens = [1500 + 7 * i for i in range(most)]
+    run_prefix([most], [1490], lens, heads, ("f32", "f32"), seed=3)
+
+
+def test_values_that_are_not_finite_in_two_sets_of_queries():
+    from tests.seqcache import filled, i32
+    n = 8
+    for where, what in ((1, float("inf")), (1, float("nan")), (0, float("nan"))):
+        c, _ = filled([600], 2, 64, torch.float32, 3)
+        page = int(c.page_table[0, 37])
+        c.kv[0, page, where, 0, 4, 7] = what  # key 596 of KV head 0: rows 4 and up attend it
+        q = torch.randn(n, 8, 64, generator=torch.Generator().manual_seed(1)).cuda()
+        out = c.prompt_attention(0, q, i32([0]), i32([0, n]))
+        assert torch.isfinite(out[:4]).all() and torch.isfinite(out[:, 4:]).all()
+        assert not torch.isfinite(out[4:, :4, 7]).any()
+        if where == 0:
+            assert torch.isnan(out[4:, :4]).all()
