@@ -130,6 +130,8 @@ __device__ __forceinline__ void store4(uint16_t* p, const float (&a)[4], float f
 // over its prefix, and each row one over the keys behind it. Jobs longer than a `chunk` are split, so that a few rows
 // behind long caches fill the GPU: chunk = all jobs' keys / pieces wanted of a KV head. The pieces are
 // handed out longest first (a counting sort of their lengths), which is what keeps the last workgroups short.
+// 512 pieces wanted, two a CU: with 256 a prefix of 8192 keys for 64 rows takes 47.5 us instead of 42.2, with 384, 768 or 1024
+// no case gains. The plan itself is a chain of loads and barriers, 6 to 8 us by rocprofv3 whatever the batch up to 1024 jobs.
 // A job of one piece writes its rows' outputs; the pieces of others leave records (o, m, l), which the merge joins in
 // the order of the keys.
 struct Item {
@@ -618,7 +620,12 @@ __device__ void finish_wide(const SeqArgs& A, const Item& it, const Records R, i
 // K and V go to LDS by direct loads, the 16-byte chunks of a row permuted by its key so that neither kind of read
 // meets itself in a bank. A step reads its V fragments before it requests the next tile: the compiler lets every read of LDS
 // wait for the direct loads before it, and so the request has the softmax and the products to land in.
-// Two workgroups are on a CU, so that one's matrix work meets the other's vector work.
+// Two workgroups are on a CU, so that one's matrix work meets the other's vector work: a step of 64 keys takes a workgroup
+// 1.17 us alone on its CU and 2.0 beside another. 64 queries a wave instead leave registers for one workgroup a CU and reached
+// 664 TFLOP/s; eight waves of 256 queries that take turns were 2% faster at 16381 rows and slower on short prompts.
+// Measured (32 heads of 128 over 8): 16381 causal rows 2.09 ms, 1050 TFLOP/s of 1360 that a square product of 16384 reaches, at 71% matrix
+// cycles with the clock down to 1.5 GHz: power bounds it. Ten packed prompts of 8191 rows 135 us, 720 TFLOP/s. fp32 queries,
+// 2048 rows: 112 us, 306 TFLOP/s of the scores and outputs, three times that in products.
 template <typename T, int DH>
 __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, int g, char* lds) {
   constexpr int NP = sizeof(T) == 4 ? 3 : 1;
@@ -868,6 +875,7 @@ __device__ void finish_few(const SeqArgs& A, const Item& it, const Records R, in
 //     8 (l / 16); accumulator register v of lane l is row 4 (l / 16) + v, column l % 16).
 //   O^T += V^T P^T over the 32 keys at once: k = 8 q .. 8 q + 7 of lanes 16 q .. are the keys 4 q + 0..3 and 16 + 4 q + 0..3 whose
 //     probabilities they hold. K and V pass through a tile of LDS of the wave's own: loads take whole rows, operands 16 rows at once.
+// Measured: a row of each of 64 sequences of 8192 keys (8 KV heads of 128) 320 us, 6.7 TB/s.
 template <typename T, int DH>
 __device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, int g, char* lds) {
   constexpr int NP = sizeof(T) == 4 ? 3 : 1;
@@ -1130,7 +1138,8 @@ __device__ void piece_few_f32(const SeqArgs& A, const Item& it, const Records R,
 
 // The same over an fp32 cache, for 32 queries a wave, with v_mfma_f32_32x32x2_f32 (lane l supplies k = l / 32 of A row
 // and B column l % 32; accumulators as above): a lane's four dims of a chunk are four steps, so the halves take chunks in
-// turn. P is used as it is. Tiles of 32 keys.
+// turn. P is used as it is. Tiles of 32 keys. Bound by the products: 4096 causal rows 1.22 ms, 113 TFLOP/s, 8 x 2048 rows 123, of 154
+// that a square product of 16384 reaches.
 template <int DH>
 __device__ void piece_f32(const SeqArgs& A, const Item& it, const Records R, int g, char* lds) {
   constexpr int KT = 32, NT = DH / 32, KS = DH / 8, NCH = DH / 4;
@@ -1306,8 +1315,9 @@ __global__ __launch_bounds__(kWG, 2) void k_attend_direct(SeqArgs A) {
 }
 
 // Records to outputs. Grid: x = KV head, y = units (strided). The DH / 4 lanes of a query first hold a piece's (m, l) each,
-// which gives the query's maximum and the pieces' factors by shuffles, then four dims each, over eight pieces at once.
-constexpr int kMergeRows = 128;
+// which gives the query's maximum and the pieces' factors by shuffles, then four dims each, over eight pieces at once. It reads the
+// records once (64 rows of 32 heads in 32 pieces: 34 MB from the caches, 6.2 us).
+constexpr int kMergeRows = 128;  // 32: 4 us more there, 64: 0.5
 
 template <int DH>
 constexpr int merge_queries() { return kWG / (DH / 4); }
