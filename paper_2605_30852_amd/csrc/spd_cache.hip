@@ -415,7 +415,8 @@ struct AppendArgs {
 };
 
 // A workgroup takes a row. A thread's unit is eight dims of a head and the eight that rotate with them, 16 bytes a load. Bound by HBM:
-// fp32 rows of prompts into a bf16 cache, 273 MB, 45 us, 6 TB/s; 64 single rows 4 us, a launch and four dependent loads.
+// fp32 rows of prompts into a bf16 cache, 273 MB, 54 us, 5 TB/s, and 45 us when the rows are those of the last call, part of which
+// the caches keep; 64 single rows 4 us, a launch and four dependent loads.
 template <typename T, typename KVT, int DH>
 __global__ __launch_bounds__(kWG) void k_append(spd_cache c, AppendArgs A) {
   constexpr int H = DH / 2, UPH = H / 8;
