@@ -625,9 +625,9 @@ __device__ void finish_wide(const SeqArgs& A, const Item& it, const Records R, i
 // 664 TFLOP/s; eight waves of 256 queries that take turns were 2% faster at 16381 rows and slower on short prompts.
 // Measured (32 heads of 128 over 8): 16381 causal rows 2.04 to 2.18 ms, 1010 to 1075 TFLOP/s of 1360 that a square product of 16384
 // reaches, two thirds of its cycles in the matrix cores with the clock down to 1.5 GHz: power bounds it. Ten packed prompts of 8191
-// rows 135 us, 720 TFLOP/s, 40% of the cycles in the matrix cores: each piece of a workgroup costs some 6 us beside its steps, of
-// which workgroups that stay and take piece after piece lost none (149 us). fp32 queries,
-// 2048 rows: 112 us, 306 TFLOP/s of the scores and outputs, three times that in products.
+// rows 135 us, 720 TFLOP/s, 40% of the cycles in the matrix cores: a piece costs some 6 us beside its steps (item, pages, first
+// keys, output), which workgroups that stay and take piece after piece did not shorten (149 us where the others took 143). fp32
+// queries, 2048 rows: 110 us, 312 TFLOP/s of the scores and outputs, three times that in products, 57% of the cycles.
 template <typename T, int DH>
 __device__ void piece_wide(const SeqArgs& A, const Item& it, const Records R, int g, char* lds) {
   constexpr int NP = sizeof(T) == 4 ? 3 : 1;
@@ -1318,7 +1318,7 @@ __global__ __launch_bounds__(kWG, 2) void k_attend_direct(SeqArgs A) {
 
 // Records to outputs. Grid: x = KV head, y = units (strided). The DH / 4 lanes of a query first hold a piece's (m, l) each,
 // which gives the query's maximum and the pieces' factors by shuffles, then four dims each, over eight pieces at once. It reads the
-// records once (64 rows of 32 heads behind 8192 shared keys: 17 MB, half of it from the caches, 6.2 us).
+// records once (64 rows of 32 heads behind 8192 shared keys: 17 MB, 6.2 us).
 constexpr int kMergeRows = 128;  // 32: 4 us more there, 64: 0.5
 
 template <int DH>
