@@ -131,7 +131,7 @@ __device__ __forceinline__ void store4(uint16_t* p, const float (&a)[4], float f
 // behind long caches fill the GPU: chunk = all jobs' keys / pieces wanted of a KV head. The pieces are
 // handed out longest first (a counting sort of their lengths), which is what keeps the last workgroups short.
 // 512 pieces wanted, two a CU: with 256 a prefix of 8192 keys for 64 rows takes 47.5 us instead of 42.2, with 384, 768 or 1024
-// no case gains. The plan itself is a chain of loads and barriers, 6 to 8 us by rocprofv3 whatever the batch up to 1024 jobs.
+// no case gains. The plan itself is a chain of loads and barriers, 5 to 8 us by rocprofv3 up to 1024 jobs.
 // A job of one piece writes its rows' outputs; the pieces of others leave records (o, m, l), which the merge joins in
 // the order of the keys.
 struct Item {
@@ -152,7 +152,7 @@ struct Merge {
   int lim0, mode;
 };
 
-constexpr int kPlanWG = 1024;
+constexpr int kPlanWG = 1024, kSmallPlanWG = 256;
 constexpr int kMinChunk = 256;
 constexpr int kWantedWGs = 512;
 constexpr size_t kMaxWGs = (1 << 24) - 1;  // of 256 threads: a launch's threads are below 2^32
@@ -294,17 +294,17 @@ __device__ bool prefix_job(const PlanArgs& P, const Batch& B, int t, Job& j, boo
 // Tiles whose records are kept in LDS for the rows that join them.
 constexpr int kPlanTiles = 1024;
 
-template <bool PREFIX>
-__global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
+template <bool PREFIX, int NTH>
+__global__ __launch_bounds__(NTH) void k_plan_attention(PlanArgs P) {
   __shared__ int s_cu[kPlanSeqs + 1], s_seqs[kPlanSeqs], s_lens[kPlanSeqs], s_base[kPlanSeqs], s_prefix[PREFIX ? kPlanSeqs : 1];
   __shared__ int4 s_tile[PREFIX ? kPlanTiles : 1];
-  __shared__ unsigned long long s_total, s_max, s_sums[kPlanWG / 64];
+  __shared__ unsigned long long s_total, s_max, s_sums[NTH / 64];
   __shared__ int s_count[kBuckets], s_items;
   const int tid = threadIdx.x;
   const Batch B{s_cu, s_seqs, s_lens, s_prefix, s_base, &P, P.nseqs <= kPlanSeqs};
   if (B.in_lds) {
     const int n = PREFIX ? P.ngroups : P.nseqs;
-    for (int i = tid; i < P.nseqs; i += kPlanWG) {
+    for (int i = tid; i < P.nseqs; i += NTH) {
       const int s = P.seqs[i], c = i < n ? P.cu[i] : 0, x = PREFIX && i < n ? P.prefix[i] : 0;
       s_seqs[i] = s;
       s_lens[i] = (unsigned)s < (unsigned)P.c.max_seqs ? seq_len(P.c, s) : -1;
@@ -322,7 +322,7 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
     s_max = 1ull;
   }
   __syncthreads();
-  // A thread's jobs are tid, tid + kPlanWG, ..: the first is kept.
+  // A thread's jobs are tid, tid + NTH, ..: the first is kept.
   struct Known {
     Job j;
     bool is, shared;
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
   if (tid < P.jobs) work_out(tid, mine);
   auto each = [&](auto f) {
     if (mine.is) f(tid, mine);
-    for (int t = tid + kPlanWG; t < P.jobs; t += kPlanWG) {
+    for (int t = tid + NTH; t < P.jobs; t += NTH) {
       Known k;
       work_out(t, k);
       if (k.is) f(t, k);
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
   // Places of records, merges and units come from a prefix sum over the jobs (64 lanes that add to one LDS word take about a
   // microsecond), packed: records of a KV head above, then merges and units, which stay below 2^16.
   unsigned long long before = 0ull;
-  for (int t0 = 0; t0 < P.jobs; t0 += kPlanWG) {
+  for (int t0 = 0; t0 < P.jobs; t0 += NTH) {
     const int t = t0 + tid;
     Known k = mine;
     if (t0 > 0) {
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
     __syncthreads();
     unsigned long long at = before + x - v;
 #pragma unroll
-    for (int i = 0; i < kPlanWG / 64; i++) {
+    for (int i = 0; i < NTH / 64; i++) {
       if (i < tid >> 6) at += s_sums[i];
       before += s_sums[i];
     }
@@ -449,15 +449,29 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_attention(PlanArgs P) {
       P.merges[at_merge] = m;
       for (int u = 0; u < units; u++) P.units[at_unit + u] = Unit{at_merge, u * P.qpu};
     }
+    int chunk = 0, whole = 0, rest = 0;
     if (n > 0) {
-      const int chunk = chunk_of(k);
-      const int whole = n > 1 ? atomicAdd(&s_count[bucket(chunk, k.j.mode)], n - 1) : 0;
-      const int rest = atomicAdd(&s_count[bucket(k.j.b - k.j.a - (n - 1) * chunk, k.j.mode)], 1);
-      for (int p = 0; p < n; p++) {
-        const int a = k.j.a + p * chunk;
-        P.items[place(p < n - 1 ? whole + p : rest)] = Item{k.j.row0, k.j.nrows, k.j.table, a, max(a, min(k.j.b, a + chunk)),
-                                                            rec < 0 ? -1 : rec + p * P.c.n_kv_heads * nq, k.j.lim0, k.j.mode};
-      }
+      chunk = chunk_of(k);
+      if (n > 1) whole = atomicAdd(&s_count[bucket(chunk, k.j.mode)], n - 1);
+      rest = atomicAdd(&s_count[bucket(k.j.b - k.j.a - (n - 1) * chunk, k.j.mode)], 1);
+    }
+    const int step = P.c.n_kv_heads * nq;
+    auto write = [&](const Job& j, int p, int n, int chunk, int whole, int rest, int rec, int step) {
+      const int a = j.a + p * chunk;
+      P.items[place(p < n - 1 ? whole + p : rest)] =
+          Item{j.row0, j.nrows, j.table, a, max(a, min(j.b, a + chunk)), rec < 0 ? -1 : rec + p * step, j.lim0, j.mode};
+    };
+    // A few long jobs are written by their wave, a piece a lane: 0.5 us of 7.1 with 16 pieces in each of two, the call 1.1 of 42.4.
+    unsigned long long many = __ballot(n > 8);
+    if (__popcll(many) > 8) many = 0ull;
+    if (!(many >> (tid & 63) & 1ull))
+      for (int p = 0; p < n; p++) write(k.j, p, n, chunk, whole, rest, rec, step);
+    for (; many != 0ull; many &= many - 1ull) {
+      const int from = __builtin_ctzll(many);
+      auto of = [&](int x) { return __builtin_amdgcn_readlane(x, from); };
+      const Job j{of(k.j.row0), of(k.j.nrows), of(k.j.table), of(k.j.a), of(k.j.b), of(k.j.lim0), of(k.j.mode)};
+      const int jn = of(n), jc = of(chunk), jw = of(whole), jr = of(rest), rec0 = of(rec), st = of(step);
+      for (int p = tid & 63; p < jn; p += 64) write(j, p, jn, jc, jw, jr, rec0, st);
     }
   }
   if (tid == 0) P.count[1] = (int)(before & 0xffff);
@@ -1453,6 +1467,19 @@ void launch(const SeqArgs& a, const Request& q, const PlanArgs& p, const Records
                        p.count, p.units, p.merges, r);
 }
 
+// A thread a job: four waves, one a SIMD, go through the plan faster than sixteen (7.1 and 8.0 us for 64 rows that share a prefix)
+// while they have one job a thread.
+template <int NTH>
+void launch_plan_of(const PlanArgs& p, bool prefix, hipStream_t s) {
+  if (prefix)
+    hipLaunchKernelGGL((k_plan_attention<true, NTH>), dim3(1), dim3(NTH), 0, s, p);
+  else
+    hipLaunchKernelGGL((k_plan_attention<false, NTH>), dim3(1), dim3(NTH), 0, s, p);
+}
+void launch_plan(const PlanArgs& p, bool prefix, hipStream_t s) {
+  p.jobs <= kSmallPlanWG ? launch_plan_of<kSmallPlanWG>(p, prefix, s) : launch_plan_of<kPlanWG>(p, prefix, s);
+}
+
 // Plan, pieces, merge; or the pieces alone.
 void run_attention(SeqArgs a, int dtype, const Request& q, bool prefix, void* workspace, hipStream_t s) {
   a.rpt = q.rpt;
@@ -1483,10 +1510,7 @@ void run_attention(SeqArgs a, int dtype, const Request& q, bool prefix, void* wo
     p.units = (Unit*)(ws + q.at_units);
     p.tile_rec = (int4*)(ws + q.at_tiles);
     r = Records{(float*)(ws + q.at_o), (float2*)(ws + q.at_ml)};
-    if (prefix)
-      hipLaunchKernelGGL((k_plan_attention<true>), dim3(1), dim3(kPlanWG), 0, s, p);
-    else
-      hipLaunchKernelGGL((k_plan_attention<false>), dim3(1), dim3(kPlanWG), 0, s, p);
+    launch_plan(p, prefix, s);
   }
   const bool wide = a.c.head_dim == 128;
   if (dtype == SPD_BF16)
