@@ -1405,8 +1405,8 @@ Request request(const spd_cache& c, int n_q_heads, int nseqs, int rows, int ngro
   const int hkv = c.n_kv_heads, G = n_q_heads / hkv;
   // Short calls go without a plan, one launch, every piece of at most 16 queries over all its keys: prompts whose tiles are at
   // most two a CU, decode rows (a shared prefix of so few keys is in the L2 for all of a group that the GPU holds at once). Planned and
-  // so: 3 fp32 prompts of 21 rows 13.7 and 5.1 us, 4 bf16 prompts of 16 rows behind 300 keys 16.7 and 9.2, decode rows of
-  // 300 keys 16.8 and 8.2, 256 of 512 keys 90 and 84. Longer calls need the splits, larger prompts the wide tiles.
+  // so: 3 fp32 prompts of 21 rows 13.9 and 5.2 us, 4 bf16 prompts of 16 rows behind 300 keys 17.1 and 9.3, decode rows of
+  // 300 keys 15.9 and 8.2, 256 of 512 keys 89 and 85. Longer calls need the splits, larger prompts the wide tiles.
   const bool fits = max_len > 0 && max_len <= 512;
   q.rpt = 16 / G;
   q.direct = fits && (prefix ? nseqs * hkv <= (ngroups > 0 ? 512 : 2048) : ((long long)rows / q.rpt + nseqs) * hkv <= 512);
