@@ -259,8 +259,10 @@ __device__ __forceinline__ void fork_pages(const spd_cache& c, int s, int d, int
   }
 }
 
-// SMALL: the same workgroup applies what it has checked, a wave a child at a time (a launch less, for at most 16384 entries of the
-// table: 64 children of up to 129 pages 7.5 us); otherwise k_apply_fork does.
+// SMALL: the same workgroup applies what it has checked, a wave a child at a time; otherwise k_apply_fork does, a launch more. For 64
+// children of up to 130 pages one launch takes 8 us and its call 3 us less than with two, in a captured graph as much; 256 children
+// of up to 64 pages take 7 us more in one.
+constexpr int kSmallFork = 12288;  // entries of the children's tables
 template <bool SMALL>
 __global__ __launch_bounds__(kPlanWG) void k_plan_fork(spd_cache c, const int* src, const int* dst, const int* keep, int n,
                                                        int* status, Plan P) {
@@ -518,7 +520,7 @@ extern "C" spd_status spd_cache_fork(const spd_cache* c, const int32_t* src, con
   if (st != SPD_OK) return st;
   const Plan p = plan_of(*c, n, workspace);
   hipStream_t s = (hipStream_t)stream;
-  if ((size_t)n * c->max_pages <= 16384) {
+  if ((size_t)n * c->max_pages <= kSmallFork) {
     hipLaunchKernelGGL(k_plan_fork<true>, dim3(1), dim3(kPlanWG), 0, s, *c, src, dst, keep, n, status, p);
   } else {
     hipLaunchKernelGGL(k_plan_fork<false>, dim3(1), dim3(kPlanWG), 0, s, *c, src, dst, keep, n, status, p);

@@ -891,7 +891,8 @@ __device__ void finish_few(const SeqArgs& A, const Item& it, const Records R, in
 //     8 (l / 16); accumulator register v of lane l is row 4 (l / 16) + v, column l % 16).
 //   O^T += V^T P^T over the 32 keys at once: k = 8 q .. 8 q + 7 of lanes 16 q .. are the keys 4 q + 0..3 and 16 + 4 q + 0..3 whose
 //     probabilities they hold. K and V pass through a tile of LDS of the wave's own: loads take whole rows, operands 16 rows at once.
-// Measured: a row of each of 64 sequences of 8192 keys (8 KV heads of 128) 320 us, 6.7 TB/s.
+// Measured: a row of each of 64 sequences of 8192 keys (8 KV heads of 128) 320 us, 6.7 TB/s; 16 queries a KV head behind 64 of 4096
+// keys 171 us, where a wide piece takes 189 for 20.
 template <typename T, int DH>
 __device__ void piece_few(const SeqArgs& A, const Item& it, const Records R, int g, char* lds) {
   constexpr int NP = sizeof(T) == 4 ? 3 : 1;
