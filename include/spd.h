@@ -466,9 +466,10 @@ spd_status spd_prompt_attention(const spd_cache* c, int32_t layer, const void* q
  * keys gets zeros. Group j is rows cu_groups[j] .. cu_groups[j + 1] - 1 (device int32[ngroups + 1], ascending, from 0 to
  * nseqs); its rows' sequences agree in their first prefix_lens[j] keys (device int32[ngroups]), as forked ones do. Those are
  * read through the pages of the group's first sequence, once for 128 queries, or, in short calls, by every row through
- * its own pages, which it has to hold. A row shorter than its group's prefix attends the
- * keys it has; the first row's sequence must hold the prefix. With ngroups 0 (both arrays NULL) no row shares
- * anything. q, out, max_len and the workspace as in spd_prompt_attention; nseqs at most 4096. */
+ * its own pages, which it has to hold. A row shorter than its group's prefix attends the keys it has; the first row's
+ * sequence must hold the prefix. With ngroups 0 (both arrays NULL) no row shares anything, and none does where cu_groups,
+ * which only the device sees, does not ascend. q, out, max_len and the workspace as in spd_prompt_attention; nseqs at
+ * most 4096. */
 spd_status spd_prefix_attention_workspace(const spd_cache* c, int32_t n_q_heads, int32_t dtype, int32_t nseqs,
                                           int32_t ngroups, int32_t max_len, size_t* bytes);
 spd_status spd_prefix_attention(const spd_cache* c, int32_t layer, const void* q, int64_t q_stride, void* out,

@@ -172,7 +172,6 @@ struct PlanArgs {
   int pair;                             // an fp32 cache: pieces of up to 32 queries
   int wide_cost;                        // of a key of a wide piece; 1: of one of few queries, 2: of a pair
   int qpu;                              // queries of a merge's workgroup
-  unsigned long long records;           // room for them
   int* count;                           // items, units
   Item* items;
   Merge* merges;
@@ -259,6 +258,7 @@ __device__ bool prefix_job(const PlanArgs& P, const Batch& B, int t, Job& j, boo
   j.lim0 = 0;
   j.a = 0;
   if (t < P.tiles) {
+    if (P.ngroups == 0) return false;
     const int g = B.of_tile(P.ngroups, t), n = shared_prefix(P, B, g, first, rows);
     if (n == 0) return false;
     const long long at = (long long)(t - B.base_at(g)) * P.rpt;
@@ -299,13 +299,16 @@ __global__ __launch_bounds__(NTH) void k_plan_attention(PlanArgs P) {
   __shared__ int s_cu[kPlanSeqs + 1], s_seqs[kPlanSeqs], s_lens[kPlanSeqs], s_base[kPlanSeqs], s_prefix[PREFIX ? kPlanSeqs : 1];
   __shared__ int4 s_tile[PREFIX ? kPlanTiles : 1];
   __shared__ unsigned long long s_total, s_max, s_sums[NTH / 64];
+  __shared__ int s_back[NTH / 64];
   __shared__ int s_count[kBuckets], s_items;
   const int tid = threadIdx.x;
   const Batch B{s_cu, s_seqs, s_lens, s_prefix, s_base, &P, P.nseqs <= kPlanSeqs};
+  bool back = false;  // a group that ends before it begins
   if (B.in_lds) {
     const int n = PREFIX ? P.ngroups : P.nseqs;
     for (int i = tid; i < P.nseqs; i += NTH) {
       const int s = P.seqs[i], c = i < n ? P.cu[i] : 0, x = PREFIX && i < n ? P.prefix[i] : 0;
+      if (PREFIX) back = back || (i < n && P.cu[i + 1] < c);
       s_seqs[i] = s;
       s_lens[i] = (unsigned)s < (unsigned)P.c.max_seqs ? seq_len(P.c, s) : -1;
       if (i < n) {
@@ -321,7 +324,18 @@ __global__ __launch_bounds__(NTH) void k_plan_attention(PlanArgs P) {
     s_total = 0ull;
     s_max = 1ull;
   }
+  if (PREFIX) {
+    const bool any = __any(back);
+    if ((tid & 63) == 0) s_back[tid >> 6] = any;
+  }
   __syncthreads();
+  // Groups that ascend have no row in common, which is what the room for records is made for. Others are none: every row goes
+  // through its own pages.
+  if (PREFIX) {
+#pragma unroll
+    for (int i = 0; i < NTH / 64; i++)
+      if (s_back[i]) P.ngroups = 0;
+  }
   // A thread's jobs are tid, tid + NTH, ..: the first is kept.
   struct Known {
     Job j;
@@ -405,8 +419,7 @@ __global__ __launch_bounds__(NTH) void k_plan_attention(PlanArgs P) {
       if (t < P.jobs) work_out(t, k);
     }
     const bool tile = PREFIX && t < P.tiles;
-    int n = k.is ? pieces_of(k) : 0;
-    const int nq = k.is ? k.j.nrows * P.G : 0, units = (nq + P.qpu - 1) / P.qpu;
+    const int n = k.is ? pieces_of(k) : 0, nq = k.is ? k.j.nrows * P.G : 0, units = (nq + P.qpu - 1) / P.qpu;
     const bool joins = k.is && (n > 1 || k.shared);
     const unsigned long long v = joins ? (unsigned long long)(unsigned)(n * nq) << 32 | (tile ? 0 : 1u << 16 | units) : 0ull;
     const unsigned long long x = wave_scan(v);
@@ -418,9 +431,7 @@ __global__ __launch_bounds__(NTH) void k_plan_attention(PlanArgs P) {
       if (i < tid >> 6) at += s_sums[i];
       before += s_sums[i];
     }
-    const long long first = (long long)(at >> 32) * P.c.n_kv_heads;
-    if (joins && first + (long long)n * nq * P.c.n_kv_heads > (long long)P.records) n = 0;  // only where cu_groups does not ascend
-    const int rec = joins ? (int)first : -1;
+    const int rec = joins ? (int)((long long)(at >> 32) * P.c.n_kv_heads) : -1;
     if (tile) {
       const int4 r = joins ? make_int4(rec, n, nq, 0) : make_int4(0, 0, 0, 0);
       if (t < kPlanTiles)
@@ -1481,10 +1492,7 @@ void launch_plan(const PlanArgs& p, bool prefix, hipStream_t s) {
   p.jobs <= kSmallPlanWG ? launch_plan_of<kSmallPlanWG>(p, prefix, s) : launch_plan_of<kPlanWG>(p, prefix, s);
 }
 
-// Plan, pieces, merge; or the pieces alone.
-void run_attention(SeqArgs a, int dtype, const Request& q, bool prefix, void* workspace, hipStream_t s) {
-  a.rpt = q.rpt;
-  if (q.direct && prefix) a.cu = nullptr;
+PlanArgs plan_args(const SeqArgs& a, int dtype, const Request& q, void* workspace) {
   char* ws = (char*)workspace;
   PlanArgs p{};
   p.c = a.c;
@@ -1502,15 +1510,23 @@ void run_attention(SeqArgs a, int dtype, const Request& q, bool prefix, void* wo
   p.pair = a.c.dtype == SPD_F32;
   p.wide_cost = dtype == SPD_BF16 ? 1 : 4;
   p.qpu = q.qpu;
-  p.records = q.records;
+  p.count = (int*)ws;
+  p.items = (Item*)(ws + q.at_items);
+  p.merges = (Merge*)(ws + q.at_merges);
+  p.units = (Unit*)(ws + q.at_units);
+  p.tile_rec = (int4*)(ws + q.at_tiles);
+  return p;
+}
+
+// Plan, pieces, merge; or the pieces alone.
+void run_attention(SeqArgs a, int dtype, const Request& q, bool prefix, void* workspace, hipStream_t s) {
+  a.rpt = q.rpt;
+  if (q.direct && prefix) a.cu = nullptr;
+  PlanArgs p{};
   Records r{};
   if (!q.direct) {
-    p.count = (int*)ws;
-    p.items = (Item*)(ws + q.at_items);
-    p.merges = (Merge*)(ws + q.at_merges);
-    p.units = (Unit*)(ws + q.at_units);
-    p.tile_rec = (int4*)(ws + q.at_tiles);
-    r = Records{(float*)(ws + q.at_o), (float2*)(ws + q.at_ml)};
+    p = plan_args(a, dtype, q, workspace);
+    r = Records{(float*)((char*)workspace + q.at_o), (float2*)((char*)workspace + q.at_ml)};
     launch_plan(p, prefix, s);
   }
   const bool wide = a.c.head_dim == 128;
