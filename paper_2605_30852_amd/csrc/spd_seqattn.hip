@@ -26,10 +26,16 @@ struct SeqArgs {
   float scale;
 };
 
+constexpr float kLog2e = 1.44269504088896341f;
+
+// 2^-down times n numbers sum to less than the largest of them.
+__device__ __forceinline__ int down_of(int n) { return 33 - __clz(n); }
+
 // A query over the keys [k0, k1) in plain fp32, by the whole workgroup, which a query, key or value that is not finite
-// needs: there 0 times a value behind the query's own keys, or a plane's 0 * inf, is NaN on matrix cores. Scores in passes of
-// a key a thread, computed twice rather than kept. M, L and a (dims 4 d4 .. + 3 of thread d4 = tid % (DH / 4)) are the
-// maximum, the sum and the output; true in the threads that hold them. lds: 6 * kWG floats.
+// needs: there 0 times a value behind the query's own keys, or a plane's 0 * inf, is NaN on matrix cores. So do finite values
+// whose sum is not, and here every probability, at most 1, is lowered by a power of two that keeps a sum below the largest value.
+// Scores in passes of a key a thread, computed twice rather than kept. M, L and a (dims 4 d4 .. + 3 of thread d4 = tid % (DH / 4))
+// are the offset of the exponents (in units of log2), the sum and the output; true in the threads that hold them. lds: 6 * kWG floats.
 template <typename T, typename KVT, int DH>
 __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* table, int g, const T* q, float scale, int k0,
                             int k1, float* lds, float& M, float& L, float (&a)[4]) {
@@ -81,11 +87,14 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
     return grp == 0;
   }
   L = a[0] = a[1] = a[2] = a[3] = 0.f;
+  const int down = down_of(k1 - k0);
+  const float top = M, part = ldexpf(1.0f, -down);
+  M = fmaf(top, kLog2e, (float)down);
   for (int base = k0; base < k1; base += kWG) {
     float p = 0.f;
     if (base + tid < k1) {
       const float s = score(base + tid);
-      p = s == -INFINITY ? 0.f : expf(s - M);
+      p = s == -INFINITY ? 0.f : expf(s - top) * part;
     }
     sp[tid] = p;
     __syncthreads();
@@ -513,8 +522,6 @@ __device__ __forceinline__ void planes3(float x, uint32_t& h, uint32_t& m, uint3
   l = __float_as_uint(r1 - __uint_as_float(b & 0xffff0000u)) >> 16;
 }
 
-constexpr float kLog2e = 1.44269504088896341f;
-
 // Two probabilities (finite, not negative) as planes of a product's operand: rounded to one bf16 each, or three that are exact.
 __device__ __forceinline__ void planes_of(float p0, float p1, uint32_t (&u)[1]) { u[0] = pack_bf16(p0, p1); }
 __device__ __forceinline__ void planes_of(float p0, float p1, uint32_t (&u)[3]) {
@@ -582,7 +589,7 @@ __device__ void plain_piece(const SeqArgs& A, const Item& it, const Records& R, 
   } else {
     const size_t at = (size_t)it.rec + (size_t)g * it.nrows * A.G + j;
     store4(R.o + at * DH + d, a, 1.0f);
-    if (d == 0) R.ml[at] = make_float2(M * kLog2e, L);
+    if (d == 0) R.ml[at] = make_float2(M, L);
   }
 }
 
@@ -597,7 +604,7 @@ __device__ void finish_wide(const SeqArgs& A, const Item& it, const Records R, i
   const bool active = w * 32 < nq, mine = jq < nq;
   l_run += __shfl_xor(l_run, 32, 64);
 
-  __shared__ uint32_t s_bad[kWG / 64];  // queries whose result here is not a number
+  __shared__ uint32_t s_bad[kWG / 64];  // queries whose result here is not finite
   if (tid < kWG / 64) s_bad[tid] = 0u;
   __syncthreads();
   if (active) {
@@ -605,7 +612,7 @@ __device__ void finish_wide(const SeqArgs& A, const Item& it, const Records R, i
 #pragma unroll
     for (int tt = 0; tt < NT; tt++)
 #pragma unroll
-      for (int v = 0; v < 16; v++) bad = bad || o[tt][v] != o[tt][v];
+      for (int v = 0; v < 16; v++) bad = bad || !(fabsf(o[tt][v]) < INFINITY);
     const unsigned long long bads = __ballot(bad && mine);
     if (lane == 0) s_bad[w] = (uint32_t)bads | (uint32_t)(bads >> 32);
     if (mine) {
@@ -880,7 +887,8 @@ __device__ void finish_few(const SeqArgs& A, const Item& it, const Records R, in
       a[2] = fmaf(v.z, f, a[2]);
       a[3] = fmaf(v.w, f, a[3]);
     }
-    if ((!(L > 0.f) && n > it.k0) || a[0] != a[0] || a[1] != a[1] || a[2] != a[2] || a[3] != a[3]) {
+    auto finite = [](float x) { return fabsf(x) < INFINITY; };
+    if ((!(L > 0.f) && n > it.k0) || !(finite(a[0]) && finite(a[1]) && finite(a[2]) && finite(a[3]))) {
       atomicOr(&s_few_bad, 1u << j);
     } else if (it.rec < 0) {
       store4((T*)A.out + r * A.os + hd * DH + d, a, n > 0 ? 1.0f / L : 0.f);
@@ -1365,40 +1373,48 @@ __global__ __launch_bounds__(kWG) void k_merge(SeqArgs A, const int* count, cons
     const int r = m.row0 + jj / G, head = g * G + jj % G;
     int lim = m.lim0 + jj / G;
     if (m.mode & ITEM_FLAT) lim = seq_len(A.c, A.seqs[r]);
-    float M = -INFINITY, L = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < np; p0 += TPQ) {  // a pass but for more pieces than lanes
-      const int p = p0 + lane;
-      const float2 ml = p < np ? R.ml[record(p)] : make_float2(-INFINITY, 0.f);
-      float mp = ml.x;
+    float L, a[4], part = 1.0f;
+    bool again;
+    do {  // once more, lowered by a power of two, where finite records add up to what is not
+      float M = -INFINITY;
+      L = a[0] = a[1] = a[2] = a[3] = 0.f;
+      for (int p0 = 0; p0 < np; p0 += TPQ) {  // a pass but for more pieces than lanes
+        const int p = p0 + lane;
+        const float2 ml = p < np ? R.ml[record(p)] : make_float2(-INFINITY, 0.f);
+        float mp = ml.x;
 #pragma unroll
-      for (int d = 1; d < TPQ; d <<= 1) mp = fmaxf(mp, __shfl_xor(mp, d, TPQ));
-      const float Mn = fmaxf(M, mp);
-      const float before = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - Mn);
-      // no key of this query in the piece: 0; a sum that is NaN goes on
-      const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - Mn);
-      float l = ml.y * f;
+        for (int d = 1; d < TPQ; d <<= 1) mp = fmaxf(mp, __shfl_xor(mp, d, TPQ));
+        const float Mn = fmaxf(M, mp);
+        const float before = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - Mn);
+        // no key of this query in the piece: 0; a sum that is NaN goes on
+        const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - Mn) * part;
+        float l = ml.y * f;
 #pragma unroll
-      for (int d = 1; d < TPQ; d <<= 1) l += __shfl_xor(l, d, TPQ);
-      M = Mn;
-      L = L * before + l;
+        for (int d = 1; d < TPQ; d <<= 1) l += __shfl_xor(l, d, TPQ);
+        M = Mn;
+        L = L * before + l;
 #pragma unroll
-      for (int e = 0; e < 4; e++) a[e] *= before;
-      const int here = min(TPQ, np - p0);
-      for (int b = 0; b < here; b += 8) {
-        float4 o[8];
+        for (int e = 0; e < 4; e++) a[e] *= before;
+        const int here = min(TPQ, np - p0);
+        for (int b = 0; b < here; b += 8) {
+          float4 o[8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) o[e] = *reinterpret_cast<const float4*>(R.o + record(min(p0 + b + e, np - 1)) * DH + 4 * lane);
+          for (int e = 0; e < 8; e++) o[e] = *reinterpret_cast<const float4*>(R.o + record(min(p0 + b + e, np - 1)) * DH + 4 * lane);
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-          const float w = __shfl(f, min(b + e, TPQ - 1), TPQ);
-          if (b + e >= here) continue;
-          a[0] = fmaf(o[e].x, w, a[0]);
-          a[1] = fmaf(o[e].y, w, a[1]);
-          a[2] = fmaf(o[e].z, w, a[2]);
-          a[3] = fmaf(o[e].w, w, a[3]);
+          for (int e = 0; e < 8; e++) {
+            const float w = __shfl(f, min(b + e, TPQ - 1), TPQ);
+            if (b + e >= here) continue;
+            a[0] = fmaf(o[e].x, w, a[0]);
+            a[1] = fmaf(o[e].y, w, a[1]);
+            a[2] = fmaf(o[e].z, w, a[2]);
+            a[3] = fmaf(o[e].w, w, a[3]);
+          }
         }
       }
-    }
+      const bool finite = fabsf(a[0]) < INFINITY && fabsf(a[1]) < INFINITY && fabsf(a[2]) < INFINITY && fabsf(a[3]) < INFINITY;
+      again = part == 1.0f && __any(!finite);
+      part = ldexpf(1.0f, -down_of(max(np, 1)));
+    } while (again);
     if (j < nq) store4((T*)A.out + r * A.os + head * DH + 4 * lane, a, lim > 0 ? 1.0f / L : 0.f);
   }
 }

@@ -189,6 +189,7 @@ inline auto min(A a, B b) -> decltype(a + b) { return a < b ? a : b; }
 template <typename A, typename B>
 inline auto max(A a, B b) -> decltype(a + b) { return a > b ? a : b; }
 inline int __popcll(unsigned long long m) { return __builtin_popcountll(m); }
+inline int __clz(int v) { return v ? __builtin_clz((unsigned)v) : 32; }
 inline float __uint_as_float(uint32_t u) { float f; __builtin_memcpy(&f, &u, 4); return f; }
 inline uint32_t __float_as_uint(float f) { uint32_t u; __builtin_memcpy(&u, &f, 4); return u; }
 unsigned long long wall_clock64();
