@@ -435,9 +435,9 @@ spd_status spd_cache_compact(const spd_cache* c, int32_t* live, void* workspace,
  * rotated at their positions (rotate-half RoPE, cos and sin: device fp32 [rope_positions][head_dim / 2], with
  * rope_positions >= 16 * max_pages; both NULL with rope_positions 0: no rotation). k, v: device [rows] of n_kv_heads *
  * head_dim elements of dtype, rows k_stride and v_stride elements apart; q and q_out likewise, n_q_heads * head_dim
- * (both NULL with n_q_heads 0: keys and values only; q_out may be q). The rotation is fp32, rounded once to the cache's
- * type (to dtype for q_out). Pointers are 16-byte aligned, strides multiples of 16 bytes. A sequence has to be named
- * once, and the pages its rows fall in have to be its own, as spd_cache_reserve leaves them. */
+ * (both NULL with n_q_heads 0: keys and values only; q_out may be q, with the same stride). The rotation is fp32,
+ * rounded once to the cache's type (to dtype for q_out). Pointers are 16-byte aligned, strides multiples of 16 bytes. A
+ * sequence has to be named once, and the pages its rows fall in have to be its own, as spd_cache_reserve leaves them. */
 spd_status spd_cache_append(const spd_cache* c, int32_t layer, const void* k, int64_t k_stride, const void* v,
                             int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
                             int32_t n_q_heads, int32_t dtype, const float* rope_cos, const float* rope_sin,

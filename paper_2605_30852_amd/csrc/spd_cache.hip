@@ -573,6 +573,7 @@ extern "C" spd_status spd_cache_append(const spd_cache* c, int32_t layer, const 
   if (rope_cos ? rope_positions < kPage * c->max_pages : rope_positions != 0)
     return invalid(call, "rope_positions must be at least 16 * max_pages (0 without cos and sin)");
   if (rows == 0) return SPD_OK;
+  if (q && q == q_out && q_stride != q_out_stride && rows > 1) return invalid(call, "q_out may be q with the same stride only");
   const AppendArgs a{k, v, q, q_out, k_stride, v_stride, q_stride, q_out_stride, rope_cos, rope_sin, seqs, cu_rows, layer,
                      n_q_heads, nseqs, rows};
   hipStream_t s = (hipStream_t)stream;
