@@ -259,10 +259,16 @@ __device__ __forceinline__ void fork_pages(const spd_cache& c, int s, int d, int
   }
 }
 
-// SMALL: the same workgroup applies what it has checked, a wave a child at a time; otherwise k_apply_fork does, a launch more. For 64
-// children of up to 130 pages one launch takes 8 us and its call 3 us less than with two, in a captured graph as much; 256 children
-// of up to 64 pages take 7 us more in one.
+// SMALL: the same workgroup applies what it has checked, its 16 waves divided among the children; otherwise k_apply_fork does, a
+// workgroup a child, a launch more. Fork and a truncate behind it, in one launch and in two, called (and replayed in a graph): 8 children
+// of 130 pages 17.7 and 20.4 us (8.1 and 8.9), 64 of them 17.6 and 20.7 (14.5 and 10.5): one saves the host a launch where that bounds
+// the calls. 128 of 90 pages 19.7 and 20.8 (20.1 and 12.8), 256 of 48 24.4 and 20.7 (25 and 15.6): two from 65 children on. Many long
+// ones want a workgroup each: 16 of 2048 pages 20.1 and 20.4 (20.5 and 13.4); one or two have more threads in one: one of 12288 25.5 and 36.2
+// (25 and 35.8). How long the children are only the device knows, so short ones in a wide table go in two as well: 64 of 16 pages,
+// 2048 wide, 17.6 and 20.9 us (10.1 and 9.4).
 constexpr int kSmallFork = 12288;  // entries of the children's tables
+bool small_fork(const spd_cache& c, int n) { return n <= 2 || (n <= 64 && (size_t)n * c.max_pages <= kSmallFork); }
+
 template <bool SMALL>
 __global__ __launch_bounds__(kPlanWG) void k_plan_fork(spd_cache c, const int* src, const int* dst, const int* keep, int n,
                                                        int* status, Plan P) {
@@ -279,10 +285,17 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_fork(spd_cache c, const int* s
     *status = s_status;
   }
   if (!SMALL || s_status != SPD_CACHE_DONE) return;
-  for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves) {
-    const int d = dst[i], k = keep[i];
-    fork_pages(c, src[i], d, k, threadIdx.x & 63, 64);
-    if ((threadIdx.x & 63) == 0) c.lens[d] = k;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (n > kPlanWaves / 2) {  // a wave a child at a time
+    for (int i = w; i < n; i += kPlanWaves) {
+      const int d = dst[i], k = keep[i];
+      fork_pages(c, src[i], d, k, lane, 64);
+      if (lane == 0) c.lens[d] = k;
+    }
+  } else if (const int per = kPlanWaves / n; w < n * per) {  // several waves each
+    const int i = w / per, d = dst[i], k = keep[i], at = (w - i * per) * 64 + lane;
+    fork_pages(c, src[i], d, k, at, 64 * per);
+    if (at == 0) c.lens[d] = k;
   }
 }
 
@@ -520,7 +533,7 @@ extern "C" spd_status spd_cache_fork(const spd_cache* c, const int32_t* src, con
   if (st != SPD_OK) return st;
   const Plan p = plan_of(*c, n, workspace);
   hipStream_t s = (hipStream_t)stream;
-  if ((size_t)n * c->max_pages <= kSmallFork) {
+  if (small_fork(*c, n)) {
     hipLaunchKernelGGL(k_plan_fork<true>, dim3(1), dim3(kPlanWG), 0, s, *c, src, dst, keep, n, status, p);
   } else {
     hipLaunchKernelGGL(k_plan_fork<false>, dim3(1), dim3(kPlanWG), 0, s, *c, src, dst, keep, n, status, p);
