@@ -402,28 +402,30 @@ enum {
   SPD_CACHE_BAD_SEQ = 3    /* a sequence outside [0, max_seqs), named twice, or (fork) a child that is not empty */
 };
 
-/* Bytes of device workspace the calls below need for n sequences of the cache. Host-only. */
+/* Bytes of device workspace, 256-byte aligned, that is enough for each of the calls below on n sequences of the cache
+ * (spd_cache_fork takes 256 bytes, spd_cache_truncate none). Host-only. */
 spd_status spd_cache_workspace(const spd_cache* c, int32_t n, size_t* bytes);
 
 /* Sequence seqs[i] grows by add[i] >= 0 keys (device int32[n] each, 1 <= n <= max_seqs), to be written by
  * spd_cache_append. Pages are taken in order of i, then of the logical page, the lowest-numbered free ones first. A
  * sequence that grows and ends inside a page that others hold too (refs > 1 before the call) gets a copy of that page,
- * of all layers, in its place: the first page it takes. status: device int32. workspace: device, 256-byte aligned. */
+ * of all layers, in its place: the first page it takes. status: device int32. */
 spd_status spd_cache_reserve(const spd_cache* c, const int32_t* seqs, const int32_t* add, int32_t n, int32_t* status,
                              void* workspace, size_t ws_bytes, void* stream);
 
 /* The empty sequence dst[i] becomes the first keep[i] keys of src[i] (device int32[n] each), sharing its pages. The
- * sources are read as they were before the call; one may be named several times. */
+ * sources are read as they were before the call; one may be named several times. workspace: 256 bytes are enough. */
 spd_status spd_cache_fork(const spd_cache* c, const int32_t* src, const int32_t* dst, const int32_t* keep, int32_t n,
                           int32_t* status, void* workspace, size_t ws_bytes, void* stream);
 
 /* Sequence seqs[i] keeps its first min(keep[i], lens[seqs[i]]) keys (device int32[n] each; 0: none) and lets go of the pages
- * behind them; their table entries become -1. A page that no sequence holds any more is free. */
+ * behind them; their table entries become -1. A page that no sequence holds any more is free. workspace is not used: it
+ * may be NULL, and ws_bytes 0. */
 spd_status spd_cache_truncate(const spd_cache* c, const int32_t* seqs, const int32_t* keep, int32_t n, int32_t* status,
                               void* workspace, size_t ws_bytes, void* stream);
 
 /* The held pages move to ids 0 .. *live - 1 (live: device int32), in all layers: those with an id of *live or more go,
- * in order, to the free ids below, in order; the table and refs follow. Workspace as for n = 1. */
+ * in order, to the free ids below, in order; the table and refs follow. */
 spd_status spd_cache_compact(const spd_cache* c, int32_t* live, void* workspace, size_t ws_bytes, void* stream);
 
 /* A batch's packed rows: sequence seqs[i] (i < nseqs) has rows cu_rows[i] .. cu_rows[i + 1] - 1 (device int32[nseqs]

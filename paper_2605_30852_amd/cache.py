@@ -13,6 +13,7 @@ import torch
 from . import binding as B
 
 PAGE = 16
+_FORK_WORKSPACE = 256
 _DTYPES = {torch.float32: B.SPD_F32, torch.bfloat16: B.SPD_BF16}
 
 
@@ -61,12 +62,12 @@ class PagedCache:
         """The empty sequence dst[i] becomes the first keep[i] keys of src[i], sharing its pages; returns the status."""
         n = self._entries(src, dst, keep)
         return self._change(n, lambda st, ws, wb, s: B.spd_cache_fork(self.c, src.data_ptr(), dst.data_ptr(), keep.data_ptr(), n,
-                                                                      st, ws, wb, s))
+                                                                      st, ws, wb, s), _FORK_WORKSPACE)
 
     def truncate(self, seqs: torch.Tensor, keep: torch.Tensor) -> torch.Tensor:
         """Sequence seqs[i] keeps its first keep[i] keys (0: none) and lets go of its other pages; returns the status."""
         n = self._entries(seqs, keep)
-        return self._change(n, lambda st, ws, wb, s: B.spd_cache_truncate(self.c, seqs.data_ptr(), keep.data_ptr(), n, st, ws, wb, s))
+        return self._change(n, lambda st, ws, wb, s: B.spd_cache_truncate(self.c, seqs.data_ptr(), keep.data_ptr(), n, st, ws, wb, s), 0)
 
     def compact(self) -> torch.Tensor:
         """Moves the held pages to the lowest ids; returns their number (int32[1])."""
@@ -194,9 +195,11 @@ class PagedCache:
         ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         return ws, ws.data_ptr()
 
-    def _change(self, n: int, call) -> torch.Tensor:
+    def _change(self, n: int, call, wb: Optional[int] = None) -> torch.Tensor:
+        """wb: the workspace's bytes, if not those for n sequences."""
         word = torch.empty(1, dtype=torch.int32, device=self.device)
-        wb = self._bytes(("pages", n), B.spd_cache_workspace) if n >= 1 else 256
+        if wb is None:
+            wb = self._bytes(("pages", n), B.spd_cache_workspace) if n >= 1 else 0
         ws, wp = self._workspace(wb)
         self._on_device(lambda s: call(word.data_ptr(), wp, wb, s))
         return word

@@ -1,11 +1,12 @@
 // The pages of a cache of several sequences: growing (with copies of shared pages), forking, truncating and compacting
 // them, and the rows that enter them.
 //
-// The state (table, lens, refs) lives on the device. A call that changes pages is two launches. The plan, one
+// The state (table, lens, refs) lives on the device. Growing, compacting and large forks are two launches. The plan, one
 // workgroup, checks the request and decides everything: a call that does not fit changes nothing. It works in tiles of
 // entries or page ids with a prefix sum over the workgroup, so that pages are handed out in one fixed order, whatever
 // the order in which waves run. Then many workgroups apply the plan: entries, counts (integer atomics, whose order
-// does not show) and the copies of pages, which are what takes time: page bytes x layers, read and written once.
+// does not show) and the copies of pages, which are what takes time: page bytes x layers, read and written once. A fork
+// of few children is applied by the workgroup that checks it, and truncating needs no plan: every workgroup checks all of it.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -59,7 +60,7 @@ namespace {
 constexpr int kPlanWG = 1024, kPlanWaves = kPlanWG / 64, kSmallPlanWG = 256;
 constexpr int kIdsPerWave = 16 * 64, kIdsPerTile = kPlanWaves * kIdsPerWave;  // page ids of a tile of a plan
 
-// Workspace of a plan, in ints: the header, four arrays of n entries, three of num_pages.
+// Workspace of a plan, in ints: the header, then what the call needs.
 enum { PH_STATUS = 0, PH_MOVES = 1, PH_LIVE = 2, PH_INTS = 16 };
 struct Plan {
   int* head;
@@ -69,16 +70,24 @@ struct Plan {
   int* map;                         // compact: where page id goes
 };
 
-size_t plan_ints(const spd_cache& c, int n) { return PH_INTS + 4 * (size_t)n + 3 * (size_t)c.num_pages; }
+size_t reserve_ints(const spd_cache& c, int n) { return PH_INTS + 4 * (size_t)n + (size_t)c.num_pages; }
+size_t compact_ints(const spd_cache& c) { return PH_INTS + 3 * (size_t)c.num_pages; }
 
-Plan plan_of(const spd_cache& c, int n, void* ws) {
-  Plan p;
+Plan reserve_plan(int n, void* ws) {
+  Plan p{};
   p.head = (int*)ws;
   p.first = p.head + PH_INTS;
   p.begin = p.first + n;
   p.want = p.begin + n;
   p.src = p.want + n;
   p.ids = p.src + n;
+  return p;
+}
+
+Plan compact_plan(const spd_cache& c, void* ws) {
+  Plan p{};
+  p.head = (int*)ws;
+  p.ids = p.head + PH_INTS;
   p.late = p.ids + c.num_pages;
   p.map = p.late + c.num_pages;
   return p;
@@ -271,7 +280,7 @@ bool small_fork(const spd_cache& c, int n) { return n <= 2 || (n <= 64 && (size_
 
 template <bool SMALL>
 __global__ __launch_bounds__(kPlanWG) void k_plan_fork(spd_cache c, const int* src, const int* dst, const int* keep, int n,
-                                                       int* status, Plan P) {
+                                                       int* status, int* head) {
   __shared__ uint32_t bits[kMaxSeqs / 32];
   __shared__ int s_status;
   const Named named{bits};
@@ -281,7 +290,7 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_fork(spd_cache c, const int* s
   check_fork(c, src, dst, keep, n, named, &s_status);
   __syncthreads();
   if (threadIdx.x == 0) {
-    P.head[PH_STATUS] = s_status;
+    if (!SMALL) head[PH_STATUS] = s_status;
     *status = s_status;
   }
   if (!SMALL || s_status != SPD_CACHE_DONE) return;
@@ -300,8 +309,8 @@ __global__ __launch_bounds__(kPlanWG) void k_plan_fork(spd_cache c, const int* s
 }
 
 // Grid: x = child.
-__global__ __launch_bounds__(kWG) void k_apply_fork(spd_cache c, const int* src, const int* dst, const int* keep, Plan P) {
-  if (P.head[PH_STATUS] != SPD_CACHE_DONE) return;
+__global__ __launch_bounds__(kWG) void k_apply_fork(spd_cache c, const int* src, const int* dst, const int* keep, const int* head) {
+  if (head[PH_STATUS] != SPD_CACHE_DONE) return;
   const int i = blockIdx.x;
   fork_pages(c, src[i], dst[i], keep[i], threadIdx.x, kWG);
   if (threadIdx.x == 0) c.lens[dst[i]] = keep[i];
@@ -489,14 +498,13 @@ int slices_of(const spd_cache& c) { return (int)((page_bytes_of(c) + kSlice - 1)
 constexpr int kCopyWGs = 4096;
 
 // The checks that reserve, fork, truncate and compact share.
-spd_status check_change(const char* call, const spd_cache* c, std::initializer_list<const void*> arrays, int n, void* ws,
-                        size_t ws_bytes) {
+spd_status check_change(const char* call, const spd_cache* c, std::initializer_list<const void*> arrays, int n) {
   const spd_status st = check_cache(call, c, true);
   if (st != SPD_OK) return st;
   for (const void* p : arrays)
     if (!p || misaligned(p, 4)) return invalid(call, "NULL or misaligned pointer");
   if (n < 1 || n > c->max_seqs) return invalid(call, "n must be in [1, max_seqs]");
-  return check_workspace(call, ws, ws_bytes, plan_ints(*c, n) * sizeof(int));
+  return SPD_OK;
 }
 
 }  // namespace
@@ -508,15 +516,16 @@ extern "C" spd_status spd_cache_workspace(const spd_cache* c, int32_t n, size_t*
   const spd_status st = check_cache("cache workspace", c, false);
   if (st != SPD_OK) return st;
   if (!bytes || n < 1 || n > c->max_seqs) return invalid("cache workspace", "NULL pointer, or n outside [1, max_seqs]");
-  *bytes = (plan_ints(*c, n) * sizeof(int) + 255) / 256 * 256;
+  *bytes = (std::max(reserve_ints(*c, n), compact_ints(*c)) * sizeof(int) + 255) / 256 * 256;
   return SPD_OK;
 }
 
 extern "C" spd_status spd_cache_reserve(const spd_cache* c, const int32_t* seqs, const int32_t* add, int32_t n, int32_t* status,
                                         void* workspace, size_t ws_bytes, void* stream) {
-  const spd_status st = check_change("cache reserve", c, {seqs, add, status}, n, workspace, ws_bytes);
+  spd_status st = check_change("cache reserve", c, {seqs, add, status}, n);
+  if (st == SPD_OK) st = check_workspace("cache reserve", workspace, ws_bytes, reserve_ints(*c, n) * sizeof(int));
   if (st != SPD_OK) return st;
-  const Plan p = plan_of(*c, n, workspace);
+  const Plan p = reserve_plan(n, workspace);
   hipStream_t s = (hipStream_t)stream;
   if (n <= kSmallPlanWG && c->num_pages <= 16 * kSmallPlanWG)  // one entry a thread, one tile of page ids: 6.2 us instead of 7.9
     hipLaunchKernelGGL(k_plan_reserve<kSmallPlanWG>, dim3(1), dim3(kSmallPlanWG), 0, s, *c, seqs, add, n, status, p);
@@ -529,31 +538,33 @@ extern "C" spd_status spd_cache_reserve(const spd_cache* c, const int32_t* seqs,
 
 extern "C" spd_status spd_cache_fork(const spd_cache* c, const int32_t* src, const int32_t* dst, const int32_t* keep, int32_t n,
                                      int32_t* status, void* workspace, size_t ws_bytes, void* stream) {
-  const spd_status st = check_change("cache fork", c, {src, dst, keep, status}, n, workspace, ws_bytes);
+  spd_status st = check_change("cache fork", c, {src, dst, keep, status}, n);
+  if (st == SPD_OK) st = check_workspace("cache fork", workspace, ws_bytes, PH_INTS * sizeof(int));
   if (st != SPD_OK) return st;
-  const Plan p = plan_of(*c, n, workspace);
+  int* head = (int*)workspace;
   hipStream_t s = (hipStream_t)stream;
   if (small_fork(*c, n)) {
-    hipLaunchKernelGGL(k_plan_fork<true>, dim3(1), dim3(kPlanWG), 0, s, *c, src, dst, keep, n, status, p);
+    hipLaunchKernelGGL(k_plan_fork<true>, dim3(1), dim3(kPlanWG), 0, s, *c, src, dst, keep, n, status, head);
   } else {
-    hipLaunchKernelGGL(k_plan_fork<false>, dim3(1), dim3(kPlanWG), 0, s, *c, src, dst, keep, n, status, p);
-    hipLaunchKernelGGL(k_apply_fork, dim3(n), dim3(kWG), 0, s, *c, src, dst, keep, p);
+    hipLaunchKernelGGL(k_plan_fork<false>, dim3(1), dim3(kPlanWG), 0, s, *c, src, dst, keep, n, status, head);
+    hipLaunchKernelGGL(k_apply_fork, dim3(n), dim3(kWG), 0, s, *c, src, dst, keep, head);
   }
   return check_launch("cache fork");
 }
 
 extern "C" spd_status spd_cache_truncate(const spd_cache* c, const int32_t* seqs, const int32_t* keep, int32_t n,
-                                         int32_t* status, void* workspace, size_t ws_bytes, void* stream) {
-  const spd_status st = check_change("cache truncate", c, {seqs, keep, status}, n, workspace, ws_bytes);
+                                         int32_t* status, void*, size_t, void* stream) {
+  const spd_status st = check_change("cache truncate", c, {seqs, keep, status}, n);
   if (st != SPD_OK) return st;
   hipLaunchKernelGGL(k_truncate, dim3(std::min(n, kTruncateWGs)), dim3(kWG), 0, (hipStream_t)stream, *c, seqs, keep, n, status);
   return check_launch("cache truncate");
 }
 
 extern "C" spd_status spd_cache_compact(const spd_cache* c, int32_t* live, void* workspace, size_t ws_bytes, void* stream) {
-  const spd_status st = check_change("cache compact", c, {live}, 1, workspace, ws_bytes);
+  spd_status st = check_change("cache compact", c, {live}, 1);
+  if (st == SPD_OK) st = check_workspace("cache compact", workspace, ws_bytes, compact_ints(*c) * sizeof(int));
   if (st != SPD_OK) return st;
-  const Plan p = plan_of(*c, 1, workspace);
+  const Plan p = compact_plan(*c, workspace);
   hipStream_t s = (hipStream_t)stream;
   hipLaunchKernelGGL(k_plan_compact, dim3(1), dim3(kPlanWG), 0, s, *c, live, p);
   hipLaunchKernelGGL(k_apply_compact, dim3(kCopyWGs), dim3(kWG), 0, s, *c, p, page_bytes_of(*c), slices_of(*c));
