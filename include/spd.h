@@ -451,7 +451,9 @@ spd_status spd_cache_append(const spd_cache* c, int32_t layer, const void* k, in
  * scores are scaled by 1 / sqrt(head_dim). A row that would stand for a key before the first attends nothing: zeros.
  *   q, out: device [rows] of n_q_heads * head_dim elements of dtype, rows q_stride and out_stride elements apart
  *     (16-byte aligned, strides multiples of 16 bytes; no element of out is one of q). dtype SPD_F32 with any cache,
- *     SPD_BF16 with a bf16 cache.
+ *     SPD_BF16 with a bf16 cache. Scores, sums and outputs are held in fp32 and rounded once to dtype. With SPD_BF16
+ *     each probability is rounded to bf16 too (by at most 2^-8 of it), before it weighs its value; the weights' sum is
+ *     that of the rounded ones. With SPD_F32 the products are those of the fp32 operands.
  *   max_len (host): the keys of the longest sequence, for the choice of key splits (0: 16 * max_pages). The result
  *     is right for any value, if not always in the same order of sums.
  *   workspace: device, 256-byte aligned, of spd_prompt_attention_workspace(the same sizes).
@@ -470,8 +472,8 @@ spd_status spd_prompt_attention(const spd_cache* c, int32_t layer, const void* q
  * read through the pages of the group's first sequence, once for 128 queries, or, in short calls, by every row through
  * its own pages, which it has to hold. A row shorter than its group's prefix attends the keys it has; the first row's
  * sequence must hold the prefix. With ngroups 0 (both arrays NULL) no row shares anything, and none does where cu_groups,
- * which only the device sees, does not ascend. q, out, max_len and the workspace as in spd_prompt_attention; nseqs at
- * most 4096. */
+ * which only the device sees, does not ascend. q, out, their types and roundings, max_len and the workspace as in
+ * spd_prompt_attention; nseqs at most 4096. */
 spd_status spd_prefix_attention_workspace(const spd_cache* c, int32_t n_q_heads, int32_t dtype, int32_t nseqs,
                                           int32_t ngroups, int32_t max_len, size_t* bytes);
 spd_status spd_prefix_attention(const spd_cache* c, int32_t layer, const void* q, int64_t q_stride, void* out,

@@ -108,6 +108,7 @@ class PagedCache:
     def prompt_attention(self, layer: int, q: torch.Tensor, seqs: torch.Tensor, cu_rows: torch.Tensor,
                          out: Optional[torch.Tensor] = None, max_len: int = 0) -> torch.Tensor:
         """Causal attention of a batch's packed rows q [rows][heads][head_dim], the newest keys of their sequences.
+        fp32 q: any cache, fp32 arithmetic; bf16 q: a bf16 cache, and the probabilities are rounded to bf16 as the output is.
         max_len: keys of the longest sequence, if known. Rows of `out` behind the last sequence are left as they are."""
         rows, n = q.shape[0], self._batch(seqs, cu_rows)
         hq, qs, out, os_ = self._query(q, rows, out)

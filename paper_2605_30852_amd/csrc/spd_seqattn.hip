@@ -648,7 +648,10 @@ __device__ void finish_wide(const SeqArgs& A, const Item& it, const Records R, i
 //   O^T += V^T P^T: registers 8 s .. 8 s + 7 of half h are the probabilities of keys 16 s + 4 h + 0..3 and 16 s + 8 + 4 h
 //     + 0..3, which two transposing LDS reads of V rows give as the A operand.
 // bf16 queries: q as it is, the scale in the exponent's FMA, p rounded to bf16 (half a step, 2^-8 of each p: as much as the
-// rounding of the output), l the sum of the rounded p. fp32 queries: q (scaled in fp32) and p as three exact planes, three products each.
+// rounding of the output), l the sum of the rounded p. The outputs' error against 64 bits is 2.0e-3 to 2.3e-3 (relative norm, values of
+// mean 0, where roundings show most); p as two planes, 16 bits, makes it the output's own rounding, 1.63e-3 to 1.66e-3, and takes 2932 us
+// for 2144 at 16381 rows, 172 for 140 in ten packed prompts, 56 for 46 behind long caches, 44.5 for 42 behind a shared prefix. Who
+// wants more than a bf16 output's accuracy has fp32 queries: q (scaled in fp32) and p as three exact planes, three products each.
 // K and V go to LDS by direct loads, the 16-byte chunks of a row permuted by its key so that neither kind of read
 // meets itself in a bank. A step reads its V fragments before it requests the next tile: the compiler lets every read of LDS
 // wait for the direct loads before it, and so the request has the softmax and the products to land in.
