@@ -481,6 +481,73 @@ spd_status spd_prefix_attention(const spd_cache* c, int32_t layer, const void* q
                                 int32_t nseqs, const int32_t* cu_groups, const int32_t* prefix_lens, int32_t ngroups,
                                 int32_t max_len, void* workspace, size_t ws_bytes, void* stream);
 
+/* Rotary frequencies theta_i = base^(-2i / dims), i < dims / 2, and how they are scaled for contexts longer than the
+ * trained one: LINEAR theta / factor; BASE base * factor^(dims / (dims - 2)) in base's place; PARTS, with r = original * theta / 2 pi
+ * the turns of a pair over the original context and g = (r - low) / (high - low) clamped to [0, 1], (1 - g) theta / factor + g theta. */
+enum { SPD_ROPE_PLAIN = 0, SPD_ROPE_LINEAR = 1, SPD_ROPE_BASE = 2, SPD_ROPE_PARTS = 3 };
+typedef struct spd_rope_scaling {
+  int32_t kind;
+  int32_t original;  /* PARTS: keys of the original context */
+  double factor;     /* finite, above 0 */
+  double low, high;  /* PARTS: low < high */
+} spd_rope_scaling;
+
+/* The frequencies in double precision. dims even, in [2, 256] (BASE: at least 4); base finite and above 1; scaling NULL:
+ * PLAIN; freq: host [dims / 2]. Host-only. */
+spd_status spd_rope_frequencies(int32_t dims, double base, const spd_rope_scaling* scaling, double* freq);
+
+/* Rows first .. first + positions - 1 of a rotary table: amplitude * cos and sin of position * freq[i], the angle reduced exactly
+ * and both rounded once to fp32. freq: host [pairs], pairs in [1, 128], each of at most 1e6 (radians a position), read during the call;
+ * first within 2^40 of 0. cosines, sines: device fp32 [positions][pairs], 16-byte aligned. Asynchronous on stream (a hipStream_t). */
+spd_status spd_rope_table(const double* freq, int32_t pairs, int64_t first, int32_t positions, double amplitude,
+                          float* cosines, float* sines, void* stream);
+
+/* What spd_cache_append_heads makes of the heads of q and k. gains: device fp32 [head_dim], 16-byte aligned; a head x
+ * becomes x / sqrt(mean(x^2) + eps) * gain, in fp32 (NULL: as it is). Then its first `rot` dims (a multiple of 16) turn: dims i and i +
+ * rot / 2, or (interleaved) 2i and 2i + 1, by cos and sin [rope_positions][rot / 2] at the row's position. */
+typedef struct spd_head_rule {
+  const float* q_gain;
+  const float* k_gain;
+  float eps;            /* finite and above 0, where a gain is given */
+  int32_t rot;          /* 0: no rotation, cos and sin NULL */
+  int32_t interleaved;  /* 0 or 1 */
+} spd_head_rule;
+
+/* spd_cache_append with norms of the heads and other rotations; rounded once, behind both. Else as that call. */
+spd_status spd_cache_append_heads(const spd_cache* c, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                                  int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                                  int32_t n_q_heads, int32_t dtype, const spd_head_rule* rule, const float* rope_cos,
+                                  const float* rope_sin, int32_t rope_positions, const int32_t* seqs,
+                                  const int32_t* cu_rows, int32_t nseqs, int32_t rows, void* stream);
+
+/* A rule for the attention of other decoders' layers. Of its sequence's keys, the row of key p sees the first
+ * open_lens[i] (of batch sequence i, at most its length; also those behind p), and those of [max(first[row], p - window + 1), p].
+ * A row that sees nothing, or would stand for a key before the first, gets zeros; keys unseen count nothing, whatever they hold. A
+ * score s (scaled) becomes cap * tanh(s / cap), then slopes[head] * |p - key| is taken from it. */
+typedef struct spd_attention_rule {
+  float cap;                /* 0: scores as they are; otherwise in [2^-20, 2^20] */
+  int32_t window;           /* 0: none */
+  const float* slopes;      /* device fp32 [n_q_heads], finite; NULL: none */
+  const int32_t* first;     /* device int32 [rows], a row's first key (of its document); NULL: 0 */
+  const int32_t* open_lens; /* device int32 [nseqs]; NULL: 0 */
+} spd_attention_rule;
+
+/* spd_prompt_attention and spd_prefix_attention under a rule (host struct, read during the call). In the latter a row is a
+ * sequence's, rows are nseqs. Else as the calls without a rule, but for the workspace, which is that of the calls here. */
+spd_status spd_prompt_attention_ruled_workspace(const spd_cache* c, int32_t n_q_heads, int32_t dtype, int32_t nseqs,
+                                                int32_t rows, int32_t max_len, size_t* bytes);
+spd_status spd_prompt_attention_ruled(const spd_cache* c, int32_t layer, const void* q, int64_t q_stride, void* out,
+                                      int64_t out_stride, int32_t n_q_heads, int32_t dtype, const int32_t* seqs,
+                                      const int32_t* cu_rows, int32_t nseqs, int32_t rows, int32_t max_len,
+                                      const spd_attention_rule* rule, void* workspace, size_t ws_bytes, void* stream);
+spd_status spd_prefix_attention_ruled_workspace(const spd_cache* c, int32_t n_q_heads, int32_t dtype, int32_t nseqs,
+                                                int32_t ngroups, int32_t max_len, size_t* bytes);
+spd_status spd_prefix_attention_ruled(const spd_cache* c, int32_t layer, const void* q, int64_t q_stride, void* out,
+                                      int64_t out_stride, int32_t n_q_heads, int32_t dtype, const int32_t* seqs,
+                                      int32_t nseqs, const int32_t* cu_groups, const int32_t* prefix_lens, int32_t ngroups,
+                                      int32_t max_len, const spd_attention_rule* rule, void* workspace, size_t ws_bytes,
+                                      void* stream);
+
 /* Release the handle's events and host buffers (not the caller's memory). NULL is ignored. */
 void spd_destroy(spd_handle* h);
 

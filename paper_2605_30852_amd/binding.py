@@ -54,6 +54,22 @@ class spd_cache(ct.Structure):
         (k, ct.c_int32) for k in ("n_layers", "num_pages", "max_seqs", "max_pages", "n_kv_heads", "head_dim", "dtype")]
 
 
+class spd_attention_rule(ct.Structure):
+    _fields_ = [("cap", ct.c_float), ("window", ct.c_int32)] + [(k, ct.c_void_p) for k in ("slopes", "first", "open_lens")]
+
+
+class spd_head_rule(ct.Structure):
+    _fields_ = [("q_gain", ct.c_void_p), ("k_gain", ct.c_void_p), ("eps", ct.c_float), ("rot", ct.c_int32),
+                ("interleaved", ct.c_int32)]
+
+
+SPD_ROPE_PLAIN, SPD_ROPE_LINEAR, SPD_ROPE_BASE, SPD_ROPE_PARTS = 0, 1, 2, 3
+
+
+class spd_rope_scaling(ct.Structure):
+    _fields_ = [("kind", ct.c_int32), ("original", ct.c_int32), ("factor", ct.c_double), ("low", ct.c_double), ("high", ct.c_double)]
+
+
 class spd_step_result(ct.Structure):
     _fields_ = [(k, ct.c_int32) for k in
                 ("decision", "target_argmax", "draft", "pdm_draft", "exited_pos", "exited_token", "verified_pos",
@@ -73,7 +89,9 @@ EXPORTS = [
     "spd_set_pdm_schedule", "spd_set_graph_steps", "spd_decode_attention", "spd_decode_attention_noalloc",
     "spd_cache_workspace", "spd_cache_reserve", "spd_cache_fork", "spd_cache_truncate", "spd_cache_compact",
     "spd_cache_append", "spd_prompt_attention_workspace", "spd_prompt_attention", "spd_prefix_attention_workspace",
-    "spd_prefix_attention",
+    "spd_prefix_attention", "spd_rope_frequencies", "spd_rope_table", "spd_cache_append_heads",
+    "spd_prompt_attention_ruled_workspace", "spd_prompt_attention_ruled", "spd_prefix_attention_ruled_workspace",
+    "spd_prefix_attention_ruled",
 ]
 
 _lib: Optional[ct.CDLL] = None
@@ -97,6 +115,8 @@ def lib() -> ct.CDLL:
         L64 = ct.c_int64
         C = ct.POINTER(spd_cache)
         Z = ct.POINTER(ct.c_size_t)
+        D = ct.c_double
+        R = ct.POINTER(spd_attention_rule)
         sig = {
             "spd_workspace_size": (I, [ct.POINTER(spd_config), ct.POINTER(ct.c_size_t)]),
             "spd_stage_bounds": (I, [ct.POINTER(spd_config), ct.POINTER(ct.c_int32)]),
@@ -140,6 +160,13 @@ def lib() -> ct.CDLL:
             "spd_prompt_attention": (I, [C, I, P, L64, P, L64, I, I, P, P, I, I, I, P, ct.c_size_t, P]),
             "spd_prefix_attention_workspace": (I, [C, I, I, I, I, I, Z]),
             "spd_prefix_attention": (I, [C, I, P, L64, P, L64, I, I, P, I, P, P, I, I, P, ct.c_size_t, P]),
+            "spd_rope_frequencies": (I, [I, D, ct.POINTER(spd_rope_scaling), ct.POINTER(D)]),
+            "spd_rope_table": (I, [ct.POINTER(D), I, L64, I, D, P, P, P]),
+            "spd_cache_append_heads": (I, [C, I, P, L64, P, L64, P, L64, P, L64, I, I, ct.POINTER(spd_head_rule), P, P, I, P, P, I, I, P]),
+            "spd_prompt_attention_ruled_workspace": (I, [C, I, I, I, I, I, Z]),
+            "spd_prompt_attention_ruled": (I, [C, I, P, L64, P, L64, I, I, P, P, I, I, I, R, P, ct.c_size_t, P]),
+            "spd_prefix_attention_ruled_workspace": (I, [C, I, I, I, I, I, Z]),
+            "spd_prefix_attention_ruled": (I, [C, I, P, L64, P, L64, I, I, P, I, P, P, I, I, R, P, ct.c_size_t, P]),
             "spd_destroy": (None, [P]),
             "spd_status_str": (ct.c_char_p, [I]),
             "spd_last_error": (ct.c_char_p, [P]),
@@ -424,6 +451,58 @@ def spd_prefix_attention(cache: spd_cache, layer: int, q: int, q_stride: int, ou
     _check("spd_prefix_attention",
            lib().spd_prefix_attention(ct.byref(cache), layer, q, q_stride, out, out_stride, n_q_heads, dtype, seqs, nseqs,
                                       cu_groups, prefix_lens, ngroups, max_len, workspace, ws_bytes, stream))
+
+
+def spd_prompt_attention_ruled_workspace(cache: spd_cache, n_q_heads: int, dtype: int, nseqs: int, rows: int, max_len: int) -> int:
+    b = ct.c_size_t(0)
+    _check("spd_prompt_attention_ruled_workspace",
+           lib().spd_prompt_attention_ruled_workspace(ct.byref(cache), n_q_heads, dtype, nseqs, rows, max_len, ct.byref(b)))
+    return b.value
+
+
+def spd_prompt_attention_ruled(cache: spd_cache, layer: int, q: int, q_stride: int, out: int, out_stride: int, n_q_heads: int,
+                               dtype: int, seqs: int, cu_rows: int, nseqs: int, rows: int, max_len: int,
+                               rule: spd_attention_rule, workspace: int, ws_bytes: int, stream: int) -> None:
+    _check("spd_prompt_attention_ruled",
+           lib().spd_prompt_attention_ruled(ct.byref(cache), layer, q, q_stride, out, out_stride, n_q_heads, dtype, seqs, cu_rows,
+                                            nseqs, rows, max_len, ct.byref(rule), workspace, ws_bytes, stream))
+
+
+def spd_prefix_attention_ruled_workspace(cache: spd_cache, n_q_heads: int, dtype: int, nseqs: int, ngroups: int, max_len: int) -> int:
+    b = ct.c_size_t(0)
+    _check("spd_prefix_attention_ruled_workspace",
+           lib().spd_prefix_attention_ruled_workspace(ct.byref(cache), n_q_heads, dtype, nseqs, ngroups, max_len, ct.byref(b)))
+    return b.value
+
+
+def spd_prefix_attention_ruled(cache: spd_cache, layer: int, q: int, q_stride: int, out: int, out_stride: int, n_q_heads: int,
+                               dtype: int, seqs: int, nseqs: int, cu_groups: int, prefix_lens: int, ngroups: int, max_len: int,
+                               rule: spd_attention_rule, workspace: int, ws_bytes: int, stream: int) -> None:
+    _check("spd_prefix_attention_ruled",
+           lib().spd_prefix_attention_ruled(ct.byref(cache), layer, q, q_stride, out, out_stride, n_q_heads, dtype, seqs, nseqs,
+                                            cu_groups, prefix_lens, ngroups, max_len, ct.byref(rule), workspace, ws_bytes, stream))
+
+
+def spd_cache_append_heads(cache: spd_cache, layer: int, k: int, k_stride: int, v: int, v_stride: int, q: int, q_stride: int,
+                           q_out: int, q_out_stride: int, n_q_heads: int, dtype: int, rule: spd_head_rule, rope_cos: int,
+                           rope_sin: int, rope_positions: int, seqs: int, cu_rows: int, nseqs: int, rows: int, stream: int) -> None:
+    _check("spd_cache_append_heads",
+           lib().spd_cache_append_heads(ct.byref(cache), layer, k, k_stride, v, v_stride, q, q_stride, q_out, q_out_stride,
+                                        n_q_heads, dtype, ct.byref(rule), rope_cos, rope_sin, rope_positions, seqs, cu_rows, nseqs,
+                                        rows, stream))
+
+
+def spd_rope_frequencies(dims: int, base: float, scaling: Optional[spd_rope_scaling] = None) -> "ct.Array":
+    """dims / 2 doubles, a ctypes array."""
+    out = (ct.c_double * max(1, dims // 2))()
+    _check("spd_rope_frequencies",
+           lib().spd_rope_frequencies(dims, base, ct.byref(scaling) if scaling is not None else None, out))
+    return out
+
+
+def spd_rope_table(freq, pairs: int, first: int, positions: int, amplitude: float, cos: int, sin: int, stream: int) -> None:
+    """freq: a ctypes array or pointer of doubles on the host."""
+    _check("spd_rope_table", lib().spd_rope_table(freq, pairs, first, positions, amplitude, cos, sin, stream))
 
 
 def spd_destroy(h: int) -> None:

@@ -17,6 +17,54 @@ _FORK_WORKSPACE = 256
 _DTYPES = {torch.float32: B.SPD_F32, torch.bfloat16: B.SPD_BF16}
 
 
+def _optional(name: str, t: Optional[torch.Tensor], dtype: torch.dtype) -> int:
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.dim() != 1 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of one dimension on a GPU")
+    return t.data_ptr()
+
+
+class AttentionRule:
+    """A rule for `prompt_attention` and `prefix_attention`. The row of key p sees the first open_lens[i] keys of its sequence
+    (batch sequence i; also those behind p), and the keys of [max(first[row], p - window + 1), p]: `first` gives each row the
+    first key of its document (one behind p: a padding row), window 0 is none. cap: a score s becomes cap tanh(s / cap), 0: not.
+    slopes: fp32 [heads], slopes[head] |p - key| is taken from it. Index tensors are int32; the tensors stay the caller's and are
+    read by every call under the rule."""
+
+    def __init__(self, cap: float = 0.0, slopes: Optional[torch.Tensor] = None, window: int = 0,
+                 first: Optional[torch.Tensor] = None, open_lens: Optional[torch.Tensor] = None):
+        self.cap, self.window, self.slopes, self.first, self.open_lens = cap, window, slopes, first, open_lens
+        if not (cap == 0 or 2.0 ** -20 <= cap <= 2.0 ** 20):
+            raise ValueError("cap must be 0 or in [2^-20, 2^20]")
+        if not 0 <= window < 1 << 31:
+            raise ValueError("window must be in [0, 2^31)")
+        self.c = B.spd_attention_rule(cap, window, _optional("slopes", slopes, torch.float32), _optional("first", first, torch.int32),
+                                      _optional("open_lens", open_lens, torch.int32))
+
+    def check(self, rows: int, seqs: int, heads: int, gpu: int) -> "B.spd_attention_rule":
+        for name, t, n in (("slopes", self.slopes, heads), ("first", self.first, rows), ("open_lens", self.open_lens, seqs)):
+            if t is not None and (t.shape[0] != n or t.get_device() != gpu):
+                raise ValueError(f"the rule's {name} must have {n} entries on the cache's device")
+        return self.c
+
+
+class HeadRule:
+    """What `append_heads` makes of the heads of q and k: x / sqrt(mean(x^2) + eps) * gain (fp32 [head_dim]; None: as it is), then
+    the rotation of its first dims, in half layout (dims i and i + half of them) or interleaved (2i and 2i + 1)."""
+
+    def __init__(self, q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 interleaved: bool = False):
+        self.q_gain, self.k_gain, self.eps, self.interleaved = q_gain, k_gain, eps, interleaved
+        self._gains = (_optional("q_gain", q_gain, torch.float32), _optional("k_gain", k_gain, torch.float32))
+
+    def check(self, head_dim: int, gpu: int, rot: int) -> "B.spd_head_rule":
+        for name, t in (("q_gain", self.q_gain), ("k_gain", self.k_gain)):
+            if t is not None and (t.shape[0] != head_dim or t.get_device() != gpu):
+                raise ValueError(f"the rule's {name} must have {head_dim} entries on the cache's device")
+        return B.spd_head_rule(*self._gains, self.eps, rot, 1 if self.interleaved else 0)
+
+
 class PagedCache:
     """kv: [layers][pages][2][KV heads][16][head_dim] (fp32 or bf16); page_table: int32 [sequences][pages of one];
     lens: int32 [sequences]; refs: int32 [pages], or None if no call changes the pages. The tensors stay the
@@ -79,6 +127,16 @@ class PagedCache:
                rope: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Optional[torch.Tensor]:
         """Writes a batch's rows k, v [rows][KV heads][head_dim] into their pages. rope: (cos, sin), fp32
         [positions][head_dim / 2], rotates k and, if given, q [rows][heads][head_dim], which is returned (in q_out, or a new tensor)."""
+        return self._append(layer, k, v, seqs, cu_rows, q, q_out, rope, None)
+
+    def append_heads(self, layer: int, k: torch.Tensor, v: torch.Tensor, seqs: torch.Tensor, cu_rows: torch.Tensor, rule: HeadRule,
+                     q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                     rope: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Optional[torch.Tensor]:
+        """`append` with the rule's norms of the heads of k and q, and its rotation: rope is (cos, sin), fp32 [positions][half of
+        the dims that turn], the first ones of a head, a multiple of 16."""
+        return self._append(layer, k, v, seqs, cu_rows, q, q_out, rope, rule)
+
+    def _append(self, layer, k, v, seqs, cu_rows, q, q_out, rope, rule):
         rows, n = k.shape[0], self._batch(seqs, cu_rows)
         ks, vs = self._rows("k", k, rows, k.dtype, self.n_kv_heads), self._rows("v", v, rows, k.dtype, self.n_kv_heads)
         qp = op = qs = os_ = hq = 0
@@ -92,28 +150,42 @@ class PagedCache:
             qp, op = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             raise ValueError("q_out without q")
-        cos = sin = places = 0
+        cos = sin = places = half = 0
         if rope is not None:
-            places, half = rope[0].shape[0], self.head_dim // 2
+            places, half = rope[0].shape[0], self.head_dim // 2 if rule is None or rope[0].dim() != 2 else rope[0].shape[1]
             for x in rope:
                 if x.dtype is not torch.float32 or x.shape != (places, half) or x.get_device() != self._gpu or not x.is_contiguous():
                     raise ValueError("rope must be two contiguous float32 tensors [positions][head_dim / 2] on the cache's device")
             cos, sin = rope[0].data_ptr(), rope[1].data_ptr()
-        if rows:
+        if rule is not None:
+            r = rule.check(self.head_dim, self._gpu, 2 * half)
+            if rows:
+                self._on_device(lambda s: B.spd_cache_append_heads(self.c, layer, k.data_ptr(), ks, v.data_ptr(), vs, qp, qs, op, os_,
+                                                                   hq, _DTYPES[k.dtype], r, cos, sin, places, seqs.data_ptr(),
+                                                                   cu_rows.data_ptr(), n, rows, s))
+        elif rows:
             self._on_device(lambda s: B.spd_cache_append(self.c, layer, k.data_ptr(), ks, v.data_ptr(), vs, qp, qs, op, os_, hq,
                                                          _DTYPES[k.dtype], cos, sin, places, seqs.data_ptr(), cu_rows.data_ptr(),
                                                          n, rows, s))
         return q_out
 
     def prompt_attention(self, layer: int, q: torch.Tensor, seqs: torch.Tensor, cu_rows: torch.Tensor,
-                         out: Optional[torch.Tensor] = None, max_len: int = 0) -> torch.Tensor:
+                         out: Optional[torch.Tensor] = None, max_len: int = 0, rule: Optional[AttentionRule] = None) -> torch.Tensor:
         """Causal attention of a batch's packed rows q [rows][heads][head_dim], the newest keys of their sequences.
         fp32 q: any cache, fp32 arithmetic; bf16 q: a bf16 cache, and the probabilities are rounded to bf16 as the output is.
-        max_len: keys of the longest sequence, if known. Rows of `out` behind the last sequence are left as they are."""
+        max_len: keys of the longest sequence, if known. Rows of `out` behind the last sequence are left as they are.
+        rule: which keys a row sees, and what becomes of its scores (its tensors: [rows] and [sequences] of this batch)."""
         rows, n = q.shape[0], self._batch(seqs, cu_rows)
         hq, qs, out, os_ = self._query(q, rows, out)
+        r = rule.check(rows, n, hq, self._gpu) if rule is not None else None
         if rows:
             dt = _DTYPES[q.dtype]
+            if r is not None:
+                wb = self._bytes(("ruled prompt", hq, dt, n, rows, max_len), B.spd_prompt_attention_ruled_workspace)
+                ws, wp = self._workspace(wb)
+                self._on_device(lambda s: B.spd_prompt_attention_ruled(self.c, layer, q.data_ptr(), qs, out.data_ptr(), os_, hq, dt,
+                                                                       seqs.data_ptr(), cu_rows.data_ptr(), n, rows, max_len, r, wp, wb, s))
+                return out
             wb = self._bytes(("prompt", hq, dt, n, rows, max_len), B.spd_prompt_attention_workspace)
             ws, wp = self._workspace(wb)
             self._on_device(lambda s: B.spd_prompt_attention(self.c, layer, q.data_ptr(), qs, out.data_ptr(), os_, hq, dt,
@@ -122,9 +194,10 @@ class PagedCache:
 
     def prefix_attention(self, layer: int, q: torch.Tensor, seqs: torch.Tensor, cu_groups: Optional[torch.Tensor] = None,
                          prefix_lens: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-                         max_len: int = 0) -> torch.Tensor:
+                         max_len: int = 0, rule: Optional[AttentionRule] = None) -> torch.Tensor:
         """Decode attention, row i of q [sequences][heads][head_dim] over all keys of seqs[i]. Rows cu_groups[j] ..
-        cu_groups[j + 1] - 1 share their first prefix_lens[j] keys, which are read once for all of them."""
+        cu_groups[j + 1] - 1 share their first prefix_lens[j] keys, which are read once for all of them. rule: as for
+        prompt_attention, a row being a sequence's."""
         n = self._entries(seqs)
         hq, qs, out, os_ = self._query(q, n, out)
         ng = cg = pl = 0
@@ -135,6 +208,13 @@ class PagedCache:
             if ng:
                 cg, pl = cu_groups.data_ptr(), prefix_lens.data_ptr()
         dt = _DTYPES[q.dtype]
+        if rule is not None:
+            r = rule.check(n, n, hq, self._gpu)
+            wb = self._bytes(("ruled prefix", hq, dt, n, ng, max_len), B.spd_prefix_attention_ruled_workspace)
+            ws, wp = self._workspace(wb)
+            self._on_device(lambda s: B.spd_prefix_attention_ruled(self.c, layer, q.data_ptr(), qs, out.data_ptr(), os_, hq, dt,
+                                                                   seqs.data_ptr(), n, cg, pl, ng, max_len, r, wp, wb, s))
+            return out
         wb = self._bytes(("prefix", hq, dt, n, ng, max_len), B.spd_prefix_attention_workspace)
         ws, wp = self._workspace(wb)
         self._on_device(lambda s: B.spd_prefix_attention(self.c, layer, q.data_ptr(), qs, out.data_ptr(), os_, hq, dt,

@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "spd_cachefn.h"
 
@@ -484,6 +485,116 @@ __global__ __launch_bounds__(kWG) void k_append(spd_cache c, AppendArgs A) {
   }
 }
 
+// The same with norms of the heads before the rotation, and rotations of other layouts. A unit is two chunks of eight dims: the
+// rotation partners (half pairs), or two chunks that rotate within themselves (interleaved pairs) or not at all, behind the turned
+// dims. The lanes of a head join their sums of squares by moves between lanes; each row is read and written once.
+struct HeadArgs : AppendArgs {
+  const float *q_gain, *k_gain;
+  float eps;
+  int rot;
+};
+
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float x) {
+#pragma unroll
+  for (int d = 1; d < LANES; d <<= 1) x += __shfl_xor(x, d, 64);
+  return x;
+}
+
+template <typename T, typename KVT, int DH, bool PAIRS>
+__global__ __launch_bounds__(kWG) void k_append_heads(spd_cache c, HeadArgs A) {
+  constexpr int UPH = DH / 16;
+  const int r = blockIdx.x;
+  const RowAt at = row_at(c, A.seqs, A.cu_rows, A.nseqs, r);
+  if (at.seq < 0 || at.key < 0) return;
+  const int page = c.page_table[(size_t)at.seq * c.max_pages + at.key / kPage];
+  const bool own = (unsigned)page < (unsigned)c.num_pages;
+  const size_t half = (size_t)c.n_kv_heads * kPage * DH;  // a page's keys, then as many values
+  KVT* base = (KVT*)c.kv + (((size_t)A.layer * c.num_pages + (own ? page : 0)) * 2) * half + (size_t)(at.key % kPage) * DH;
+  const int nq = A.hq * UPH, nk = c.n_kv_heads * UPH, turned = A.rot / 8, reach = A.rot / 2;
+  for (int u = threadIdx.x; u < nq + 2 * nk; u += kWG) {
+    const int kind = u < nq ? 0 : u < nq + nk ? 1 : 2;
+    const int x = u - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk), h = x / UPH, m = x % UPH;
+    const bool halves = !PAIRS && 2 * m < turned;
+    const int da = halves ? m * 8 : m * 16, db = halves ? da + reach : da + 8;
+    const T* in = (kind == 0 ? (const T*)A.q + r * A.qs : kind == 1 ? (const T*)A.k + r * A.ks : (const T*)A.v + r * A.vs) + h * DH;
+    float a[8], b[8];
+    load8(in + da, a);
+    load8(in + db, b);
+    const float* gain = kind == 0 ? A.q_gain : kind == 1 ? A.k_gain : nullptr;
+    if (gain != nullptr) {
+      float ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; e++) ss = fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
+      ss = lanes_sum<UPH>(ss);
+      float f;
+      if (ss < INFINITY) {
+        f = 1.0f / sqrtf(ss * (1.0f / DH) + A.eps);
+      } else {  // squares past fp32's range: the same of rows 2^-70 as large, of which eps is nothing
+        ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          const float y = a[e] * 0x1p-70f, z = b[e] * 0x1p-70f;
+          ss = fmaf(y, y, fmaf(z, z, ss));
+        }
+        f = 0x1p-70f / sqrtf(lanes_sum<UPH>(ss) * (1.0f / DH));
+      }
+      float ga[8], gb[8];
+      load8(gain + da, ga);
+      load8(gain + db, gb);
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        a[e] = a[e] * f * ga[e];
+        b[e] = b[e] * f * gb[e];
+      }
+    }
+    if (kind < 2 && (PAIRS ? 2 * m < turned : halves)) {
+      const float *cp = A.cos + (size_t)at.key * reach + (PAIRS ? da / 2 : da), *sp = A.sin + (size_t)at.key * reach + (PAIRS ? da / 2 : da);
+      float cs[8], sn[8];
+      load8(cp, cs);
+      load8(sp, sn);
+      if constexpr (PAIRS) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const float a0 = a[2 * e], a1 = a[2 * e + 1], b0 = b[2 * e], b1 = b[2 * e + 1];
+          a[2 * e] = fmaf(a0, cs[e], -(a1 * sn[e]));
+          a[2 * e + 1] = fmaf(a1, cs[e], a0 * sn[e]);
+          b[2 * e] = fmaf(b0, cs[e + 4], -(b1 * sn[e + 4]));
+          b[2 * e + 1] = fmaf(b1, cs[e + 4], b0 * sn[e + 4]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          const float ra = fmaf(a[e], cs[e], -(b[e] * sn[e])), rb = fmaf(b[e], cs[e], a[e] * sn[e]);
+          a[e] = ra;
+          b[e] = rb;
+        }
+      }
+    }
+    if (kind == 0) {
+      T* o = (T*)A.qo + r * A.qos + h * DH;
+      store8(o + da, a);
+      store8(o + db, b);
+    } else if (own) {
+      KVT* o = base + (kind == 2 ? half : 0) + (size_t)h * kPage * DH;
+      store8(o + da, a);
+      store8(o + db, b);
+    }
+  }
+}
+
+template <typename T, typename KVT, int DH>
+void launch_heads_of(const spd_cache& c, const HeadArgs& a, bool pairs, hipStream_t s) {
+  if (pairs)
+    hipLaunchKernelGGL((k_append_heads<T, KVT, DH, true>), dim3(a.rows), dim3(kWG), 0, s, c, a);
+  else
+    hipLaunchKernelGGL((k_append_heads<T, KVT, DH, false>), dim3(a.rows), dim3(kWG), 0, s, c, a);
+}
+template <typename T, typename KVT>
+void launch_heads(const spd_cache& c, const HeadArgs& a, bool pairs, hipStream_t s) {
+  c.head_dim == 128 ? launch_heads_of<T, KVT, 128>(c, a, pairs, s) : launch_heads_of<T, KVT, 64>(c, a, pairs, s);
+}
+
 template <typename T, typename KVT>
 void launch_append(const spd_cache& c, const AppendArgs& a, hipStream_t s) {
   if (c.head_dim == 128)
@@ -504,6 +615,36 @@ spd_status check_change(const char* call, const spd_cache* c, std::initializer_l
   for (const void* p : arrays)
     if (!p || misaligned(p, 4)) return invalid(call, "NULL or misaligned pointer");
   if (n < 1 || n > c->max_seqs) return invalid(call, "n must be in [1, max_seqs]");
+  return SPD_OK;
+}
+
+// What both appends check but for the rotation.
+spd_status check_append(const char* call, const spd_cache* c, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                        int64_t v_stride, const void* q, int64_t q_stride, const void* q_out, int64_t q_out_stride,
+                        int32_t n_q_heads, int32_t dtype, const int32_t* seqs, const int32_t* cu_rows, int32_t nseqs, int32_t rows) {
+  spd_status st = check_cache(call, c, false);
+  if (st != SPD_OK) return st;
+  if (dtype != SPD_F32 && dtype != SPD_BF16) return invalid(call, "dtype must be SPD_F32 or SPD_BF16");
+  if (layer < 0 || layer >= c->n_layers) return invalid(call, "no such layer");
+  if (!seqs || !cu_rows || misaligned(seqs, 4) || misaligned(cu_rows, 4)) return invalid(call, "NULL or misaligned pointer");
+  if (nseqs < 1 || nseqs > c->max_seqs) return invalid(call, "nseqs must be in [1, max_seqs]");
+  if (rows < 0 || rows >= 1 << 24) return invalid(call, "rows must be in [0, 2^24)");
+  if ((st = check_rows(call, k, k_stride, c->n_kv_heads, c->head_dim, dtype)) != SPD_OK) return st;
+  if ((st = check_rows(call, v, v_stride, c->n_kv_heads, c->head_dim, dtype)) != SPD_OK) return st;
+  if (n_q_heads < 0 || n_q_heads > 16384 || (n_q_heads == 0) != (q == nullptr) || (q == nullptr) != (q_out == nullptr))
+    return invalid(call, "q and q_out come with n_q_heads in [1, 16384], or are NULL with n_q_heads 0");
+  if (q) {
+    if ((st = check_rows(call, q, q_stride, n_q_heads, c->head_dim, dtype)) != SPD_OK) return st;
+    if ((st = check_rows(call, q_out, q_out_stride, n_q_heads, c->head_dim, dtype)) != SPD_OK) return st;
+  }
+  return SPD_OK;
+}
+
+spd_status check_rope(const char* call, const spd_cache* c, const float* rope_cos, const float* rope_sin, int32_t rope_positions) {
+  if ((rope_cos == nullptr) != (rope_sin == nullptr)) return invalid(call, "cos and sin come together");
+  if (misaligned(rope_cos, 16) || misaligned(rope_sin, 16)) return invalid(call, "cos and sin must be 16-byte aligned");
+  if (rope_cos ? rope_positions < kPage * c->max_pages : rope_positions != 0)
+    return invalid(call, "rope_positions must be at least 16 * max_pages (0 without cos and sin)");
   return SPD_OK;
 }
 
@@ -577,25 +718,10 @@ extern "C" spd_status spd_cache_append(const spd_cache* c, int32_t layer, const 
                                        int32_t rope_positions, const int32_t* seqs, const int32_t* cu_rows, int32_t nseqs,
                                        int32_t rows, void* stream) {
   const char* call = "cache append";
-  spd_status st = check_cache(call, c, false);
+  spd_status st = check_append(call, c, layer, k, k_stride, v, v_stride, q, q_stride, q_out, q_out_stride, n_q_heads, dtype, seqs,
+                               cu_rows, nseqs, rows);
+  if (st == SPD_OK) st = check_rope(call, c, rope_cos, rope_sin, rope_positions);
   if (st != SPD_OK) return st;
-  if (dtype != SPD_F32 && dtype != SPD_BF16) return invalid(call, "dtype must be SPD_F32 or SPD_BF16");
-  if (layer < 0 || layer >= c->n_layers) return invalid(call, "no such layer");
-  if (!seqs || !cu_rows || misaligned(seqs, 4) || misaligned(cu_rows, 4)) return invalid(call, "NULL or misaligned pointer");
-  if (nseqs < 1 || nseqs > c->max_seqs) return invalid(call, "nseqs must be in [1, max_seqs]");
-  if (rows < 0 || rows >= 1 << 24) return invalid(call, "rows must be in [0, 2^24)");
-  if ((st = check_rows(call, k, k_stride, c->n_kv_heads, c->head_dim, dtype)) != SPD_OK) return st;
-  if ((st = check_rows(call, v, v_stride, c->n_kv_heads, c->head_dim, dtype)) != SPD_OK) return st;
-  if (n_q_heads < 0 || n_q_heads > 16384 || (n_q_heads == 0) != (q == nullptr) || (q == nullptr) != (q_out == nullptr))
-    return invalid(call, "q and q_out come with n_q_heads in [1, 16384], or are NULL with n_q_heads 0");
-  if (q) {
-    if ((st = check_rows(call, q, q_stride, n_q_heads, c->head_dim, dtype)) != SPD_OK) return st;
-    if ((st = check_rows(call, q_out, q_out_stride, n_q_heads, c->head_dim, dtype)) != SPD_OK) return st;
-  }
-  if ((rope_cos == nullptr) != (rope_sin == nullptr)) return invalid(call, "cos and sin come together");
-  if (misaligned(rope_cos, 16) || misaligned(rope_sin, 16)) return invalid(call, "cos and sin must be 16-byte aligned");
-  if (rope_cos ? rope_positions < kPage * c->max_pages : rope_positions != 0)
-    return invalid(call, "rope_positions must be at least 16 * max_pages (0 without cos and sin)");
   if (rows == 0) return SPD_OK;
   if (q && q == q_out && q_stride != q_out_stride && rows > 1) return invalid(call, "q_out may be q with the same stride only");
   const AppendArgs a{k, v, q, q_out, k_stride, v_stride, q_stride, q_out_stride, rope_cos, rope_sin, seqs, cu_rows, layer,
@@ -605,5 +731,37 @@ extern "C" spd_status spd_cache_append(const spd_cache* c, int32_t layer, const 
     c->dtype == SPD_BF16 ? launch_append<uint16_t, uint16_t>(*c, a, s) : launch_append<uint16_t, float>(*c, a, s);
   else
     c->dtype == SPD_BF16 ? launch_append<float, uint16_t>(*c, a, s) : launch_append<float, float>(*c, a, s);
+  return check_launch(call);
+}
+
+extern "C" spd_status spd_cache_append_heads(const spd_cache* c, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                                             int64_t v_stride, const void* q, int64_t q_stride, void* q_out,
+                                             int64_t q_out_stride, int32_t n_q_heads, int32_t dtype, const spd_head_rule* rule,
+                                             const float* rope_cos, const float* rope_sin, int32_t rope_positions,
+                                             const int32_t* seqs, const int32_t* cu_rows, int32_t nseqs, int32_t rows,
+                                             void* stream) {
+  const char* call = "cache append of heads";
+  spd_status st = check_append(call, c, layer, k, k_stride, v, v_stride, q, q_stride, q_out, q_out_stride, n_q_heads, dtype, seqs,
+                               cu_rows, nseqs, rows);
+  if (st == SPD_OK) st = check_rope(call, c, rope_cos, rope_sin, rope_positions);
+  if (st != SPD_OK) return st;
+  if (!rule) return invalid(call, "NULL rule");
+  if (misaligned(rule->q_gain, 16) || misaligned(rule->k_gain, 16)) return invalid(call, "gains must be 16-byte aligned");
+  if (rule->q_gain && !q) return invalid(call, "a gain of queries without queries");
+  if ((rule->q_gain || rule->k_gain) && !(rule->eps > 0.f && std::isfinite(rule->eps))) return invalid(call, "eps must be finite and above 0");
+  if (rule->rot < 0 || rule->rot % 16 || rule->rot > c->head_dim || (rule->rot > 0) != (rope_cos != nullptr))
+    return invalid(call, "rot must be a multiple of 16 up to head_dim with cos and sin, 0 without");
+  if (rule->interleaved != 0 && rule->interleaved != 1) return invalid(call, "interleaved must be 0 or 1");
+  if (rows == 0) return SPD_OK;
+  if (q && q == q_out && q_stride != q_out_stride && rows > 1) return invalid(call, "q_out may be q with the same stride only");
+  const HeadArgs a{AppendArgs{k, v, q, q_out, k_stride, v_stride, q_stride, q_out_stride, rope_cos, rope_sin, seqs, cu_rows, layer,
+                              n_q_heads, nseqs, rows},
+                   rule->q_gain, rule->k_gain, rule->eps, rule->rot};
+  const bool pairs = rule->interleaved != 0;
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == SPD_BF16)
+    c->dtype == SPD_BF16 ? launch_heads<uint16_t, uint16_t>(*c, a, pairs, s) : launch_heads<uint16_t, float>(*c, a, pairs, s);
+  else
+    c->dtype == SPD_BF16 ? launch_heads<float, uint16_t>(*c, a, pairs, s) : launch_heads<float, float>(*c, a, pairs, s);
   return check_launch(call);
 }

@@ -1,0 +1,110 @@
+// What a rule makes of the attention over a cache of several sequences: which keys a row sees, and what becomes of a score.
+// The row of key p sees the first `open` keys of its sequence, and those of [lo, p] with lo = max(first[row], p - window + 1). A
+// score s = scale q.k becomes cap tanh(s / cap), less slope |p - key|.
+#pragma once
+#include "spd_cachefn.h"
+
+namespace spd {
+namespace {
+
+// Parts of a rule that a kernel is made for: keys unseen (all rules), capped scores, scores lowered with the distance.
+enum { RULE_KEYS = 1, RULE_CAP = 2, RULE_SLOPES = 4 };
+
+struct RuleArgs {
+  float cap;
+  int window;
+  const float* slopes;
+  const int *first, *open;
+};
+
+// Keys below `open` and keys of [lo, lim).
+struct Sight {
+  int lo, lim, open;
+};
+
+// Of a row that stands for key p; before the first key it sees nothing.
+__device__ __forceinline__ Sight sight_of(const RuleArgs& R, int row, int p, int open) {
+  if (p < 0) return Sight{0, 0, 0};
+  int lo = R.first != nullptr ? max(R.first[row], 0) : 0;
+  if (R.window > 0) lo = max(lo, p - R.window + 1);
+  return Sight{min(lo, p + 1), p + 1, open};
+}
+
+__device__ __forceinline__ int open_of(const RuleArgs& R, int i, int len) {
+  return R.open != nullptr ? min(max(R.open[i], 0), max(len, 0)) : 0;
+}
+
+// What some row of `rows` sees: of [lo, lim), and below open. key(r), open(r): of row row0 + r.
+template <typename K, typename O>
+__device__ __forceinline__ Sight sight_of_rows(const RuleArgs& R, int row0, int rows, K key, O open) {
+  Sight h{0x7fffffff, 0, 0};
+  if (R.first == nullptr && R.window <= 0) h.lo = 0;
+#pragma unroll 8
+  for (int r = 0; r < rows; r++) {
+    const Sight s = sight_of(R, row0 + r, key(r), open(r));
+    h.open = max(h.open, s.open);
+    if (s.lo >= s.lim) continue;
+    h.lo = min(h.lo, s.lo);
+    h.lim = max(h.lim, s.lim);
+  }
+  return h;
+}
+
+// The keys [a, b) without those that no row sees: keys before `a` or behind `b` are dropped, and a run of them between the open keys
+// and the others is a gap. Keys are counted without it: c stands for key c, from gap_at on for key c + gap. gap_at lies whole tiles
+// of 64 keys behind the page of a, and gap is whole pages, so that no tile has keys of both sides.
+struct Keys {
+  int a, b, gap_at, gap;
+};
+__device__ __forceinline__ Keys keys_of(int a, int b, const Sight& h) {
+  Keys k{a, b, 0x7fffffff, 0};
+  const int open = min(b, h.open), lo = max(a, h.lo), lim = min(b, h.lim);
+  if (lim <= lo) {
+    k.b = max(a, open);
+  } else if (open <= a) {
+    k.a = lo;
+    k.b = lim;
+  } else {
+    const int start = a & ~(kPage - 1), at = start + (open - start + 63) / 64 * 64, to = lo & ~(kPage - 1);
+    k.b = max(open, lim);
+    if (to > at) {
+      k.gap_at = at;
+      k.gap = to - at;
+      k.b -= k.gap;
+    }
+  }
+  return k;
+}
+
+// tanh(x), as spd_ruleattn.hip computes it.
+template <int RL>
+__device__ float tanh_of(float x);
+
+// A row's part of a rule, of one head. In units of log2: a score s becomes top tanh(s to_x) - slope |center - key|. The distance
+// is measured from the nearest key that the row sees (its own one, or the last open one): the softmax is the same, and rows that
+// see far keys alone keep their scores' bits. RL 0: the keys below lim.
+template <int RL>
+struct RowRule {
+  int lo, lim, open, center;
+  float top, to_x, slope;
+  __device__ __forceinline__ bool sees(int key) const { return key < open || (key >= lo && key < lim); }
+  // some key of [a, b)
+  __device__ __forceinline__ bool sees_any(int a, int b) const { return (b > a && a < open) || max(a, lo) < min(b, lim); }
+  __device__ __forceinline__ float distance(int key) const { return fabsf((float)(center - key)); }
+  // to: from s to units of log2
+  __device__ __forceinline__ float shaped(float s, float to, int key) const {
+    float e = s * to;
+    if constexpr ((RL & RULE_CAP) != 0) e = top * tanh_of<RL>(e * to_x);
+    if constexpr ((RL & RULE_SLOPES) != 0) e = fmaf(-slope, distance(key), e);
+    return e;
+  }
+};
+template <>
+struct RowRule<0> {
+  int lim;
+  __device__ __forceinline__ bool sees(int key) const { return key < lim; }
+  __device__ __forceinline__ bool sees_any(int a, int) const { return lim > a; }
+};
+
+}  // namespace
+}  // namespace spd

@@ -1,0 +1,115 @@
+// Attention over a cache of several sequences under a rule (spd_rule.h): its calls.
+#include "spd_seqattn.h"
+
+namespace spd {
+namespace {
+
+// tanh to 2^-22 of itself: below kTanhPoly a polynomial of x^2 (fitted to the least largest relative error, 9e-10; above it 1 - 2 / (1 +
+// e^2x) loses at most a bit.
+constexpr float kTanhPoly = 0.55f;
+template <int RL>
+__device__ __forceinline__ float tanh_of(float x) {
+  const float y = x * x;
+  float p = -0.00627423963f;
+  p = fmaf(y, p, 0.0210716799f);
+  p = fmaf(y, p, -0.0538523085f);
+  p = fmaf(y, p, 0.13332586f);
+  p = fmaf(y, p, -0.333333164f);
+  const float small = fmaf(x * y, p, x), t = __builtin_amdgcn_exp2f(fabsf(x) * 2.88539008177792681f);
+  const float big = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + t), 1.0f);
+  return fabsf(x) < kTanhPoly ? small : copysignf(big, x);
+}
+
+spd_status check_rule(const char* call, const spd_attention_rule* r) {
+  if (!r) return invalid(call, "NULL rule");
+  if (r->cap != 0.f && !(r->cap >= 0x1p-20f && r->cap <= 0x1p20f)) return invalid(call, "cap must be 0 or in [2^-20, 2^20]");
+  if (r->window < 0) return invalid(call, "window must not be negative");
+  if (misaligned(r->slopes, 4) || misaligned(r->first, 4) || misaligned(r->open_lens, 4)) return invalid(call, "misaligned pointer");
+  return SPD_OK;
+}
+
+// The kernels of a rule's parts.
+void run_ruled(const SeqArgs& plain, const spd_attention_rule& r, int dtype, const Request& q, bool prefix, void* workspace,
+               hipStream_t s) {
+  RuledSeqArgs a{plain, RuleArgs{r.cap, r.window, r.slopes, r.first, r.open_lens}};
+  if (r.cap != 0.f)
+    r.slopes ? run_attention<RULE_KEYS | RULE_CAP | RULE_SLOPES>(a, dtype, q, prefix, workspace, s)
+             : run_attention<RULE_KEYS | RULE_CAP>(a, dtype, q, prefix, workspace, s);
+  else
+    r.slopes ? run_attention<RULE_KEYS | RULE_SLOPES>(a, dtype, q, prefix, workspace, s)
+             : run_attention<RULE_KEYS>(a, dtype, q, prefix, workspace, s);
+}
+
+}  // namespace
+}  // namespace spd
+
+using namespace spd;
+
+extern "C" spd_status spd_prompt_attention_ruled_workspace(const spd_cache* c, int32_t n_q_heads, int32_t dtype, int32_t nseqs,
+                                                           int32_t rows, int32_t max_len, size_t* bytes) {
+  const char* call = "ruled prompt attention workspace";
+  const spd_status st = check_sizes(call, c, n_q_heads, dtype, nseqs, max_len);
+  if (st != SPD_OK) return st;
+  if (!bytes || rows < 0) return invalid(call, "NULL pointer or negative rows");
+  const Request q = request(*c, n_q_heads, nseqs, rows, 0, max_len, false, true);
+  if (q.items * c->n_kv_heads > kMaxWGs) return invalid(call, "more rows than one launch takes (2^24 tiles of 128 queries, with all KV heads)");
+  *bytes = q.bytes;
+  return SPD_OK;
+}
+
+extern "C" spd_status spd_prompt_attention_ruled(const spd_cache* c, int32_t layer, const void* q, int64_t q_stride, void* out,
+                                                 int64_t out_stride, int32_t n_q_heads, int32_t dtype, const int32_t* seqs,
+                                                 const int32_t* cu_rows, int32_t nseqs, int32_t rows, int32_t max_len,
+                                                 const spd_attention_rule* rule, void* workspace, size_t ws_bytes, void* stream) {
+  const char* call = "ruled prompt attention";
+  spd_status st = check_sizes(call, c, n_q_heads, dtype, nseqs, max_len);
+  if (st == SPD_OK) st = check_call(call, c, layer, q, q_stride, out, out_stride, n_q_heads, dtype, seqs);
+  if (st == SPD_OK) st = check_rule(call, rule);
+  if (st != SPD_OK) return st;
+  if (!cu_rows || misaligned(cu_rows, 4)) return invalid(call, "NULL or misaligned pointer");
+  if (rows < 0) return invalid(call, "rows must not be negative");
+  size_t need = 0;
+  if ((st = spd_prompt_attention_ruled_workspace(c, n_q_heads, dtype, nseqs, rows, max_len, &need)) != SPD_OK) return st;
+  if ((st = check_workspace(call, workspace, ws_bytes, need)) != SPD_OK) return st;
+  if (rows == 0) return SPD_OK;
+  SeqArgs a = args_of(c, layer, q, q_stride, out, out_stride, n_q_heads, seqs, nseqs);
+  a.cu = cu_rows;
+  a.rows = rows;
+  run_ruled(a, *rule, dtype, request(*c, n_q_heads, nseqs, rows, 0, max_len, false, true), false, workspace, (hipStream_t)stream);
+  return check_launch(call);
+}
+
+extern "C" spd_status spd_prefix_attention_ruled_workspace(const spd_cache* c, int32_t n_q_heads, int32_t dtype, int32_t nseqs,
+                                                           int32_t ngroups, int32_t max_len, size_t* bytes) {
+  const char* call = "ruled prefix attention workspace";
+  const spd_status st = check_sizes(call, c, n_q_heads, dtype, nseqs, max_len);
+  if (st != SPD_OK) return st;
+  if (nseqs > 4096) return invalid(call, "nseqs must be at most 4096");
+  if (!bytes || ngroups < 0 || ngroups > nseqs) return invalid(call, "NULL pointer, or ngroups outside [0, nseqs]");
+  *bytes = request(*c, n_q_heads, nseqs, nseqs, ngroups, max_len, true, true).bytes;
+  return SPD_OK;
+}
+
+extern "C" spd_status spd_prefix_attention_ruled(const spd_cache* c, int32_t layer, const void* q, int64_t q_stride, void* out,
+                                                 int64_t out_stride, int32_t n_q_heads, int32_t dtype, const int32_t* seqs,
+                                                 int32_t nseqs, const int32_t* cu_groups, const int32_t* prefix_lens,
+                                                 int32_t ngroups, int32_t max_len, const spd_attention_rule* rule, void* workspace,
+                                                 size_t ws_bytes, void* stream) {
+  const char* call = "ruled prefix attention";
+  size_t need = 0;
+  spd_status st = spd_prefix_attention_ruled_workspace(c, n_q_heads, dtype, nseqs, ngroups, max_len, &need);
+  if (st == SPD_OK) st = check_call(call, c, layer, q, q_stride, out, out_stride, n_q_heads, dtype, seqs);
+  if (st == SPD_OK) st = check_rule(call, rule);
+  if (st != SPD_OK) return st;
+  if ((ngroups > 0) != (cu_groups != nullptr) || (ngroups > 0) != (prefix_lens != nullptr))
+    return invalid(call, "cu_groups and prefix_lens come with ngroups > 0, or are NULL with 0");
+  if (misaligned(cu_groups, 4) || misaligned(prefix_lens, 4)) return invalid(call, "misaligned pointer");
+  if ((st = check_workspace(call, workspace, ws_bytes, need)) != SPD_OK) return st;
+  SeqArgs a = args_of(c, layer, q, q_stride, out, out_stride, n_q_heads, seqs, nseqs);
+  a.cu = cu_groups;
+  a.prefix = prefix_lens;
+  a.ngroups = ngroups;
+  a.rows = nseqs;
+  run_ruled(a, *rule, dtype, request(*c, n_q_heads, nseqs, nseqs, ngroups, max_len, true, true), true, workspace, (hipStream_t)stream);
+  return check_launch(call);
+}
