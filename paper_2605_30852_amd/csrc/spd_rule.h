@@ -10,11 +10,15 @@ namespace {
 // Parts of a rule that a kernel is made for: keys unseen (all rules), capped scores, scores lowered with the distance.
 enum { RULE_KEYS = 1, RULE_CAP = 2, RULE_SLOPES = 4 };
 
+constexpr int kTanhTerms = 7;  // of fp32 queries; 5 of bf16 ones
+
 struct RuleArgs {
   float cap;
   int window;
   const float* slopes;
   const int *first, *open;
+  // Of products S up to `limit`, top tanh(S / (top to)) = S (c[0] + y (c[1] + ...)), y = S^2, in units of log2 (scaled_poly)
+  float limit, c[kTanhTerms];
 };
 
 // Keys below `open` and keys of [lo, lim).
@@ -90,12 +94,11 @@ struct RowRule {
   __device__ __forceinline__ bool sees(int key) const { return key < open || (key >= lo && key < lim); }
   // some key of [a, b)
   __device__ __forceinline__ bool sees_any(int a, int b) const { return (b > a && a < open) || max(a, lo) < min(b, lim); }
-  __device__ __forceinline__ float distance(int key) const { return fabsf((float)(center - key)); }
-  // to: from s to units of log2
-  __device__ __forceinline__ float shaped(float s, float to, int key) const {
+  // to: from s to units of log2; distance: center - key
+  __device__ __forceinline__ float shaped(float s, float to, float distance) const {
     float e = s * to;
     if constexpr ((RL & RULE_CAP) != 0) e = top * tanh_of<RL>(e * to_x);
-    if constexpr ((RL & RULE_SLOPES) != 0) e = fmaf(-slope, distance(key), e);
+    if constexpr ((RL & RULE_SLOPES) != 0) e = fmaf(-slope, fabsf(distance), e);
     return e;
   }
 };

@@ -67,7 +67,7 @@ __device__ bool plain_query(const spd_cache& c, const KVT* pool, const int* tabl
 #pragma unroll
       for (int e = 0; e < 8; e++) s = fmaf(x[e] * scale, f[e], s);
     }
-    if constexpr (RL != 0) s = rule.shaped(s, kLog2e, key) * (1.0f / kLog2e);
+    if constexpr (RL != 0) s = rule.shaped(s, kLog2e, (float)(rule.center - key)) * (1.0f / kLog2e);
     return s;
   };
   float m = -INFINITY;
@@ -692,10 +692,24 @@ __device__ __forceinline__ Span span_of(const ItemOf<RL>& it) {
   }
 }
 
+// What a lane's row sees of a piece's tile, its keys counted from key k on: a comparison with a number is one instruction, and needs no
+// register for the key.
+template <int RL>
+struct TileSight {
+  int a, lo, lim, open;
+  __device__ __forceinline__ TileSight(const RowRule<RL>& r, const Span& keys, int k)
+      : a(keys.a - k), lo(r.lo - k), lim(min(r.lim, keys.b) - k), open(min(r.open, keys.b) - k) {}
+  __device__ __forceinline__ bool sees(int i) const { return i >= a && (i < open || (i >= lo && i < lim)); }
+};
+template <>
+struct TileSight<0> {
+  __device__ __forceinline__ TileSight(const RowRule<0>&, const Span&, int) {}
+};
+
 // The keys that the queries of some lanes see: tiles of n keys from k on that all of them see whole, or none of them any key of.
 template <int LANES>
 struct WaveRule {
-  int lo_min, lo_max, lim_min, lim_max, open_min, open_max;
+  int lo_min, lo_max, lim_min, lim_max, open_min, open_max, center_min;
   template <int RL>
   __device__ __forceinline__ void set(const RowRule<RL>& r) {
     lo_min = r.lo < r.lim ? r.lo : 0x7fffffff;
@@ -703,6 +717,7 @@ struct WaveRule {
     lo_max = r.lo;
     lim_min = r.lim;
     open_min = open_max = r.open;
+    center_min = r.center;
   }
   __device__ __forceinline__ void join() {
 #pragma unroll
@@ -713,6 +728,7 @@ struct WaveRule {
       lim_max = max(lim_max, __shfl_xor(lim_max, d, 64));
       open_min = min(open_min, __shfl_xor(open_min, d, 64));
       open_max = max(open_max, __shfl_xor(open_max, d, 64));
+      center_min = min(center_min, __shfl_xor(center_min, d, 64));
     }
     lo_min = __builtin_amdgcn_readfirstlane(lo_min);
     lo_max = __builtin_amdgcn_readfirstlane(lo_max);
@@ -720,10 +736,79 @@ struct WaveRule {
     lim_max = __builtin_amdgcn_readfirstlane(lim_max);
     open_min = __builtin_amdgcn_readfirstlane(open_min);
     open_max = __builtin_amdgcn_readfirstlane(open_max);
+    center_min = __builtin_amdgcn_readfirstlane(center_min);
   }
   __device__ __forceinline__ bool none(int k, int n) const { return k >= open_max && (k >= lim_max || k + n <= lo_min); }
   __device__ __forceinline__ bool whole(int k, int n) const { return k + n <= open_min || (k >= lo_max && k + n <= lim_min); }
+  // no key that is seen lies behind its row's center
+  __device__ __forceinline__ bool one_side(int k, int n) const { return k + n <= center_min + 1 || k >= open_max; }
 };
+
+// a n + b with n in the instruction: as constants in registers the n of a tile would take as many as its scores.
+template <int RL>
+__device__ __forceinline__ float multiple_plus(float a, float n, float b) {
+  float r;
+  asm("v_fmamk_f32 %0, %1, %3, %2" : "=v"(r) : "v"(a), "v"(b), "n"(__builtin_bit_cast(int, n)));
+  return r;
+}
+
+// A tile's products S of a lane's query become exponents less `off`: top tanh, and less slope times the distance. at(i): the
+// tile's key of product i, from key k of the lane's on; to: from S to units of log2. Where every key's distance counts down to the
+// center and every |S| is within the polynomial's range, which nearly all tiles are, this takes a multiplication and TERMS FMAs a
+// score for the cap and one instruction more for the distance; else the general formula. Scores are done four at a time: all at once
+// would take more registers than there are.
+template <int RL, int TERMS, int W, typename V, int NV, typename At>
+__device__ __forceinline__ void shape(V (&s)[NV], const RuleArgs& R, const RowRule<RL>& rule, float to, int k, bool one_side, float off, At at) {
+  constexpr int N = W * NV;
+  const float away = (RL & RULE_SLOPES) != 0 ? (float)(rule.center - k) : 0.f;
+  bool usual = true;
+  if constexpr ((RL & RULE_SLOPES) != 0) usual = one_side;
+  if constexpr ((RL & RULE_CAP) != 0) {
+    float far = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) far = fmaxf(fmaxf(far, fabsf(s[i / W][i % W])), fabsf(s[(i + 1) / W][(i + 1) % W]));
+    usual = usual && !__any(far > R.limit);
+  }
+  if (usual) {
+    float base = -off;
+    [[maybe_unused]] float step[4];  // slope times 0 .. 3
+    if constexpr ((RL & RULE_SLOPES) != 0) {
+      base = fmaf(-rule.slope, away, -off);
+#pragma unroll
+      for (int j = 1; j < 4; j++) step[j] = rule.slope * (float)j;
+    }
+#pragma unroll
+    for (int i0 = 0; i0 < N; i0 += 4) {  // four keys one after the other
+      float e[4], from = base;
+      if constexpr ((RL & RULE_SLOPES) != 0) from = multiple_plus<RL>(rule.slope, (float)at(i0), base);
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        float add = from;
+        if constexpr ((RL & RULE_SLOPES) != 0) add = i > 0 ? from + step[i] : from;
+        const float x = s[i0 / W][i0 % W + i];
+        if constexpr ((RL & RULE_CAP) != 0) {
+          const float y = x * x;
+          float t = R.c[TERMS - 1];
+#pragma unroll
+          for (int j = TERMS - 2; j >= 0; j--) t = fmaf(y, t, R.c[j]);
+          e[i] = fmaf(x, t, add);
+        } else {
+          e[i] = fmaf(x, to, add);
+        }
+      }
+      asm volatile("" : "+v"(e[0]), "+v"(e[1]), "+v"(e[2]), "+v"(e[3]));
+#pragma unroll
+      for (int i = 0; i < 4; i++) s[i0 / W][i0 % W + i] = e[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      float e = rule.shaped(s[i / W][i % W], to, away - (float)at(i)) - off;
+      asm volatile("" : "+v"(e));
+      s[i / W][i % W] = e;
+    }
+  }
+}
 
 // Query j of a piece again, in plain arithmetic, in the place of its result.
 template <typename T, typename KVT, int DH, int RL>
@@ -837,11 +922,15 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
   const int* table = C.page_table + (size_t)it.table * C.max_pages;
   // The pages of a tile, one a lane (mod their number), are read a tile ahead of their use, and looked at only there: a look
   // at them here would wait for them and for the keys requested before them.
-  auto pages = [&](int t) { return table[min(key_of<RL>(it, start + t * KT) / kPage + (lane & (KT / kPage - 1)), last / kPage)]; };
+  // The first key of the t-th tile. Scores that fall with the distance are taken from the last tile down, which has the largest ones:
+  // from the first up, a steep slope renews the offset at every tile.
+  auto tile_key = [&](int t) { return key_of<RL>(it, start + ((RL & RULE_SLOPES) != 0 ? max(tiles - 1 - t, 0) : t) * KT); };
+  auto pages = [&](int t) { return table[min(tile_key(t) / kPage + (lane & (KT / kPage - 1)), last / kPage)]; };
   const int pg0 = tiles > 0 ? pages(0) : 0;
   int pg = tiles > 0 ? pages(1) : 0;
   const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;  // from products to scores in units of log2
-  const float to = (RL & (RULE_CAP | RULE_SLOPES)) != 0 ? 1.0f : sc;  // from scores to exponents
+  constexpr bool SHAPED = (RL & (RULE_CAP | RULE_SLOPES)) != 0;
+  const float to = SHAPED ? 1.0f : sc;  // from scores to exponents
   const bool active = w * 32 < nq;
   const int jq = w * 32 + col, jj = min(jq, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
   RowRule<RL> rule = row_rule<RL>(A, it, row, head);
@@ -875,7 +964,7 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
   // Tile t. Keys outside [k0, k1) are read as the nearest one inside: their probability is 0, and 0 times a value must be 0. The
   // pages go to scalar registers first: looked at between loads, a lane's register would wait for those before it.
   auto request = [&](int t, int pg) {
-    const int first = key_of<RL>(it, start + t * KT), to = (t & 1) * 2 * KBUF;
+    const int first = tile_key(t), to = (t & 1) * 2 * KBUF;
     int page[LPT];
 #pragma unroll
     for (int i = 0; i < LPT; i++) page[i] = page_to_read(C, __builtin_amdgcn_readlane(pg, (i * kWG + w * 64) / (NCH * kPage)));
@@ -888,7 +977,8 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
       __builtin_amdgcn_global_load_lds(p + half * sizeof(uint16_t) + (at + voff), l + KBUF, 16, 0, 0);
     }
   };
-  // A lane's bytes of a K or V tile.
+  // A lane's bytes of a K or V tile. Chunk 2 k + h differs from chunk h in bits that the row has not: under a rule, whose parts need the
+  // registers, one XOR in a step stands for an address in each.
   uint32_t ka[KS], va[NT];
 #pragma unroll
   for (int k = 0; k < KS; k++) ka[k] = col * DH * 2 + (((2 * k + h) ^ (col >> KROT) % NCH) << 4);
@@ -903,11 +993,12 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
 #pragma unroll
   for (int t = 0; t < NT; t++) o[t] = (f32x16)(0.f);
   float m_run = -INFINITY, l_run = 0.f;
+  [[maybe_unused]] float off_run = 0.f, bound = -INFINITY;  // SHAPED: what the exponents are less, and from where on it is renewed
 
   if (tiles > 0) request(0, pg0);
   for (int t = 0; t < tiles; t++) {
     const char* tile = lds + (t & 1) * 2 * KBUF;
-    const int kb = key_of<RL>(it, start + t * KT);  // the tile's first key
+    const int kb = tile_key(t);  // the tile's first key
     // tile t has landed, every wave's part of it, and every wave is done with the one before
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     bool none = kb >= wmax;
@@ -919,12 +1010,15 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
       }
       continue;
     }
+    if constexpr (RL != 0) asm volatile("" : "+v"(ka[0]), "+v"(va[0]));  // the others come from these, in the step
+    auto k_at = [&](int k) { return RL != 0 ? ka[0] ^ (uint32_t)(k << 5) : ka[k]; };
+    auto v_at = [&](int tt) { return RL != 0 ? va[0] ^ (uint32_t)(tt << 6) : va[tt]; };
     f32x16 s[SB];
 #pragma unroll
     for (int x = 0; x < SB; x++)
 #pragma unroll
       for (int k = 0; k < KS; k++) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + ka[k] + x * 32 * DH * 2);
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + k_at(k) + x * 32 * DH * 2);
 #pragma unroll
         for (int p = NP - 1; p >= 0; p--)
           s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[p][k], (p == NP - 1 && k == 0) ? (f32x16)(0.f) : s[x], 0, 0, 0);
@@ -939,7 +1033,7 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
           union { bf16x4 q[2]; bf16x8 f; } u;
 #pragma unroll
           for (int y = 0; y < 2; y++)
-            u.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lbf16x4*)(lbytes*)(tile + va[tt] + (x * 32 + ks * 16 + y * 8) * DH * 2));
+            u.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lbf16x4*)(lbytes*)(tile + v_at(tt) + (x * 32 + ks * 16 + y * 8) * DH * 2));
           vf[x][ks][tt] = u.f;
         }
     // the keys' fragments half a block ahead of their products, the values' among the last products
@@ -960,23 +1054,22 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
       request(t + 1, pg);
       pg = pages(t + 2);
     }
-    if constexpr ((RL & (RULE_CAP | RULE_SLOPES)) != 0) {
-#pragma unroll
-      for (int x = 0; x < SB; x++)
-#pragma unroll
-        for (int v = 0; v < 16; v++) s[x][v] = rule.shaped(s[x][v], sc, kb + x * 32 + 8 * (v >> 2) + 4 * h + (v & 3));
+    if constexpr (SHAPED) {
+      shape<RL, NP == 1 ? 5 : 7, 16>(s, A.rule, rule, sc, kb + 4 * h, seen.one_side(kb, KT), off_run,
+                                     [](int i) { return (i >> 4) * 32 + 8 * (i >> 2 & 3) + (i & 3); });
     }
     bool part = kb < keys.a || kb + KT > wmin;  // some key is not every query's
     if constexpr (RL != 0) part = kb < keys.a || kb + KT > keys.b || !seen.whole(kb, KT);
     if (part) {
+      const TileSight<RL> hides(rule, keys, kb + 4 * h);
       asm volatile("");  // stays a branch: the masks cost as much as a third of the step's vector work
 #pragma unroll
       for (int x = 0; x < SB; x++)
 #pragma unroll
         for (int v = 0; v < 16; v++) {
-          const int kk = kb + x * 32 + 8 * (v >> 2) + 4 * h + (v & 3);
+          const int i = x * 32 + 8 * (v >> 2) + (v & 3), kk = kb + i + 4 * h;
           bool is = kk < lim && kk >= keys.a;
-          if constexpr (RL != 0) is = rule.sees(kk) && kk >= keys.a && kk < keys.b;
+          if constexpr (RL != 0) is = hides.sees(i);
           s[x][v] = is ? s[x][v] : -INFINITY;
         }
     }
@@ -986,7 +1079,48 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
 #pragma unroll
       for (int v = 0; v < 16; v += 2) mx = fmaxf(fmaxf(mx, s[x][v]), s[x][v + 1]);
     mx *= to;
-    if (__any(mx > m_run + 8.0f)) {  // -inf + 8 is -inf: the first keys of a query come through here
+    if constexpr (SHAPED) {  // the exponents are less off_run already, which is renewed where one exceeds it by more than 8
+      if (__any(mx > bound)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const bool first = bound == -INFINITY;
+        const float up = first ? (mx == -INFINITY ? 0.f : mx) : fmaxf(mx, 0.f);
+        [[maybe_unused]] const bool far = __any(!first && up > 64.0f);
+        const float al = first ? 1.0f : __builtin_amdgcn_exp2f(-up);
+        l_run *= al;
+#pragma unroll
+        for (int tt = 0; tt < NT; tt++)
+#pragma unroll
+          for (int v = 0; v < 16; v++) o[tt][v] *= al;
+        off_run += up;
+        if ((RL & RULE_SLOPES) != 0 && far) {  // what keys far from these left as the offset has taken these ones' bits
+          const TileSight<RL> hides(rule, keys, kb + 4 * h);
+          const float away = (float)(rule.center - (kb + 4 * h));
+#pragma unroll
+          for (int x = 0; x < SB; x++) {
+#pragma unroll
+            for (int k = 0; k < KS; k++) {
+              const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + k_at(k) + x * 32 * DH * 2);
+#pragma unroll
+              for (int p = NP - 1; p >= 0; p--)
+                s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[p][k], (p == NP - 1 && k == 0) ? (f32x16)(0.f) : s[x], 0, 0, 0);
+            }
+#pragma unroll
+            for (int v = 0; v < 16; v++) {
+              const int i = x * 32 + 8 * (v >> 2) + (v & 3);
+              float e = rule.shaped(s[x][v], sc, away - (float)i) - off_run;
+              asm volatile("" : "+v"(e));
+              s[x][v] = hides.sees(i) ? e : -INFINITY;
+            }
+          }
+        } else {
+#pragma unroll
+          for (int x = 0; x < SB; x++)
+#pragma unroll
+            for (int v = 0; v < 16; v++) s[x][v] -= up;
+        }
+        bound = first && mx == -INFINITY ? -INFINITY : 8.0f;
+      }
+    } else if (__any(mx > m_run + 8.0f)) {  // -inf + 8 is -inf: the first keys of a query come through here
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
       const float mn = fmaxf(m_run, mx);
       const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - mn);
@@ -997,7 +1131,7 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
         for (int v = 0; v < 16; v++) o[tt][v] *= al;
       m_run = mn;
     }
-    const float off = m_run == -INFINITY ? 0.f : m_run;  // a query without a key yet: every p is 0
+    const float off = SHAPED || m_run == -INFINITY ? 0.f : m_run;  // a query without a key yet: every p is 0
 #pragma unroll
     for (int x = 0; x < SB; x++) {
       union { uint32_t u[8]; bf16x8 f[2]; } pf[NP];
@@ -1019,6 +1153,7 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
             o[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x][ks][tt], pf[p].f[ks], o[tt], 0, 0, 0);
     }
   }
+  if constexpr (SHAPED) m_run = bound == -INFINITY ? -INFINITY : off_run;
   finish_wide<T, uint16_t, DH, RL>(A, it, R, g, o, m_run, l_run, rule, lds);
 }
 
@@ -1184,7 +1319,7 @@ __device__ void piece_few(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const Re
       }
     if constexpr ((RL & (RULE_CAP | RULE_SLOPES)) != 0) {
 #pragma unroll
-      for (int e = 0; e < 8; e++) s[e >> 2][e & 3] = rule.shaped(s[e >> 2][e & 3], sc, kb + (e >> 2) * 16 + 4 * q4 + (e & 3));
+      for (int e = 0; e < 8; e++) s[e >> 2][e & 3] = rule.shaped(s[e >> 2][e & 3], sc, (float)(rule.center - (kb + (e >> 2) * 16 + 4 * q4 + (e & 3))));
     }
     bool part = kb < keys.a || kb + KT > wmin;
     if constexpr (RL != 0) part = kb < keys.a || kb + KT > keys.b || !seen.whole(kb, KT);
@@ -1329,7 +1464,7 @@ __device__ void piece_few_f32(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, cons
 #pragma unroll
       for (int v = 0; v < 4; v++) {
         const int kk = kb + 4 * q4 + v;
-        if constexpr ((RL & (RULE_CAP | RULE_SLOPES)) != 0) s[x][v] = rule[x].shaped(s[x][v], 1.0f, kk);
+        if constexpr ((RL & (RULE_CAP | RULE_SLOPES)) != 0) s[x][v] = rule[x].shaped(s[x][v], 1.0f, (float)(rule[x].center - kk));
         bool is = rule[x].sees(kk) && kk >= keys.a;
         if constexpr (RL != 0) is = is && kk < keys.b;
         s[x][v] = is ? s[x][v] : -INFINITY;
@@ -1458,7 +1593,7 @@ __device__ void piece_f32(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const Re
 #pragma unroll
     for (int v = 0; v < 16; v++) {
       const int kk = kb + 8 * (v >> 2) + 4 * h + (v & 3);
-      if constexpr ((RL & (RULE_CAP | RULE_SLOPES)) != 0) s[v] = rule.shaped(s[v], 1.0f, kk);
+      if constexpr ((RL & (RULE_CAP | RULE_SLOPES)) != 0) s[v] = rule.shaped(s[v], 1.0f, (float)(rule.center - kk));
       bool is = rule.sees(kk) && kk >= keys.a;
       if constexpr (RL != 0) is = is && kk < keys.b;
       s[v] = is ? s[v] : -INFINITY;
