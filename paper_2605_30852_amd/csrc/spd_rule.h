@@ -7,8 +7,17 @@
 namespace spd {
 namespace {
 
-// Parts of a rule that a kernel is made for: keys unseen (all rules), capped scores, scores lowered with the distance.
-enum { RULE_KEYS = 1, RULE_CAP = 2, RULE_SLOPES = 4 };
+// Parts of a rule that a kernel is made for: keys unseen (all rules), capped scores, scores lowered with the distance; caps low
+// enough for one offset of the exponents.
+// That offset, kFixed: the nearest key that a row sees has a distance of 0 (RowRule), and so the largest of its exponents lies in [-top,
+// top]. With top of at most kFixedTop no running maximum is needed: probabilities, 2^-64 to 2^96, have sums over 2^20 keys below 2^116,
+// and of keys that the distance lowers below fp32's range none counts beside 2^-64.
+enum { RULE_KEYS = 1, RULE_CAP = 2, RULE_SLOPES = 4, RULE_FIXED = 8 };
+constexpr float kFixed = -16.0f, kFixedTop = 80.0f;
+
+// Without a cap the offset starts at the maximum of the first tile, but not below this: a row's nearest key decides, and the offsets that
+// keys far from it would set would take the bits of its score. Rows whose sum stays below kLeastSum are computed again (plain_query).
+constexpr float kLeastOffset = -64.0f, kLeastSum = 0x1p-60f;
 
 constexpr int kTanhTerms = 7;  // of fp32 queries; 5 of bf16 ones
 
@@ -17,8 +26,9 @@ struct RuleArgs {
   int window;
   const float* slopes;
   const int *first, *open;
-  // Of products S up to `limit`, top tanh(S / (top to)) = S (c[0] + y (c[1] + ...)), y = S^2, in units of log2 (scaled_poly)
-  float limit, c[kTanhTerms];
+  // Of products S up to `limit`, top tanh(S / (top to)) = S (c[0] + y (c[1] + ...)), y = S^2, in units of log2 (scaled_poly); up to
+  // `near` the three of n are enough
+  float limit, c[kTanhTerms], near, n[3];
 };
 
 // Keys below `open` and keys of [lo, lim).

@@ -24,18 +24,23 @@ __device__ __forceinline__ float tanh_of(float x) {
 // for probabilities that are rounded to bf16 (a score of 30 is off by 2e-4 of a unit of log2, as p by 1.5e-4 of itself, the rounding by
 // 2e-3); seven, 5e-8, are what fp32 holds.
 constexpr double kTanh5[] = {0.999993089, -0.332980653, 0.130368112, -0.0448175544, 0.00903642415};
+constexpr double kTanh3[] = {0.99998766, -0.332227042, 0.11835343};  // of [0, 0.45]: 1.2e-5
 constexpr double kTanh7[] = {0.99999995, -0.333328392, 0.133252041, -0.0534570295, 0.0202899804, -0.00620337906, 0.00104102262};
 
 // The polynomial with the scale of the products S in its coefficients. Caps for which these would leave fp32's range have none (limit -1):
 // their scores take the other formula.
 void scaled_poly(RuleArgs& r, int dtype, float scale) {
-  r.limit = -1.f;
+  r.limit = r.near = -1.f;
   if (!(r.cap >= 0x1p-6f && r.cap <= 0x1p9f)) return;
   const bool bf16 = dtype == SPD_BF16;
   const double top = (double)r.cap * kLog2e, k = bf16 ? (double)scale / r.cap : 1.0 / top;  // x = S k
   double power = k * top;
   for (int i = 0; i < (bf16 ? 5 : kTanhTerms); i++, power *= k * k) r.c[i] = (float)((bf16 ? kTanh5 : kTanh7)[i] * power);
   r.limit = (float)(1.0 / k);
+  if (!bf16) return;
+  power = k * top;
+  for (int i = 0; i < 3; i++, power *= k * k) r.n[i] = (float)(kTanh3[i] * power);
+  r.near = (float)(0.45 / k);
 }
 
 spd_status check_rule(const char* call, const spd_attention_rule* r) {
@@ -49,14 +54,17 @@ spd_status check_rule(const char* call, const spd_attention_rule* r) {
 // The kernels of a rule's parts.
 void run_ruled(const SeqArgs& plain, const spd_attention_rule& r, int dtype, const Request& q, bool prefix, void* workspace,
                hipStream_t s) {
-  RuledSeqArgs a{plain, RuleArgs{r.cap, r.window, r.slopes, r.first, r.open_lens, 0.f, {}}};
+  RuledSeqArgs a{plain, RuleArgs{r.cap, r.window, r.slopes, r.first, r.open_lens, 0.f, {}, 0.f, {}}};
   scaled_poly(a.rule, dtype, plain.scale);
-  if (r.cap != 0.f)
-    r.slopes ? run_attention<RULE_KEYS | RULE_CAP | RULE_SLOPES>(a, dtype, q, prefix, workspace, s)
-             : run_attention<RULE_KEYS | RULE_CAP>(a, dtype, q, prefix, workspace, s);
-  else
+  constexpr int CAP = RULE_KEYS | RULE_CAP;
+  if (r.cap == 0.f)
     r.slopes ? run_attention<RULE_KEYS | RULE_SLOPES>(a, dtype, q, prefix, workspace, s)
              : run_attention<RULE_KEYS>(a, dtype, q, prefix, workspace, s);
+  else if (r.cap * kLog2e > kFixedTop)
+    run_attention<CAP | RULE_SLOPES>(a, dtype, q, prefix, workspace, s);
+  else
+    r.slopes ? run_attention<CAP | RULE_SLOPES | RULE_FIXED>(a, dtype, q, prefix, workspace, s)
+             : run_attention<CAP | RULE_FIXED>(a, dtype, q, prefix, workspace, s);
 }
 
 }  // namespace

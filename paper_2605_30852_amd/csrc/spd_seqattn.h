@@ -188,7 +188,7 @@ struct Merge {
 };
 
 struct RuledMerge : Merge {
-  int open;
+  int open, table;
 };
 template <int RL>
 using MergeOf = std::conditional_t<RL != 0, RuledMerge, Merge>;
@@ -524,7 +524,10 @@ __global__ __launch_bounds__(NTH) void k_plan_attention(PlanArgsOf<RL> P) {
       int4 r = make_int4(0, 0, 0, 0);
       if (PREFIX && k.shared) r = k.tile < kPlanTiles ? s_tile[k.tile] : P.tile_rec[k.tile];
       MergeOf<RL> m;
-      if constexpr (RL != 0) m.open = k.j.open;
+      if constexpr (RL != 0) {
+        m.open = k.j.open;
+        m.table = k.j.table;
+      }
       m.row0 = k.j.row0;
       m.nrows = k.j.nrows;
       m.rec[0] = r.x;
@@ -666,7 +669,7 @@ __device__ __forceinline__ RowRule<RL> rule_of(const SeqArgsOf<RL>& A, int row, 
   x.center = s.lo < s.lim || s.open > p ? p : s.open - 1;
   x.top = A.rule.cap * kLog2e;
   x.to_x = 1.0f / x.top;
-  x.slope = (RL & RULE_SLOPES) != 0 ? A.rule.slopes[head] * kLog2e : 0.f;
+  x.slope = (RL & RULE_SLOPES) != 0 && A.rule.slopes != nullptr ? A.rule.slopes[head] * kLog2e : 0.f;
   return x;
 }
 template <int RL>
@@ -754,10 +757,43 @@ __device__ __forceinline__ float multiple_plus(float a, float n, float b) {
 
 // A tile's products S of a lane's query become exponents less `off`: top tanh, and less slope times the distance. at(i): the
 // tile's key of product i, from key k of the lane's on; to: from S to units of log2. Where every key's distance counts down to the
-// center and every |S| is within the polynomial's range, which nearly all tiles are, this takes a multiplication and TERMS FMAs a
-// score for the cap and one instruction more for the distance; else the general formula. Scores are done four at a time: all at once
-// would take more registers than there are.
+// center and every |S| is within a polynomial's range, which nearly all tiles are, this takes a multiplication and a FMA for each of its
+// terms (3, 5 or 7) a score for the cap and one instruction more for the distance; else the general formula. Scores are done four at a
+// time: all at once would take more registers than there are.
 template <int RL, int TERMS, int W, typename V, int NV, typename At>
+__device__ __forceinline__ void shape_by(V (&s)[NV], const float* c, const RowRule<RL>& rule, float to, float away, float off, At at) {
+  float base = -off;
+  [[maybe_unused]] float step[4];  // slope times 0 .. 3
+  if constexpr ((RL & RULE_SLOPES) != 0) {
+    base = fmaf(-rule.slope, away, -off);
+#pragma unroll
+    for (int j = 1; j < 4; j++) step[j] = rule.slope * (float)j;
+  }
+#pragma unroll
+  for (int i0 = 0; i0 < W * NV; i0 += 4) {  // four keys one after the other
+    float e[4], from = base;
+    if constexpr ((RL & RULE_SLOPES) != 0) from = multiple_plus<RL>(rule.slope, (float)at(i0), base);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      float add = from;
+      if constexpr ((RL & RULE_SLOPES) != 0) add = i > 0 ? from + step[i] : from;
+      const float x = s[i0 / W][i0 % W + i];
+      if constexpr ((RL & RULE_CAP) != 0) {
+        const float y = x * x;
+        float t = c[TERMS - 1];
+#pragma unroll
+        for (int j = TERMS - 2; j >= 0; j--) t = fmaf(y, t, c[j]);
+        e[i] = fmaf(x, t, add);
+      } else {
+        e[i] = fmaf(x, to, add);
+      }
+    }
+    asm volatile("" : "+v"(e[0]), "+v"(e[1]), "+v"(e[2]), "+v"(e[3]));
+#pragma unroll
+    for (int i = 0; i < 4; i++) s[i0 / W][i0 % W + i] = e[i];
+  }
+}
+template <int RL, bool FEW_BITS, int W, typename V, int NV, typename At>
 __device__ __forceinline__ void shape(V (&s)[NV], const RuleArgs& R, const RowRule<RL>& rule, float to, int k, bool one_side, float off, At at) {
   constexpr int N = W * NV;
   const float away = (RL & RULE_SLOPES) != 0 ? (float)(rule.center - k) : 0.f;
@@ -767,39 +803,14 @@ __device__ __forceinline__ void shape(V (&s)[NV], const RuleArgs& R, const RowRu
     float far = 0.f;
 #pragma unroll
     for (int i = 0; i < N; i += 2) far = fmaxf(fmaxf(far, fabsf(s[i / W][i % W])), fabsf(s[(i + 1) / W][(i + 1) % W]));
+    if (FEW_BITS && usual && !__any(far > R.near)) {
+      shape_by<RL, 3, W>(s, R.n, rule, to, away, off, at);
+      return;
+    }
     usual = usual && !__any(far > R.limit);
   }
   if (usual) {
-    float base = -off;
-    [[maybe_unused]] float step[4];  // slope times 0 .. 3
-    if constexpr ((RL & RULE_SLOPES) != 0) {
-      base = fmaf(-rule.slope, away, -off);
-#pragma unroll
-      for (int j = 1; j < 4; j++) step[j] = rule.slope * (float)j;
-    }
-#pragma unroll
-    for (int i0 = 0; i0 < N; i0 += 4) {  // four keys one after the other
-      float e[4], from = base;
-      if constexpr ((RL & RULE_SLOPES) != 0) from = multiple_plus<RL>(rule.slope, (float)at(i0), base);
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        float add = from;
-        if constexpr ((RL & RULE_SLOPES) != 0) add = i > 0 ? from + step[i] : from;
-        const float x = s[i0 / W][i0 % W + i];
-        if constexpr ((RL & RULE_CAP) != 0) {
-          const float y = x * x;
-          float t = R.c[TERMS - 1];
-#pragma unroll
-          for (int j = TERMS - 2; j >= 0; j--) t = fmaf(y, t, R.c[j]);
-          e[i] = fmaf(x, t, add);
-        } else {
-          e[i] = fmaf(x, to, add);
-        }
-      }
-      asm volatile("" : "+v"(e[0]), "+v"(e[1]), "+v"(e[2]), "+v"(e[3]));
-#pragma unroll
-      for (int i = 0; i < 4; i++) s[i0 / W][i0 % W + i] = e[i];
-    }
+    shape_by<RL, FEW_BITS ? 5 : 7, W>(s, R.c, rule, to, away, off, at);
   } else {
 #pragma unroll
     for (int i = 0; i < N; i++) {
@@ -833,6 +844,15 @@ __device__ void plain_piece(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const 
   }
 }
 
+// Whether the sum of a row that sees some key has to be made again. Scores that fall with the distance leave little or nothing of a
+// piece of far keys: that is seen by the merge, which has all of them (whole: the piece is all of the row's).
+template <int RL>
+__device__ __forceinline__ bool small_sum(float l, bool whole) {
+  if constexpr ((RL & RULE_FIXED) != 0) return !(l >= 0.f);
+  else if constexpr ((RL & RULE_SLOPES) != 0) return !(l >= (whole ? kLeastSum : 0.f));
+  else return !(l > 0.f);
+}
+
 // The end of a piece of 32 queries a wave: registers 4 v .. + 3 of tile t are dims 32 t + 8 v + 4 h .. + 3 of the lane's query.
 template <typename T, typename KVT, int DH, int RL>
 __device__ void finish_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const Records R, int g, const f32x16 (&o)[DH / 32],
@@ -848,7 +868,7 @@ __device__ void finish_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const 
   __syncthreads();
   if (active) {
     const Span keys = span_of<RL>(it);
-    bool bad = !(l_run > 0.f) && rule.sees_any(keys.a, keys.b);  // NaN, or nothing but scores of -inf
+    bool bad = small_sum<RL>(l_run, it.rec < 0) && rule.sees_any(keys.a, keys.b);  // NaN, or nothing but scores of -inf
 #pragma unroll
     for (int tt = 0; tt < NT; tt++)
 #pragma unroll
@@ -922,14 +942,12 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
   const int* table = C.page_table + (size_t)it.table * C.max_pages;
   // The pages of a tile, one a lane (mod their number), are read a tile ahead of their use, and looked at only there: a look
   // at them here would wait for them and for the keys requested before them.
-  // The first key of the t-th tile. Scores that fall with the distance are taken from the last tile down, which has the largest ones:
-  // from the first up, a steep slope renews the offset at every tile.
-  auto tile_key = [&](int t) { return key_of<RL>(it, start + ((RL & RULE_SLOPES) != 0 ? max(tiles - 1 - t, 0) : t) * KT); };
+  auto tile_key = [&](int t) { return key_of<RL>(it, start + t * KT); };
   auto pages = [&](int t) { return table[min(tile_key(t) / kPage + (lane & (KT / kPage - 1)), last / kPage)]; };
   const int pg0 = tiles > 0 ? pages(0) : 0;
   int pg = tiles > 0 ? pages(1) : 0;
   const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;  // from products to scores in units of log2
-  constexpr bool SHAPED = (RL & (RULE_CAP | RULE_SLOPES)) != 0;
+  constexpr bool SHAPED = (RL & (RULE_CAP | RULE_SLOPES)) != 0, FIXED = (RL & RULE_FIXED) != 0;
   const float to = SHAPED ? 1.0f : sc;  // from scores to exponents
   const bool active = w * 32 < nq;
   const int jq = w * 32 + col, jj = min(jq, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
@@ -1055,8 +1073,8 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
       pg = pages(t + 2);
     }
     if constexpr (SHAPED) {
-      shape<RL, NP == 1 ? 5 : 7, 16>(s, A.rule, rule, sc, kb + 4 * h, seen.one_side(kb, KT), off_run,
-                                     [](int i) { return (i >> 4) * 32 + 8 * (i >> 2 & 3) + (i & 3); });
+      shape<RL, NP == 1, 16>(s, A.rule, rule, sc, kb + 4 * h, seen.one_side(kb, KT), FIXED ? kFixed : off_run,
+                             [](int i) { return (i >> 4) * 32 + 8 * (i >> 2 & 3) + (i & 3); });
     }
     bool part = kb < keys.a || kb + KT > wmin;  // some key is not every query's
     if constexpr (RL != 0) part = kb < keys.a || kb + KT > keys.b || !seen.whole(kb, KT);
@@ -1074,50 +1092,30 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
         }
     }
     float mx = s[0][0];
+    if constexpr (!FIXED) {
 #pragma unroll
-    for (int x = 0; x < SB; x++)
+      for (int x = 0; x < SB; x++)
 #pragma unroll
-      for (int v = 0; v < 16; v += 2) mx = fmaxf(fmaxf(mx, s[x][v]), s[x][v + 1]);
-    mx *= to;
-    if constexpr (SHAPED) {  // the exponents are less off_run already, which is renewed where one exceeds it by more than 8
+        for (int v = 0; v < 16; v += 2) mx = fmaxf(fmaxf(mx, s[x][v]), s[x][v + 1]);
+      mx *= to;
+    }
+    if constexpr (FIXED) {
+    } else if constexpr (SHAPED) {  // the exponents are less off_run already, which is renewed where one exceeds it by more than 8
       if (__any(mx > bound)) {
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
         const bool first = bound == -INFINITY;
-        const float up = first ? (mx == -INFINITY ? 0.f : mx) : fmaxf(mx, 0.f);
-        [[maybe_unused]] const bool far = __any(!first && up > 64.0f);
+        const float up = first ? (mx == -INFINITY ? 0.f : fmaxf(mx, kLeastOffset)) : fmaxf(mx, 0.f);
         const float al = first ? 1.0f : __builtin_amdgcn_exp2f(-up);
         l_run *= al;
 #pragma unroll
         for (int tt = 0; tt < NT; tt++)
 #pragma unroll
           for (int v = 0; v < 16; v++) o[tt][v] *= al;
+#pragma unroll
+        for (int x = 0; x < SB; x++)
+#pragma unroll
+          for (int v = 0; v < 16; v++) s[x][v] -= up;
         off_run += up;
-        if ((RL & RULE_SLOPES) != 0 && far) {  // what keys far from these left as the offset has taken these ones' bits
-          const TileSight<RL> hides(rule, keys, kb + 4 * h);
-          const float away = (float)(rule.center - (kb + 4 * h));
-#pragma unroll
-          for (int x = 0; x < SB; x++) {
-#pragma unroll
-            for (int k = 0; k < KS; k++) {
-              const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + k_at(k) + x * 32 * DH * 2);
-#pragma unroll
-              for (int p = NP - 1; p >= 0; p--)
-                s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[p][k], (p == NP - 1 && k == 0) ? (f32x16)(0.f) : s[x], 0, 0, 0);
-            }
-#pragma unroll
-            for (int v = 0; v < 16; v++) {
-              const int i = x * 32 + 8 * (v >> 2) + (v & 3);
-              float e = rule.shaped(s[x][v], sc, away - (float)i) - off_run;
-              asm volatile("" : "+v"(e));
-              s[x][v] = hides.sees(i) ? e : -INFINITY;
-            }
-          }
-        } else {
-#pragma unroll
-          for (int x = 0; x < SB; x++)
-#pragma unroll
-            for (int v = 0; v < 16; v++) s[x][v] -= up;
-        }
         bound = first && mx == -INFINITY ? -INFINITY : 8.0f;
       }
     } else if (__any(mx > m_run + 8.0f)) {  // -inf + 8 is -inf: the first keys of a query come through here
@@ -1153,7 +1151,8 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
             o[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x][ks][tt], pf[p].f[ks], o[tt], 0, 0, 0);
     }
   }
-  if constexpr (SHAPED) m_run = bound == -INFINITY ? -INFINITY : off_run;
+  if constexpr (FIXED) m_run = kFixed;
+  else if constexpr (SHAPED) m_run = bound == -INFINITY ? -INFINITY : off_run;
   finish_wide<T, uint16_t, DH, RL>(A, it, R, g, o, m_run, l_run, rule, lds);
 }
 
@@ -1721,6 +1720,11 @@ constexpr int kMergeRows = 128;  // 32: 4 us more there, 64: 0.5
 template <int DH>
 constexpr int merge_queries() { return kWG / (DH / 4); }
 
+template <int RL>
+__device__ __forceinline__ RowRule<RL> merged_rule(const SeqArgsOf<RL>& A, const MergeOf<RL>& m, int r, int lim, int head) {
+  return rule_of<RL>(A, r, lim - 1, m.mode & ITEM_FLAT ? open_of(A.rule, r, lim) : m.open, head);
+}
+
 template <typename T, int DH, int RL>
 __global__ __launch_bounds__(kWG) void k_merge(SeqArgsOf<RL> A, const int* count, const Unit* units, const MergeOf<RL>* merges, Records R) {
   constexpr int TPQ = DH / 4;
@@ -1737,8 +1741,7 @@ __global__ __launch_bounds__(kWG) void k_merge(SeqArgsOf<RL> A, const int* count
     int lim = m.lim0 + jj / G;
     if (m.mode & ITEM_FLAT) lim = seq_len(A.c, A.seqs[r]);
     bool any = lim > 0;  // some key is seen
-    if constexpr (RL != 0)
-      any = rule_of<RL>(A, r, lim - 1, m.mode & ITEM_FLAT ? open_of(A.rule, r, lim) : m.open, head).sees_any(0, 0x7fffffff);
+    if constexpr (RL != 0) any = merged_rule<RL>(A, m, r, lim, head).sees_any(0, 0x7fffffff);
     float L, a[4], part = 1.0f;
     bool again;
     do {  // once more, lowered by a power of two, where finite records add up to what is not
@@ -1782,6 +1785,27 @@ __global__ __launch_bounds__(kWG) void k_merge(SeqArgsOf<RL> A, const int* count
       part = ldexpf(1.0f, -down_of(max(np, 1)));
     } while (again);
     if (j < nq) store4((T*)A.out + r * A.os + head * DH + 4 * lane, a, any ? 1.0f / L : 0.f);
+    if constexpr ((RL & RULE_SLOPES) != 0 && (RL & RULE_FIXED) == 0) {  // sums of keys too far below the offset: the row's keys again
+      __shared__ uint32_t s_small;
+      __shared__ float lds[6 * kWG];
+      __syncthreads();
+      if (threadIdx.x == 0) s_small = 0u;
+      __syncthreads();
+      if (j < nq && any && !(L >= kLeastSum) && lane == 0) atomicOr(&s_small, 1u << threadIdx.x / TPQ);
+      __syncthreads();
+      for (uint32_t left = __builtin_amdgcn_readfirstlane(s_small); left != 0u; left &= left - 1u) {
+        const int jb = un.query + __builtin_ctz(left), rb = m.row0 + jb / G, hb = g * G + jb % G;
+        const int limb = m.mode & ITEM_FLAT ? seq_len(A.c, A.seqs[rb]) : m.lim0 + jb / G;
+        const RowRule<RL> rule = merged_rule<RL>(A, m, rb, limb, hb);
+        float M, b[4];
+        const bool holds = A.c.dtype == SPD_BF16
+            ? plain_query<T, uint16_t, DH, RL>(A.c, (const uint16_t*)A.kv, A.c.page_table + (size_t)m.table * A.c.max_pages, g,
+                                               (const T*)A.q + rb * A.qs + hb * DH, A.scale, rule, 0, max(limb, rule.open), lds, M, L, b)
+            : plain_query<T, float, DH, RL>(A.c, (const float*)A.kv, A.c.page_table + (size_t)m.table * A.c.max_pages, g,
+                                            (const T*)A.q + rb * A.qs + hb * DH, A.scale, rule, 0, max(limb, rule.open), lds, M, L, b);
+        if (holds) store4((T*)A.out + rb * A.os + hb * DH + 4 * (threadIdx.x % TPQ), b, 1.0f / L);
+      }
+    }
   }
 }
 
