@@ -19,14 +19,14 @@ constexpr float kFixed = -16.0f, kFixedTop = 80.0f;
 // keys far from it would set would take the bits of its score. Rows whose sum stays below kLeastSum are computed again (plain_query).
 constexpr float kLeastOffset = -64.0f, kLeastSum = 0x1p-60f;
 
-constexpr int kTanhTerms = 7;  // of fp32 queries; 5 of bf16 ones
+constexpr int kTanhTerms = 7;  // of fp32 queries; 4 of bf16 ones
 
 struct RuleArgs {
   float cap;
   int window;
   const float* slopes;
   const int *first, *open;
-  // Of products S up to `limit`, top tanh(S / (top to)) = S (c[0] + y (c[1] + ...)), y = S^2, in units of log2 (scaled_poly); up to
+  // Of products S up to `limit`, top tanh(S / (top to)) = S (c[0] + y (c[1] + ...)), y = S^2, in units of log2 (scaled_polys); up to
   // `near` the three of n are enough
   float limit, c[kTanhTerms], near, n[3];
 };

@@ -20,27 +20,30 @@ __device__ __forceinline__ float tanh_of(float x) {
   return fabsf(x) < kTanhPoly ? small : copysignf(big, x);
 }
 
-// tanh(x) / x in powers of x^2, for x of [0, 1]: fitted to the least largest error of tanh(x) relative to itself. Five terms, 7e-6, are enough
-// for probabilities that are rounded to bf16 (a score of 30 is off by 2e-4 of a unit of log2, as p by 1.5e-4 of itself, the rounding by
-// 2e-3); seven, 5e-8, are what fp32 holds.
-constexpr double kTanh5[] = {0.999993089, -0.332980653, 0.130368112, -0.0448175544, 0.00903642415};
-constexpr double kTanh3[] = {0.99998766, -0.332227042, 0.11835343};  // of [0, 0.45]: 1.2e-5
-constexpr double kTanh7[] = {0.99999995, -0.333328392, 0.133252041, -0.0534570295, 0.0202899804, -0.00620337906, 0.00104102262};
+// tanh(x) / x in powers of x^2, for x from 0 up to `to`, fitted to the least largest error of tanh(x) relative to itself. Three terms,
+// 3.9e-5, and four, 4.0e-5, are enough for probabilities that are rounded to bf16: a score of 10 is off by 4e-4, as p of itself, its
+// rounding by up to 2e-3; seven, 5e-8, are what fp32 holds.
+struct Tanh {
+  double to;
+  int terms;
+  double c[7];
+};
+constexpr Tanh kTanh3{0.55, 3, {0.999961253, -0.330998277, 0.111880151}}, kTanh4{0.9, 4, {0.999960199, -0.331725224, 0.122781884, -0.0300411835}},
+    kTanh7{1.0, 7, {0.99999995, -0.333328392, 0.133252041, -0.0534570295, 0.0202899804, -0.00620337906, 0.00104102262}};
 
-// The polynomial with the scale of the products S in its coefficients. Caps for which these would leave fp32's range have none (limit -1):
-// their scores take the other formula.
-void scaled_poly(RuleArgs& r, int dtype, float scale) {
+// The polynomials with the scale of the products S in their coefficients. Caps for which these would leave fp32's range have none (a
+// limit of -1): their scores take the other formula.
+void scaled_polys(RuleArgs& r, int dtype, float scale) {
   r.limit = r.near = -1.f;
   if (!(r.cap >= 0x1p-6f && r.cap <= 0x1p9f)) return;
-  const bool bf16 = dtype == SPD_BF16;
-  const double top = (double)r.cap * kLog2e, k = bf16 ? (double)scale / r.cap : 1.0 / top;  // x = S k
-  double power = k * top;
-  for (int i = 0; i < (bf16 ? 5 : kTanhTerms); i++, power *= k * k) r.c[i] = (float)((bf16 ? kTanh5 : kTanh7)[i] * power);
-  r.limit = (float)(1.0 / k);
-  if (!bf16) return;
-  power = k * top;
-  for (int i = 0; i < 3; i++, power *= k * k) r.n[i] = (float)(kTanh3[i] * power);
-  r.near = (float)(0.45 / k);
+  const double top = (double)r.cap * kLog2e, k = dtype == SPD_BF16 ? (double)scale / r.cap : 1.0 / top;  // x = S k
+  auto take = [&](const Tanh& t, float* c) {
+    double power = k * top;
+    for (int i = 0; i < t.terms; i++, power *= k * k) c[i] = (float)(t.c[i] * power);
+    return (float)(t.to / k);
+  };
+  r.limit = take(dtype == SPD_BF16 ? kTanh4 : kTanh7, r.c);
+  if (dtype == SPD_BF16) r.near = take(kTanh3, r.n);
 }
 
 spd_status check_rule(const char* call, const spd_attention_rule* r) {
@@ -55,7 +58,7 @@ spd_status check_rule(const char* call, const spd_attention_rule* r) {
 void run_ruled(const SeqArgs& plain, const spd_attention_rule& r, int dtype, const Request& q, bool prefix, void* workspace,
                hipStream_t s) {
   RuledSeqArgs a{plain, RuleArgs{r.cap, r.window, r.slopes, r.first, r.open_lens, 0.f, {}, 0.f, {}}};
-  scaled_poly(a.rule, dtype, plain.scale);
+  scaled_polys(a.rule, dtype, plain.scale);
   constexpr int CAP = RULE_KEYS | RULE_CAP;
   if (r.cap == 0.f)
     r.slopes ? run_attention<RULE_KEYS | RULE_SLOPES>(a, dtype, q, prefix, workspace, s)

@@ -695,17 +695,27 @@ __device__ __forceinline__ Span span_of(const ItemOf<RL>& it) {
   }
 }
 
-// What a lane's row sees of a piece's tile, its keys counted from key k on: a comparison with a number is one instruction, and needs no
-// register for the key.
-template <int RL>
+// What a lane's row sees of a piece's tile, a bit a key from key k on (32 of a word): two instructions a score, where comparisons
+// with the four bounds take eight.
+template <int RL, int WORDS>
 struct TileSight {
-  int a, lo, lim, open;
-  __device__ __forceinline__ TileSight(const RowRule<RL>& r, const Span& keys, int k)
-      : a(keys.a - k), lo(r.lo - k), lim(min(r.lim, keys.b) - k), open(min(r.open, keys.b) - k) {}
-  __device__ __forceinline__ bool sees(int i) const { return i >= a && (i < open || (i >= lo && i < lim)); }
+  uint32_t w[WORDS];
+  // the bits below n
+  static __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? ~0u : ~(~0u << max(n, 0)); }
+  __device__ __forceinline__ TileSight(const RowRule<RL>& r, const Span& keys, int k) {
+    const int lim = min(r.lim, keys.b) - k, open = min(r.open, keys.b) - k;
+#pragma unroll
+    for (int x = 0; x < WORDS; x++)
+      w[x] = (below(open - 32 * x) | (below(lim - 32 * x) & ~below(r.lo - k - 32 * x))) & ~below(keys.a - k - 32 * x);
+  }
+  // s, or -inf where key i is not seen
+  __device__ __forceinline__ float seen(float s, int i) const {
+    const uint32_t m = (uint32_t)((int)(w[i / 32] << (31 - i % 32)) >> 31);
+    return __uint_as_float((m & __float_as_uint(s)) | (~m & 0xff800000u));
+  }
 };
-template <>
-struct TileSight<0> {
+template <int WORDS>
+struct TileSight<0, WORDS> {
   __device__ __forceinline__ TileSight(const RowRule<0>&, const Span&, int) {}
 };
 
@@ -747,32 +757,35 @@ struct WaveRule {
   __device__ __forceinline__ bool one_side(int k, int n) const { return k + n <= center_min + 1 || k >= open_max; }
 };
 
-// a n + b with n in the instruction: as constants in registers the n of a tile would take as many as its scores.
+// a n + b with n in the instruction: as constants in registers the n of a tile would take as many as its scores. (volatile: in its
+// place among the groups of four, where results made ahead would too.)
 template <int RL>
 __device__ __forceinline__ float multiple_plus(float a, float n, float b) {
   float r;
-  asm("v_fmamk_f32 %0, %1, %3, %2" : "=v"(r) : "v"(a), "v"(b), "n"(__builtin_bit_cast(int, n)));
+  asm volatile("v_fmamk_f32 %0, %1, %3, %2" : "=v"(r) : "v"(a), "v"(b), "n"(__builtin_bit_cast(int, n)));
   return r;
 }
 
 // A tile's products S of a lane's query become exponents less `off`: top tanh, and less slope times the distance. at(i): the
 // tile's key of product i, from key k of the lane's on; to: from S to units of log2. Where every key's distance counts down to the
 // center and every |S| is within a polynomial's range, which nearly all tiles are, this takes a multiplication and a FMA for each of its
-// terms (3, 5 or 7) a score for the cap and one instruction more for the distance; else the general formula. Scores are done four at a
+// terms (3, 4 or 7) a score for the cap and one instruction more for the distance; else the general formula. Scores are done four at a
 // time: all at once would take more registers than there are.
 template <int RL, int TERMS, int W, typename V, int NV, typename At>
 __device__ __forceinline__ void shape_by(V (&s)[NV], const float* c, const RowRule<RL>& rule, float to, float away, float off, At at) {
   float base = -off;
+  float slope = rule.slope;
   [[maybe_unused]] float step[4];  // slope times 0 .. 3
   if constexpr ((RL & RULE_SLOPES) != 0) {
-    base = fmaf(-rule.slope, away, -off);
+    asm volatile("" : "+v"(slope));  // the steps are made here, not kept
+    base = fmaf(-slope, away, -off);
 #pragma unroll
-    for (int j = 1; j < 4; j++) step[j] = rule.slope * (float)j;
+    for (int j = 1; j < 4; j++) step[j] = slope * (float)j;
   }
 #pragma unroll
   for (int i0 = 0; i0 < W * NV; i0 += 4) {  // four keys one after the other
     float e[4], from = base;
-    if constexpr ((RL & RULE_SLOPES) != 0) from = multiple_plus<RL>(rule.slope, (float)at(i0), base);
+    if constexpr ((RL & RULE_SLOPES) != 0) from = multiple_plus<RL>(slope, (float)at(i0), base);
 #pragma unroll
     for (int i = 0; i < 4; i++) {
       float add = from;
@@ -810,7 +823,7 @@ __device__ __forceinline__ void shape(V (&s)[NV], const RuleArgs& R, const RowRu
     usual = usual && !__any(far > R.limit);
   }
   if (usual) {
-    shape_by<RL, FEW_BITS ? 5 : 7, W>(s, R.c, rule, to, away, off, at);
+    shape_by<RL, FEW_BITS ? 4 : 7, W>(s, R.c, rule, to, away, off, at);
   } else {
 #pragma unroll
     for (int i = 0; i < N; i++) {
@@ -948,6 +961,8 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
   int pg = tiles > 0 ? pages(1) : 0;
   const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;  // from products to scores in units of log2
   constexpr bool SHAPED = (RL & (RULE_CAP | RULE_SLOPES)) != 0, FIXED = (RL & RULE_FIXED) != 0;
+  // The values of a tile's second half are read, and the next tile requested, behind the first half's probabilities
+  constexpr bool LATE = SB > 1 && (RL & RULE_SLOPES) != 0;
   const float to = SHAPED ? 1.0f : sc;  // from scores to exponents
   const bool active = w * 32 < nq;
   const int jq = w * 32 + col, jj = min(jq, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
@@ -995,7 +1010,7 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
       __builtin_amdgcn_global_load_lds(p + half * sizeof(uint16_t) + (at + voff), l + KBUF, 16, 0, 0);
     }
   };
-  // A lane's bytes of a K or V tile. Chunk 2 k + h differs from chunk h in bits that the row has not: under a rule, whose parts need the
+  // A lane's bytes of a K or V tile. Chunk 2 k + h differs from chunk h in bits that the row has not: with a cap or distances, which need the
   // registers, one XOR in a step stands for an address in each.
   uint32_t ka[KS], va[NT];
 #pragma unroll
@@ -1028,9 +1043,9 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
       }
       continue;
     }
-    if constexpr (RL != 0) asm volatile("" : "+v"(ka[0]), "+v"(va[0]));  // the others come from these, in the step
-    auto k_at = [&](int k) { return RL != 0 ? ka[0] ^ (uint32_t)(k << 5) : ka[k]; };
-    auto v_at = [&](int tt) { return RL != 0 ? va[0] ^ (uint32_t)(tt << 6) : va[tt]; };
+    if constexpr (SHAPED) asm volatile("" : "+v"(ka[0]), "+v"(va[0]));  // the others come from these, in the step
+    auto k_at = [&](int k) { return SHAPED ? ka[0] ^ (uint32_t)(k << 5) : ka[k]; };
+    auto v_at = [&](int tt) { return SHAPED ? va[0] ^ (uint32_t)(tt << 6) : va[tt]; };
     f32x16 s[SB];
 #pragma unroll
     for (int x = 0; x < SB; x++)
@@ -1042,8 +1057,7 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
           s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[p][k], (p == NP - 1 && k == 0) ? (f32x16)(0.f) : s[x], 0, 0, 0);
       }
     bf16x8 vf[SB][2][NT];
-#pragma unroll
-    for (int x = 0; x < SB; x++)
+    auto read_values = [&](int x) {
 #pragma unroll
       for (int ks = 0; ks < 2; ks++)
 #pragma unroll
@@ -1054,6 +1068,9 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
             u.q[y] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lbf16x4*)(lbytes*)(tile + v_at(tt) + (x * 32 + ks * 16 + y * 8) * DH * 2));
           vf[x][ks][tt] = u.f;
         }
+    };
+#pragma unroll
+    for (int x = 0; x < (LATE ? 1 : SB); x++) read_values(x);
     // the keys' fragments half a block ahead of their products, the values' among the last products
     __builtin_amdgcn_sched_group_barrier(0x100, KS, 0);
     if constexpr (SB > 1) {
@@ -1066,12 +1083,15 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
 #pragma unroll
     for (int k = 0; k < KS; k++) {
       __builtin_amdgcn_sched_group_barrier(0x008, NP, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 4 * NT * SB / KS, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4 * NT * (LATE ? 1 : SB) / KS, 0);
     }
-    if (t + 1 < tiles) {
-      request(t + 1, pg);
-      pg = pages(t + 2);
-    }
+    auto next = [&] {
+      if (t + 1 < tiles) {
+        request(t + 1, pg);
+        pg = pages(t + 2);
+      }
+    };
+    if constexpr (!LATE) next();
     if constexpr (SHAPED) {
       shape<RL, NP == 1, 16>(s, A.rule, rule, sc, kb + 4 * h, seen.one_side(kb, KT), FIXED ? kFixed : off_run,
                              [](int i) { return (i >> 4) * 32 + 8 * (i >> 2 & 3) + (i & 3); });
@@ -1079,16 +1099,17 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
     bool part = kb < keys.a || kb + KT > wmin;  // some key is not every query's
     if constexpr (RL != 0) part = kb < keys.a || kb + KT > keys.b || !seen.whole(kb, KT);
     if (part) {
-      const TileSight<RL> hides(rule, keys, kb + 4 * h);
+      const TileSight<RL, SB> sight(rule, keys, kb + 4 * h);
       asm volatile("");  // stays a branch: the masks cost as much as a third of the step's vector work
 #pragma unroll
       for (int x = 0; x < SB; x++)
 #pragma unroll
         for (int v = 0; v < 16; v++) {
           const int i = x * 32 + 8 * (v >> 2) + (v & 3), kk = kb + i + 4 * h;
-          bool is = kk < lim && kk >= keys.a;
-          if constexpr (RL != 0) is = hides.sees(i);
-          s[x][v] = is ? s[x][v] : -INFINITY;
+          if constexpr (RL != 0)
+            s[x][v] = sight.seen(s[x][v], i);
+          else
+            s[x][v] = kk < lim && kk >= keys.a ? s[x][v] : -INFINITY;
         }
     }
     float mx = s[0][0];
@@ -1141,6 +1162,10 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
         l_run = add_planes(l_run, p0, p1, pl);
 #pragma unroll
         for (int p = 0; p < NP; p++) pf[p].u[e >> 1] = pl[p];
+      }
+      if (LATE && x == 0) {
+        read_values(1);
+        next();
       }
 #pragma unroll
       for (int ks = 0; ks < 2; ks++)
@@ -1323,14 +1348,16 @@ __device__ void piece_few(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const Re
     bool part = kb < keys.a || kb + KT > wmin;
     if constexpr (RL != 0) part = kb < keys.a || kb + KT > keys.b || !seen.whole(kb, KT);
     if (part) {
+      const TileSight<RL, 1> sight(rule, keys, kb + 4 * q4);
 #pragma unroll
       for (int b = 0; b < 2; b++)
 #pragma unroll
         for (int v = 0; v < 4; v++) {
           const int kk = kb + b * 16 + 4 * q4 + v;
-          bool is = kk < lim && kk >= keys.a;
-          if constexpr (RL != 0) is = rule.sees(kk) && kk >= keys.a && kk < keys.b;
-          s[b][v] = is ? s[b][v] : -INFINITY;
+          if constexpr (RL != 0)
+            s[b][v] = sight.seen(s[b][v], b * 16 + v);
+          else
+            s[b][v] = kk < lim && kk >= keys.a ? s[b][v] : -INFINITY;
         }
     }
     float mx = s[0][0];
@@ -1460,13 +1487,15 @@ __device__ void piece_few_f32(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, cons
 #pragma unroll
     for (int x = 0; x < QS; x++) {
       mx[x] = -INFINITY;
+      const TileSight<RL, 1> sight(rule[x], keys, kb + 4 * q4);
 #pragma unroll
       for (int v = 0; v < 4; v++) {
         const int kk = kb + 4 * q4 + v;
         if constexpr ((RL & (RULE_CAP | RULE_SLOPES)) != 0) s[x][v] = rule[x].shaped(s[x][v], 1.0f, (float)(rule[x].center - kk));
-        bool is = rule[x].sees(kk) && kk >= keys.a;
-        if constexpr (RL != 0) is = is && kk < keys.b;
-        s[x][v] = is ? s[x][v] : -INFINITY;
+        if constexpr (RL != 0)
+          s[x][v] = sight.seen(s[x][v], v);
+        else
+          s[x][v] = rule[x].sees(kk) && kk >= keys.a ? s[x][v] : -INFINITY;
         mx[x] = fmaxf(mx[x], s[x][v]);
       }
       renew = renew || mx[x] > m_run[x] + 8.0f;
@@ -1589,13 +1618,15 @@ __device__ void piece_f32(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const Re
       s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.w, qf[k].w, s, 0, 0, 0);
     }
     float mx = -INFINITY;
+    const TileSight<RL, 1> sight(rule, keys, kb + 4 * h);
 #pragma unroll
     for (int v = 0; v < 16; v++) {
       const int kk = kb + 8 * (v >> 2) + 4 * h + (v & 3);
       if constexpr ((RL & (RULE_CAP | RULE_SLOPES)) != 0) s[v] = rule.shaped(s[v], 1.0f, (float)(rule.center - kk));
-      bool is = rule.sees(kk) && kk >= keys.a;
-      if constexpr (RL != 0) is = is && kk < keys.b;
-      s[v] = is ? s[v] : -INFINITY;
+      if constexpr (RL != 0)
+        s[v] = sight.seen(s[v], 8 * (v >> 2) + (v & 3));
+      else
+        s[v] = rule.sees(kk) && kk >= keys.a ? s[v] : -INFINITY;
       mx = fmaxf(mx, s[v]);
     }
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));

@@ -369,3 +369,67 @@ def test_a_layer_of_another_decoder(types):
             k, v, n = held(s)
             want, mag = attend(q[i:i + 1], k, v, [(n - 1, 0, 0)], 20.0, slopes, 50)
             check(out[i:i + 1], want, mag, (types[0], "step", step, s))
+
+
+@pytest.mark.parametrize("types", TYPES, ids="-".join)
+@pytest.mark.parametrize("cap", [0.0, 500.0])
+def test_scores_far_below_zero(types, cap):
+    """Every score of a row some hundreds below 0, and keys that the distance lowers as much: one piece, split pieces, a shared prefix."""
+    from tests.ruled import attend
+    from tests.seqcache import filled, i32
+    hq, hkv, dh = 4, 1, 128
+    steep = [20.0, 2.0, 0.02, 0.0]
+    for n, new in ((300, 300), (2500, 40)):
+        cache, kv = filled([n], hkv, dh, dt(types[1]), 12)
+        k = kv[0][0, 0].clone()
+        k[..., 0] = -300.0
+        j = torch.arange(n, device="cuda")
+        page = cache.page_table[0].long()[j // 16]
+        cache.kv[0, page, 0, :, j % 16] = k.transpose(0, 1).cuda()
+        q = torch.randn(new, hq, dh, generator=torch.Generator().manual_seed(4)).to(dt(types[0])).cuda()
+        q[..., 0] = 12.0
+        rule = rule_of(cap, steep, 0, None, None)
+        out = cache.prompt_attention(0, q, i32([0]), i32([0, new]), rule=rule)
+        rows = [r for r in range(new) if r % 9 == 0 or r > new - 3]
+        want, mag = attend(q[rows], k, kv[0][0, 1], [(n - new + r, 0, 0) for r in rows], cap, steep)
+        # a score of 300 beside products of 3600 / sqrt(128): fp32 holds it to some 128 roundings of 2^-24 of 318, a few 1e-5 each way; three
+        # planes of a query likewise; with a cap of 500 the tanh of it, off by 2^-22 of 280
+        bound = (2e-3 + (2 ** -7 if types[0] == "bf16" else 0.0)) * (mag + want.abs())
+        assert torch.isfinite(out).all() and ((out[rows].double().cpu() - want).abs() <= bound).all(), (n, cap)
+    cache, kv = filled([2400, 2400], hkv, dh, dt(types[1]), 13)
+    from tests.seqcache import agree
+    for s in range(2):
+        j = torch.arange(2400, device="cuda")
+        page = cache.page_table[s].long()[j // 16]
+        cache.kv[0, page, 0, :, j % 16, 0] = -300.0
+    agree(cache, 0, 1, 2300)
+    q = torch.randn(2, hq, dh, generator=torch.Generator().manual_seed(4)).to(dt(types[0])).cuda()
+    q[..., 0] = 12.0
+    out = cache.prefix_attention(0, q, i32([0, 1]), i32([0, 2]), i32([2300]), rule=rule_of(cap, steep, 0, None, None))
+    for s in range(2):
+        j = torch.arange(2400, device="cuda")
+        x = cache.kv[0, cache.page_table[s].long()[j // 16], :, :, j % 16]
+        want, mag = attend(q[s:s + 1], x[:, 0].transpose(0, 1), x[:, 1].transpose(0, 1), [(2399, 0, 0)], cap, steep)
+        bound = (2e-3 + (2 ** -7 if types[0] == "bf16" else 0.0)) * (mag + want.abs())
+        assert ((out[s:s + 1].double().cpu() - want).abs() <= bound).all(), (s, cap)
+
+
+@pytest.mark.parametrize("types", TYPES, ids="-".join)
+def test_small_values_under_a_cap(types):
+    """Every score at the lower end of the cap, and values of 2^-40: nothing of them is lost."""
+    from tests.ruled import attend, check
+    from tests.seqcache import filled, i32
+    hq, hkv, dh = 4, 2, 128
+    cache, kv = filled([200], hkv, dh, dt(types[1]), 14)
+    k, v = kv[0][0, 0].clone(), kv[0][0, 1] * 2.0 ** -40
+    k[..., 0] = -3000.0
+    j = torch.arange(200, device="cuda")
+    page = cache.page_table[0].long()[j // 16]
+    cache.kv[0, page, 0, :, j % 16] = k.transpose(0, 1).cuda()
+    cache.kv[0, page, 1, :, j % 16] = v.transpose(0, 1).cuda()
+    q = torch.randn(200, hq, dh, generator=torch.Generator().manual_seed(4)).to(dt(types[0])).cuda()
+    q[..., 0] = 12.0
+    for slopes in (None, slopes_of(hq)):
+        out = cache.prompt_attention(0, q, i32([0]), i32([0, 200]), rule=rule_of(55.0, slopes, 0, None, None))
+        want, mag = attend(q, k, v, [(r, 0, 0) for r in range(200)], 55.0, slopes)
+        check(out, want, mag, (types[0], slopes))
