@@ -19,7 +19,7 @@ constexpr float kFixed = -16.0f, kFixedTop = 80.0f;
 // keys far from it would set would take the bits of its score. Rows whose sum stays below kLeastSum are computed again (plain_query).
 constexpr float kLeastOffset = -64.0f, kLeastSum = 0x1p-60f;
 
-constexpr int kTanhTerms = 7;  // of fp32 queries; 4 of bf16 ones
+constexpr int kTanhTerms = 7, kNearTerms = 5;  // of fp32 queries; 4 and 3 of bf16 ones
 
 struct RuleArgs {
   float cap;
@@ -27,8 +27,8 @@ struct RuleArgs {
   const float* slopes;
   const int *first, *open;
   // Of products S up to `limit`, top tanh(S / (top to)) = S (c[0] + y (c[1] + ...)), y = S^2, in units of log2 (scaled_polys); up to
-  // `near` the three of n are enough
-  float limit, c[kTanhTerms], near, n[3];
+  // `near` the fewer of n are enough
+  float limit, c[kTanhTerms], near, n[kNearTerms];
 };
 
 // Keys below `open` and keys of [lo, lim).
@@ -48,12 +48,11 @@ __device__ __forceinline__ int open_of(const RuleArgs& R, int i, int len) {
   return R.open != nullptr ? min(max(R.open[i], 0), max(len, 0)) : 0;
 }
 
-// What some row of `rows` sees: of [lo, lim), and below open. key(r), open(r): of row row0 + r.
+// What some row of `rows` sees: of [lo, lim), and below open. key(r), open(r): of row row0 + r; `open` where all have one.
 template <typename K, typename O>
 __device__ __forceinline__ Sight sight_of_rows(const RuleArgs& R, int row0, int rows, K key, O open) {
   Sight h{0x7fffffff, 0, 0};
-  if (R.first == nullptr && R.window <= 0) h.lo = 0;
-#pragma unroll 8
+#pragma unroll 16
   for (int r = 0; r < rows; r++) {
     const Sight s = sight_of(R, row0 + r, key(r), open(r));
     h.open = max(h.open, s.open);
@@ -62,6 +61,14 @@ __device__ __forceinline__ Sight sight_of_rows(const RuleArgs& R, int row0, int 
     h.lim = max(h.lim, s.lim);
   }
   return h;
+}
+// The same for rows of consecutive keys, the first of which is `key`.
+__device__ __forceinline__ Sight sight_of_run(const RuleArgs& R, int row0, int rows, int key, int open) {
+  if (R.first != nullptr)
+    return sight_of_rows(R, row0, rows, [&](int r) { return key + r; }, [&](int) { return open; });
+  const int from = max(key, 0);  // the first row that sees anything
+  if (key + rows <= from) return Sight{0, 0, 0};
+  return Sight{R.window > 0 ? max(from - R.window + 1, 0) : 0, key + rows, open};
 }
 
 // The keys [a, b) without those that no row sees: keys before `a` or behind `b` are dropped, and a run of them between the open keys

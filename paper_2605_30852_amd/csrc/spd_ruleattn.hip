@@ -22,13 +22,14 @@ __device__ __forceinline__ float tanh_of(float x) {
 
 // tanh(x) / x in powers of x^2, for x from 0 up to `to`, fitted to the least largest error of tanh(x) relative to itself. Three terms,
 // 3.9e-5, and four, 4.0e-5, are enough for probabilities that are rounded to bf16: a score of 10 is off by 4e-4, as p of itself, its
-// rounding by up to 2e-3; seven, 5e-8, are what fp32 holds.
+// rounding by up to 2e-3; five, 3.2e-08, and seven, 5e-8, are what fp32 holds.
 struct Tanh {
   double to;
   int terms;
   double c[7];
 };
 constexpr Tanh kTanh3{0.55, 3, {0.999961253, -0.330998277, 0.111880151}}, kTanh4{0.9, 4, {0.999960199, -0.331725224, 0.122781884, -0.0300411835}},
+    kTanh5{0.55, 5, {0.999999968, -0.33332795, 0.133188769, -0.0525893176, 0.0163154405}},
     kTanh7{1.0, 7, {0.99999995, -0.333328392, 0.133252041, -0.0534570295, 0.0202899804, -0.00620337906, 0.00104102262}};
 
 // The polynomials with the scale of the products S in their coefficients. Caps for which these would leave fp32's range have none (a
@@ -43,7 +44,7 @@ void scaled_polys(RuleArgs& r, int dtype, float scale) {
     return (float)(t.to / k);
   };
   r.limit = take(dtype == SPD_BF16 ? kTanh4 : kTanh7, r.c);
-  if (dtype == SPD_BF16) r.near = take(kTanh3, r.n);
+  r.near = take(dtype == SPD_BF16 ? kTanh3 : kTanh5, r.n);
 }
 
 spd_status check_rule(const char* call, const spd_attention_rule* r) {

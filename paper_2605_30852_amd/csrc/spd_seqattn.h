@@ -288,7 +288,7 @@ __device__ __forceinline__ int size_mode(const PlanArgs& P, int nq) {
 template <typename J>
 __device__ __forceinline__ void narrow_prompt(const RuleArgs& R, J& j, int i, int len) {
   j.open = open_of(R, i, len);
-  const Sight h = sight_of_rows(R, j.row0, j.nrows, [&](int r) { return j.lim0 + r - 1; }, [&](int) { return j.open; });
+  const Sight h = sight_of_run(R, j.row0, j.nrows, j.lim0 - 1, j.open);
   j.b = max(j.b, h.open);
   narrow(j, h);
 }
@@ -327,6 +327,9 @@ __device__ bool prefix_job(const PlanArgsOf<RL>& P, const Batch& B, int t, JobOf
   auto narrowed = [&] {
     if constexpr (RL != 0) {
       j.open = 0;  // each row's own
+      j.gap_at = 0x7fffffff;
+      j.gap = 0;
+      if (P.rule.first == nullptr && P.rule.window <= 0) return;  // all keys are seen
       narrow(j, sight_of_rows(P.rule, j.row0, j.nrows, [&](int r) { return B.len_at(j.row0 + r) - 1; },
                               [&](int r) { return open_of(P.rule, j.row0 + r, B.len_at(j.row0 + r)); }));
     }
@@ -769,7 +772,7 @@ __device__ __forceinline__ float multiple_plus(float a, float n, float b) {
 // A tile's products S of a lane's query become exponents less `off`: top tanh, and less slope times the distance. at(i): the
 // tile's key of product i, from key k of the lane's on; to: from S to units of log2. Where every key's distance counts down to the
 // center and every |S| is within a polynomial's range, which nearly all tiles are, this takes a multiplication and a FMA for each of its
-// terms (3, 4 or 7) a score for the cap and one instruction more for the distance; else the general formula. Scores are done four at a
+// terms (3 or 4 of bf16 queries, 5 or 7 of fp32 ones) a score for the cap and one instruction more for the distance; else the general formula. Scores are done four at a
 // time: all at once would take more registers than there are.
 template <int RL, int TERMS, int W, typename V, int NV, typename At>
 __device__ __forceinline__ void shape_by(V (&s)[NV], const float* c, const RowRule<RL>& rule, float to, float away, float off, At at) {
@@ -816,8 +819,8 @@ __device__ __forceinline__ void shape(V (&s)[NV], const RuleArgs& R, const RowRu
     float far = 0.f;
 #pragma unroll
     for (int i = 0; i < N; i += 2) far = fmaxf(fmaxf(far, fabsf(s[i / W][i % W])), fabsf(s[(i + 1) / W][(i + 1) % W]));
-    if (FEW_BITS && usual && !__any(far > R.near)) {
-      shape_by<RL, 3, W>(s, R.n, rule, to, away, off, at);
+    if (usual && !__any(far > R.near)) {
+      shape_by<RL, FEW_BITS ? 3 : 5, W>(s, R.n, rule, to, away, off, at);
       return;
     }
     usual = usual && !__any(far > R.limit);
@@ -1668,7 +1671,7 @@ __device__ __forceinline__ bool direct_item(const SeqArgsOf<RL>& A, int y, ItemO
     if constexpr (RL != 0) {
       it.open = open_of(A.rule, i, len);
       const bool flat = it.mode & ITEM_FLAT;
-      const Sight h = sight_of_rows(A.rule, it.row0, it.nrows, [&](int r) { return flat ? len - 1 : it.lim0 + r - 1; }, [&](int) { return it.open; });
+      const Sight h = sight_of_run(A.rule, it.row0, it.nrows, flat ? len - 1 : it.lim0 - 1, it.open);
       const Keys k = keys_of(0, max(it.k1, h.open), h);
       it.k0 = k.a;
       it.k1 = k.b;
