@@ -161,7 +161,7 @@ def lib() -> ct.CDLL:
             "spd_prefix_attention_workspace": (I, [C, I, I, I, I, I, Z]),
             "spd_prefix_attention": (I, [C, I, P, L64, P, L64, I, I, P, I, P, P, I, I, P, ct.c_size_t, P]),
             "spd_rope_frequencies": (I, [I, D, ct.POINTER(spd_rope_scaling), ct.POINTER(D)]),
-            "spd_rope_table": (I, [ct.POINTER(D), I, L64, I, D, P, P, P]),
+            "spd_rope_table": (I, [P, I, L64, I, D, P, P, P]),
             "spd_cache_append_heads": (I, [C, I, P, L64, P, L64, P, L64, P, L64, I, I, ct.POINTER(spd_head_rule), P, P, I, P, P, I, I, P]),
             "spd_prompt_attention_ruled_workspace": (I, [C, I, I, I, I, I, Z]),
             "spd_prompt_attention_ruled": (I, [C, I, P, L64, P, L64, I, I, P, P, I, I, I, R, P, ct.c_size_t, P]),
@@ -501,7 +501,7 @@ def spd_rope_frequencies(dims: int, base: float, scaling: Optional[spd_rope_scal
 
 
 def spd_rope_table(freq, pairs: int, first: int, positions: int, amplitude: float, cos: int, sin: int, stream: int) -> None:
-    """freq: a ctypes array or pointer of doubles on the host."""
+    """freq: a ctypes array of doubles, or the address of some, on the host."""
     _check("spd_rope_table", lib().spd_rope_table(freq, pairs, first, positions, amplitude, cos, sin, stream))
 
 

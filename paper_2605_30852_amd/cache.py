@@ -57,12 +57,15 @@ class HeadRule:
                  interleaved: bool = False):
         self.q_gain, self.k_gain, self.eps, self.interleaved = q_gain, k_gain, eps, interleaved
         self._gains = (_optional("q_gain", q_gain, torch.float32), _optional("k_gain", k_gain, torch.float32))
+        self._c = B.spd_head_rule(*self._gains, eps, 0, 1 if interleaved else 0)
 
     def check(self, head_dim: int, gpu: int, rot: int) -> "B.spd_head_rule":
         for name, t in (("q_gain", self.q_gain), ("k_gain", self.k_gain)):
             if t is not None and (t.shape[0] != head_dim or t.get_device() != gpu):
                 raise ValueError(f"the rule's {name} must have {head_dim} entries on the cache's device")
-        return B.spd_head_rule(*self._gains, self.eps, rot, 1 if self.interleaved else 0)
+        if self._c.rot != rot:
+            self._c = B.spd_head_rule(*self._gains, self.eps, rot, 1 if self.interleaved else 0)
+        return self._c
 
 
 class PagedCache:

@@ -64,8 +64,25 @@ __device__ __forceinline__ Sight sight_of_rows(const RuleArgs& R, int row0, int 
 }
 // The same for rows of consecutive keys, the first of which is `key`.
 __device__ __forceinline__ Sight sight_of_run(const RuleArgs& R, int row0, int rows, int key, int open) {
-  if (R.first != nullptr)
-    return sight_of_rows(R, row0, rows, [&](int r) { return key + r; }, [&](int) { return open; });
+  if (R.first != nullptr) {  // four rows a load, all of a tile on the way at once
+    Sight h{0x7fffffff, 0, 0};
+    auto join = [&](int first, int p) {
+      const int lo = max(first, R.window > 0 ? max(p - R.window + 1, 0) : 0);
+      const bool any = p >= 0 && lo <= p;
+      h.lo = any ? min(h.lo, lo) : h.lo;
+      h.lim = any ? p + 1 : h.lim;
+    };
+    int r = 0;
+#pragma unroll 8
+    for (; r + 4 <= rows; r += 4) {
+      int v[4];
+      __builtin_memcpy(v, R.first + row0 + r, sizeof(v));
+      for (int i = 0; i < 4; i++) join(v[i], key + r + i);
+    }
+    for (; r < rows; r++) join(R.first[row0 + r], key + r);
+    if (key + rows > 0) h.open = open;
+    return h;
+  }
   const int from = max(key, 0);  // the first row that sees anything
   if (key + rows <= from) return Sight{0, 0, 0};
   return Sight{R.window > 0 ? max(from - R.window + 1, 0) : 0, key + rows, open};

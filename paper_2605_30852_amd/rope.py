@@ -4,7 +4,6 @@
 Frequencies are few and live on the host; a table is computed on the device's current stream, in one launch."""
 from __future__ import annotations
 
-import ctypes as ct
 from dataclasses import dataclass
 from typing import Optional, Tuple
 
@@ -48,14 +47,25 @@ def rope_table(freq: torch.Tensor, positions: int, first: int = 0, amplitude: fl
     if out is None:
         if positions < 0:
             raise ValueError("positions must not be negative")
-        out = tuple(torch.empty((2, positions, pairs), dtype=torch.float32, device=device)) if positions * pairs % 4 == 0 else \
-            tuple(torch.empty((positions, pairs), dtype=torch.float32, device=device) for _ in range(2))
-    for x in out:
-        if x.dtype is not torch.float32 or x.shape != (positions, pairs) or not x.is_cuda or not x.is_contiguous() or \
-                x.get_device() != out[0].get_device():
-            raise ValueError("out must be two contiguous float32 tensors [positions][pairs] on one GPU")
-    i = out[0].get_device()
-    with torch.cuda.device(i):
-        B.spd_rope_table(ct.cast(freq.data_ptr(), ct.POINTER(ct.c_double)), pairs, first, positions, amplitude, out[0].data_ptr(),
-                         out[1].data_ptr(), torch._C._cuda_getCurrentRawStream(i))
-    return out[0], out[1]
+        cos = torch.empty((positions, pairs), dtype=torch.float32, device=device)
+        sin = torch.empty_like(cos)
+        if not cos.is_cuda:
+            raise ValueError("a table is made on a GPU")
+    else:
+        cos, sin = out
+        for x in out:
+            if x.dtype is not torch.float32 or x.shape != (positions, pairs) or not x.is_cuda or not x.is_contiguous() or \
+                    x.get_device() != cos.get_device():
+                raise ValueError("out must be two contiguous float32 tensors [positions][pairs] on one GPU")
+    i = cos.get_device()
+
+    def call():
+        B.spd_rope_table(freq.data_ptr(), pairs, first, positions, amplitude, cos.data_ptr(), sin.data_ptr(),
+                         torch._C._cuda_getCurrentRawStream(i))
+
+    if torch._C._cuda_getDevice() == i:  # the library launches on the current device
+        call()
+    else:
+        with torch.cuda.device(i):
+            call()
+    return cos, sin

@@ -123,9 +123,9 @@ def test_rope():
     def table(freq=f, pairs=4, first=0, positions=3, amplitude=1.0, cos=16, sin=32):
         B.spd_rope_table(freq, pairs, first, positions, amplitude, cos, sin, 0)
 
-    for bad in (dict(pairs=0), dict(pairs=129), dict(positions=-1), dict(first=(1 << 40) + 1), dict(first=-(1 << 40) - 1),
+    for bad in (dict(pairs=0), dict(pairs=129), dict(positions=-1), dict(first=(1 << 30) + 1), dict(first=-(1 << 30) - 1),
                 dict(amplitude=float("nan")), dict(cos=0), dict(sin=8), dict(freq=None),
-                dict(freq=(ct.c_double * 4)(1.0, float("nan"), 0, 0)), dict(freq=(ct.c_double * 4)(1.0, 0, 0, 2e6))):
+                dict(freq=(ct.c_double * 4)(1.0, float("nan"), 0, 0)), dict(freq=(ct.c_double * 4)(1.0, 0, 0, 1001.0))):
         refused(table, **bad)
     table(positions=0, cos=0, sin=0)  # nothing
 
