@@ -90,11 +90,11 @@ __device__ __forceinline__ Sight sight_of_run(const RuleArgs& R, int row0, int r
 
 // The keys [a, b) without those that no row sees: keys before `a` or behind `b` are dropped, and a run of them between the open keys
 // and the others is a gap. Keys are counted without it: c stands for key c, from gap_at on for key c + gap. gap_at lies whole tiles
-// of 64 keys behind the page of a, and gap is whole pages, so that no tile has keys of both sides.
+// (of `tile` keys) behind the page of a, and gap is whole pages, so that no tile has keys of both sides.
 struct Keys {
   int a, b, gap_at, gap;
 };
-__device__ __forceinline__ Keys keys_of(int a, int b, const Sight& h) {
+__device__ __forceinline__ Keys keys_of(int a, int b, const Sight& h, int tile) {
   Keys k{a, b, 0x7fffffff, 0};
   const int open = min(b, h.open), lo = max(a, h.lo), lim = min(b, h.lim);
   if (lim <= lo) {
@@ -103,7 +103,7 @@ __device__ __forceinline__ Keys keys_of(int a, int b, const Sight& h) {
     k.a = lo;
     k.b = lim;
   } else {
-    const int start = a & ~(kPage - 1), at = start + (open - start + 63) / 64 * 64, to = lo & ~(kPage - 1);
+    const int start = a & ~(kPage - 1), at = start + (open - start + tile - 1) / tile * tile, to = lo & ~(kPage - 1);
     k.b = max(open, lim);
     if (to > at) {
       k.gap_at = at;

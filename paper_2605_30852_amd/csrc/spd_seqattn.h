@@ -177,6 +177,7 @@ __device__ __forceinline__ int key_of(const ItemOf<RL>& it, int k) {
   if constexpr (RL != 0) return k >= it.gap_at ? k + it.gap : k;
   else return k;
 }
+constexpr int kFewKeys = 32, kWideKeys = 64;  // of a tile of a piece of few queries, of others: at most
 enum { ITEM_FEW = 1, ITEM_PAIR = 2, ITEM_FLAT = 4 };  // at most 16 queries; at most 32 (of an fp32 cache); each row attends its sequence's keys
 
 // Rows whose pieces' records are to be joined: those of up to two jobs.
@@ -235,7 +236,7 @@ struct RuledJob : Job {
 template <int RL>
 using JobOf = std::conditional_t<RL != 0, RuledJob, Job>;
 __device__ __forceinline__ void narrow(RuledJob& j, const Sight& h) {
-  const Keys k = keys_of(j.a, j.b, h);
+  const Keys k = keys_of(j.a, j.b, h, j.mode & ITEM_FEW ? kFewKeys : kWideKeys);
   j.a = k.a;
   j.b = k.b;
   j.gap_at = k.gap_at;
@@ -1672,7 +1673,7 @@ __device__ __forceinline__ bool direct_item(const SeqArgsOf<RL>& A, int y, ItemO
       it.open = open_of(A.rule, i, len);
       const bool flat = it.mode & ITEM_FLAT;
       const Sight h = sight_of_run(A.rule, it.row0, it.nrows, flat ? len - 1 : it.lim0 - 1, it.open);
-      const Keys k = keys_of(0, max(it.k1, h.open), h);
+      const Keys k = keys_of(0, max(it.k1, h.open), h, kFewKeys);
       it.k0 = k.a;
       it.k1 = k.b;
       it.gap_at = k.gap_at;
@@ -1852,16 +1853,23 @@ struct Request {
   size_t at_items, at_merges, at_units, at_tiles, at_ml, at_o, bytes;
 };
 
-Request request(const spd_cache& c, int n_q_heads, int nseqs, int rows, int ngroups, int max_len, bool prefix, bool ruled = false) {
+Request request(const spd_cache& c, int n_q_heads, int nseqs, int rows, int ngroups, int max_len, bool prefix, bool ruled = false,
+                int window = 0) {
   Request q{};
   const int hkv = c.n_kv_heads, G = n_q_heads / hkv;
   // Short calls go without a plan, one launch, every piece of at most 16 queries over all its keys: prompts whose tiles are at
   // most two a CU, decode rows (a shared prefix of so few keys is in the L2 for all of a group that the GPU holds at once). Planned and
   // so: 3 fp32 prompts of 21 rows 13.9 and 5.2 us, 4 bf16 prompts of 16 rows behind 300 keys 17.1 and 9.3, decode rows of
   // 300 keys 15.9 and 8.2, 256 of 512 keys 89 and 85. Longer calls need the splits, larger prompts the wide tiles.
-  const bool fits = max_len > 0 && max_len <= 512;
+  // A window bounds a row's keys as a short sequence does (a tile's rows and open keys come on top).
+  const int reach = window > 0 && (max_len == 0 || window < max_len) ? window : max_len;
+  const bool fits = reach > 0 && reach <= 512;
   q.rpt = 16 / G;
   q.direct = fits && (prefix ? nseqs * hkv <= (ngroups > 0 ? 512 : 2048) : ((long long)rows / q.rpt + nseqs) * hkv <= 512);
+  // Decode rows under a window that fill the GPU are as good as equal: 64 of 8 KV heads and up to 1028 keys
+  // take 43 us so, 55 with a plan and its merge. A row with thousands of
+  // open keys beside it, which a plan would split, keeps its workgroup as long as they take.
+  q.direct = q.direct || (window > 0 && prefix && ngroups == 0 && reach <= 2048 && nseqs * hkv >= kWantedWGs);
   if (q.direct) {
     q.jobs = prefix ? nseqs : rows / q.rpt + nseqs;
     return q;

@@ -67,7 +67,7 @@ std::string look(Case& k, long long& pieces, long long& used, long long& keys) {
     if (it.table < 0 || it.table >= k.c.max_seqs) return fault("a piece's sequence", i, it.table);
     const Span s = span_of<RULE_KEYS>(it);
     if (it.k0 < 0 || it.k1 < it.k0 || s.a < 0 || s.b < s.a || s.b > 16 * k.c.max_pages) return fault("a piece's keys", i, s.b);
-    if (it.gap < 0 || it.gap % 16 || (it.gap && (it.gap_at - (it.k0 & ~15)) % 64)) return fault("a tile with keys of both sides", i, it.gap_at);
+    if (it.gap < 0 || it.gap % 16 || (it.gap && (it.gap_at - (it.k0 & ~15)) % (it.mode & ITEM_FEW ? 32 : 64))) return fault("a tile with keys of both sides", i, it.gap_at);
     const int len = std::min(std::max(k.lens[it.table], 0), 16 * k.c.max_pages);
     if (s.b > len) return fault("keys behind the sequence's", i, s.b);
     keys += it.k1 - it.k0;
