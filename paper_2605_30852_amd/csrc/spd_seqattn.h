@@ -177,6 +177,9 @@ __device__ __forceinline__ int key_of(const ItemOf<RL>& it, int k) {
   if constexpr (RL != 0) return k >= it.gap_at ? k + it.gap : k;
   else return k;
 }
+// The page of the first key of the t-th tile of n keys.
+template <int RL>
+__device__ __forceinline__ int page_of(int key, int start, int t, int n) { return RL != 0 ? key / kPage : start / kPage + t * (n / kPage); }
 constexpr int kFewKeys = 32, kWideKeys = 64;  // of a tile of a piece of few queries, of others: at most
 enum { ITEM_FEW = 1, ITEM_PAIR = 2, ITEM_FLAT = 4 };  // at most 16 queries; at most 32 (of an fp32 cache); each row attends its sequence's keys
 
@@ -773,10 +776,20 @@ __device__ __forceinline__ float multiple_plus(float a, float n, float b) {
 // A tile's products S of a lane's query become exponents less `off`: top tanh, and less slope times the distance. at(i): the
 // tile's key of product i, from key k of the lane's on; to: from S to units of log2. Where every key's distance counts down to the
 // center and every |S| is within a polynomial's range, which nearly all tiles are, this takes a multiplication and a FMA for each of its
-// terms (3 or 4 of bf16 queries, 5 or 7 of fp32 ones) a score for the cap and one instruction more for the distance; else the general formula. Scores are done four at a
+// terms (3 or 4 of bf16 queries, 5 or 7 of fp32 ones) a score for the cap and one instruction more for the distance; else the general formula. RAMP: the products came with their keys'
+// distances, ramp[v] from each vector's first key on. Scores are done four at a
 // time: all at once would take more registers than there are.
-template <int RL, int TERMS, int W, typename V, int NV, typename At>
+template <int RL, int TERMS, int W, bool RAMP, typename V, int NV, typename At>
 __device__ __forceinline__ void shape_by(V (&s)[NV], const float* c, const RowRule<RL>& rule, float to, float away, float off, At at) {
+  if constexpr (RAMP) {
+#pragma unroll
+    for (int x = 0; x < NV; x++) {
+      const float base = fmaf(-rule.slope, away - (float)at(x * W), -off);
+#pragma unroll
+      for (int v = 0; v < W; v++) s[x][v] = fmaf(s[x][v], to, base);
+    }
+    return;
+  }
   float base = -off;
   float slope = rule.slope;
   [[maybe_unused]] float step[4];  // slope times 0 .. 3
@@ -810,8 +823,9 @@ __device__ __forceinline__ void shape_by(V (&s)[NV], const float* c, const RowRu
     for (int i = 0; i < 4; i++) s[i0 / W][i0 % W + i] = e[i];
   }
 }
-template <int RL, bool FEW_BITS, int W, typename V, int NV, typename At>
-__device__ __forceinline__ void shape(V (&s)[NV], const RuleArgs& R, const RowRule<RL>& rule, float to, int k, bool one_side, float off, At at) {
+template <int RL, bool FEW_BITS, int W, bool RAMP, typename V, int NV, typename At>
+__device__ __forceinline__ void shape(V (&s)[NV], const RuleArgs& R, const RowRule<RL>& rule, float to, int k, bool one_side, float off,
+                                      const V& ramp, At at) {
   constexpr int N = W * NV;
   const float away = (RL & RULE_SLOPES) != 0 ? (float)(rule.center - k) : 0.f;
   bool usual = true;
@@ -821,17 +835,17 @@ __device__ __forceinline__ void shape(V (&s)[NV], const RuleArgs& R, const RowRu
 #pragma unroll
     for (int i = 0; i < N; i += 2) far = fmaxf(fmaxf(far, fabsf(s[i / W][i % W])), fabsf(s[(i + 1) / W][(i + 1) % W]));
     if (usual && !__any(far > R.near)) {
-      shape_by<RL, FEW_BITS ? 3 : 5, W>(s, R.n, rule, to, away, off, at);
+      shape_by<RL, FEW_BITS ? 3 : 5, W, false>(s, R.n, rule, to, away, off, at);
       return;
     }
     usual = usual && !__any(far > R.limit);
   }
   if (usual) {
-    shape_by<RL, FEW_BITS ? 4 : 7, W>(s, R.c, rule, to, away, off, at);
+    shape_by<RL, FEW_BITS ? 4 : 7, W, RAMP>(s, R.c, rule, to, away, off, at);
   } else {
 #pragma unroll
     for (int i = 0; i < N; i++) {
-      float e = rule.shaped(s[i / W][i % W], to, away - (float)at(i)) - off;
+      float e = rule.shaped(RAMP ? s[i / W][i % W] - ramp[i % W] : s[i / W][i % W], to, away - (float)at(i)) - off;
       asm volatile("" : "+v"(e));
       s[i / W][i % W] = e;
     }
@@ -842,10 +856,10 @@ __device__ __forceinline__ void shape(V (&s)[NV], const RuleArgs& R, const RowRu
 template <typename T, typename KVT, int DH, int RL>
 __device__ void plain_piece(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const Records& R, int g, int j, float* lds) {
   const int r = it.row0 + j / A.G, head = g * A.G + j % A.G, d = 4 * (threadIdx.x % (DH / 4));
-  const RowRule<RL> rule = row_rule<RL>(A, it, r, head);
   const Span keys = span_of<RL>(it);
+  RowRule<RL> rule = row_rule<RL>(A, it, r, head);
   int n = keys.b;
-  if constexpr (RL == 0) n = min(rule.lim, keys.b);
+  if constexpr (RL == 0) rule.lim = n = min(rule.lim, keys.b);
   float a[4] = {0.f, 0.f, 0.f, 0.f}, M = -INFINITY, L = 0.f;
   bool holds = threadIdx.x < DH / 4;
   if (rule.sees_any(keys.a, n))
@@ -959,39 +973,14 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
   const int* table = C.page_table + (size_t)it.table * C.max_pages;
   // The pages of a tile, one a lane (mod their number), are read a tile ahead of their use, and looked at only there: a look
   // at them here would wait for them and for the keys requested before them.
-  auto tile_key = [&](int t) { return key_of<RL>(it, start + t * KT); };
-  auto pages = [&](int t) { return table[min(tile_key(t) / kPage + (lane & (KT / kPage - 1)), last / kPage)]; };
+  // The first key of the t-th tile. Scores that fall with the distance are taken from the last tile down, which has the largest ones:
+  // from the first up, all but flat slopes renew the offset at every tile.
+  auto tile_key = [&](int t) {
+    return key_of<RL>(it, start + ((RL & RULE_SLOPES) != 0 && (RL & RULE_FIXED) == 0 ? max(tiles - 1 - t, 0) : t) * KT);
+  };
+  auto pages = [&](int t) { return table[min(page_of<RL>(tile_key(t), start, t, KT) + (lane & (KT / kPage - 1)), last / kPage)]; };
   const int pg0 = tiles > 0 ? pages(0) : 0;
   int pg = tiles > 0 ? pages(1) : 0;
-  const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;  // from products to scores in units of log2
-  constexpr bool SHAPED = (RL & (RULE_CAP | RULE_SLOPES)) != 0, FIXED = (RL & RULE_FIXED) != 0;
-  // The values of a tile's second half are read, and the next tile requested, behind the first half's probabilities
-  constexpr bool LATE = SB > 1 && (RL & RULE_SLOPES) != 0;
-  const float to = SHAPED ? 1.0f : sc;  // from scores to exponents
-  const bool active = w * 32 < nq;
-  const int jq = w * 32 + col, jj = min(jq, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
-  RowRule<RL> rule = row_rule<RL>(A, it, row, head);
-  const int lim = min(rule.lim, keys.b);
-
-  bf16x8 qf[NP][KS];
-  load_query<T, KS, 16>(qf, (const T*)A.q + row * A.qs + head * DH + h * 8, A.scale * kLog2e);
-  // keys below wmin are attended by every query of the wave, none at wmax and above by any
-  int wmin = it.lim0 + w * 32 / G, wmax = it.lim0 + min(w * 32 + 31, nq - 1) / G;
-  WaveRule<32> seen;
-  if constexpr (RL != 0) {
-    seen.set(rule);
-    seen.join();
-  } else if (it.mode & ITEM_FLAT) {
-    wmin = wmax = lim;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      wmin = min(wmin, __shfl_xor(wmin, d, 64));
-      wmax = max(wmax, __shfl_xor(wmax, d, 64));
-    }
-  }
-  wmin = __builtin_amdgcn_readfirstlane(min(wmin, it.k1));
-  wmax = __builtin_amdgcn_readfirstlane(active ? min(wmax, it.k1) : 0);
-
   // A thread's bytes of a page, load i: chunk lc of key lk, or of keys 16 apart.
   const int lk = tid / NCH, lc = tid % NCH;
   static_assert(kWG / NCH % kPage == 0 && LPT >= 1, "a pass of the workgroup is whole pages");
@@ -1014,8 +1003,50 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
       __builtin_amdgcn_global_load_lds(p + half * sizeof(uint16_t) + (at + voff), l + KBUF, 16, 0, 0);
     }
   };
+  if constexpr (RL != 0) {  // a rule's part of a row takes longer to come by
+    if (tiles > 0) request(0, pg0);
+  }
+  const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;  // from products to scores in units of log2
+  constexpr bool SHAPED = (RL & (RULE_CAP | RULE_SLOPES)) != 0, FIXED = (RL & RULE_FIXED) != 0;
+  // The values of a tile's second half are read, and the next tile requested, behind the first half's probabilities
+  constexpr bool LATE = SB > 1 && (RL & RULE_SLOPES) != 0;
+  // Distances without a cap: the products of a block start at the slope times the keys' distances from its first one (in products'
+  // units), 16 numbers of the lane's that every block has, and come out with them.
+  constexpr bool RAMP = (RL & RULE_SLOPES) != 0 && (RL & RULE_CAP) == 0 && NP == 1;
+  const float to = SHAPED ? 1.0f : sc;  // from scores to exponents
+  const bool active = w * 32 < nq;
+  const int jq = w * 32 + col, jj = min(jq, nq - 1), row = it.row0 + jj / G, head = g * G + jj % G;
+  RowRule<RL> rule = row_rule<RL>(A, it, row, head);
+  const int lim = min(rule.lim, keys.b);
+  if constexpr (RL == 0) rule.lim = lim;
+
+  bf16x8 qf[NP][KS];
+  load_query<T, KS, 16>(qf, (const T*)A.q + row * A.qs + head * DH + h * 8, A.scale * kLog2e);
+  [[maybe_unused]] f32x16 ramp;
+  if constexpr (RAMP) {
+#pragma unroll
+    for (int v = 0; v < 16; v++) ramp[v] = rule.slope / sc * (float)(8 * (v >> 2) + (v & 3));
+  }
+  // keys below wmin are attended by every query of the wave, none at wmax and above by any
+  int wmin = it.lim0 + w * 32 / G, wmax = it.lim0 + min(w * 32 + 31, nq - 1) / G;
+  WaveRule<32> seen;
+  if constexpr (RL != 0) {
+    seen.set(rule);
+    seen.join();
+  } else if (it.mode & ITEM_FLAT) {
+    wmin = wmax = lim;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      wmin = min(wmin, __shfl_xor(wmin, d, 64));
+      wmax = max(wmax, __shfl_xor(wmax, d, 64));
+    }
+  }
+  wmin = __builtin_amdgcn_readfirstlane(min(wmin, it.k1));
+  wmax = __builtin_amdgcn_readfirstlane(active ? min(wmax, it.k1) : 0);
+
   // A lane's bytes of a K or V tile. Chunk 2 k + h differs from chunk h in bits that the row has not: with a cap or distances, which need the
   // registers, one XOR in a step stands for an address in each.
+  constexpr bool XORED = SHAPED || (RL != 0 && NP == 3);
   uint32_t ka[KS], va[NT];
 #pragma unroll
   for (int k = 0; k < KS; k++) ka[k] = col * DH * 2 + (((2 * k + h) ^ (col >> KROT) % NCH) << 4);
@@ -1032,7 +1063,7 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
   float m_run = -INFINITY, l_run = 0.f;
   [[maybe_unused]] float off_run = 0.f, bound = -INFINITY;  // SHAPED: what the exponents are less, and from where on it is renewed
 
-  if (tiles > 0) request(0, pg0);
+  if (RL == 0 && tiles > 0) request(0, pg0);
   for (int t = 0; t < tiles; t++) {
     const char* tile = lds + (t & 1) * 2 * KBUF;
     const int kb = tile_key(t);  // the tile's first key
@@ -1047,9 +1078,9 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
       }
       continue;
     }
-    if constexpr (SHAPED) asm volatile("" : "+v"(ka[0]), "+v"(va[0]));  // the others come from these, in the step
-    auto k_at = [&](int k) { return SHAPED ? ka[0] ^ (uint32_t)(k << 5) : ka[k]; };
-    auto v_at = [&](int tt) { return SHAPED ? va[0] ^ (uint32_t)(tt << 6) : va[tt]; };
+    if constexpr (XORED) asm volatile("" : "+v"(ka[0]), "+v"(va[0]));  // the others come from these, in the step
+    auto k_at = [&](int k) { return XORED ? ka[0] ^ (uint32_t)(k << 5) : ka[k]; };
+    auto v_at = [&](int tt) { return XORED ? va[0] ^ (uint32_t)(tt << 6) : va[tt]; };
     f32x16 s[SB];
 #pragma unroll
     for (int x = 0; x < SB; x++)
@@ -1058,7 +1089,7 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
         const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + k_at(k) + x * 32 * DH * 2);
 #pragma unroll
         for (int p = NP - 1; p >= 0; p--)
-          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[p][k], (p == NP - 1 && k == 0) ? (f32x16)(0.f) : s[x], 0, 0, 0);
+          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[p][k], (p == NP - 1 && k == 0) ? (RAMP ? ramp : (f32x16)(0.f)) : s[x], 0, 0, 0);
       }
     bf16x8 vf[SB][2][NT];
     auto read_values = [&](int x) {
@@ -1097,8 +1128,8 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
     };
     if constexpr (!LATE) next();
     if constexpr (SHAPED) {
-      shape<RL, NP == 1, 16>(s, A.rule, rule, sc, kb + 4 * h, seen.one_side(kb, KT), FIXED ? kFixed : off_run,
-                             [](int i) { return (i >> 4) * 32 + 8 * (i >> 2 & 3) + (i & 3); });
+      shape<RL, NP == 1, 16, RAMP>(s, A.rule, rule, sc, kb + 4 * h, seen.one_side(kb, KT), FIXED ? kFixed : off_run, ramp,
+                                   [](int i) { return (i >> 4) * 32 + 8 * (i >> 2 & 3) + (i & 3); });
     }
     bool part = kb < keys.a || kb + KT > wmin;  // some key is not every query's
     if constexpr (RL != 0) part = kb < keys.a || kb + KT > keys.b || !seen.whole(kb, KT);
@@ -1109,9 +1140,9 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
       for (int x = 0; x < SB; x++)
 #pragma unroll
         for (int v = 0; v < 16; v++) {
-          const int i = x * 32 + 8 * (v >> 2) + (v & 3), kk = kb + i + 4 * h;
+          const int kk = kb + x * 32 + 8 * (v >> 2) + 4 * h + (v & 3);
           if constexpr (RL != 0)
-            s[x][v] = sight.seen(s[x][v], i);
+            s[x][v] = sight.seen(s[x][v], x * 32 + 8 * (v >> 2) + (v & 3));
           else
             s[x][v] = kk < lim && kk >= keys.a ? s[x][v] : -INFINITY;
         }
@@ -1212,8 +1243,9 @@ __device__ void finish_few(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
   __syncthreads();
   for (int i = tid; i < nq * (DH / 4); i += kWG) {
     const int j = i / (DH / 4), d = i % (DH / 4) * 4, r = it.row0 + j / G, hd = g * G + j % G;
-    const RowRule<RL> rule = row_rule<RL>(A, it, r, hd);
     const Span keys = span_of<RL>(it);
+    RowRule<RL> rule = row_rule<RL>(A, it, r, hd);
+    if constexpr (RL == 0) rule.lim = min(rule.lim, keys.b);
     float M = -INFINITY, L = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < NW; x++) M = fmaxf(M, s_ml[x][j].x);
@@ -1229,7 +1261,7 @@ __device__ void finish_few(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
       a[3] = fmaf(v.w, f, a[3]);
     }
     auto finite = [](float x) { return fabsf(x) < INFINITY; };
-    if ((!(L > 0.f) && keys.b > keys.a && rule.sees_any(keys.a, keys.b)) || !(finite(a[0]) && finite(a[1]) && finite(a[2]) && finite(a[3]))) {
+    if ((!(L > 0.f) && rule.sees_any(keys.a, keys.b)) || !(finite(a[0]) && finite(a[1]) && finite(a[2]) && finite(a[3]))) {
       atomicOr(&s_few_bad, 1u << j);
     } else if (it.rec < 0) {
       store4((T*)A.out + r * A.os + hd * DH + d, a, rule.sees_any(0, 0x7fffffff) ? 1.0f / L : 0.f);
@@ -1267,7 +1299,7 @@ __device__ void piece_few(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const Re
   const size_t half = (size_t)C.n_kv_heads * kPage * DH;
   const uint16_t* pool = (const uint16_t*)A.kv + (size_t)g * kPage * DH;
   const int* table = C.page_table + (size_t)it.table * C.max_pages;
-  auto pages = [&](int t) { return table[min(key_of<RL>(it, start + t * KT) / kPage + (lane & 1), last / kPage)]; };
+  auto pages = [&](int t) { return table[min(page_of<RL>(key_of<RL>(it, start + t * KT), start, t, KT) + (lane & 1), last / kPage)]; };
   const int pg0 = w < tiles ? pages(w) : 0;
   int pg = w < tiles ? pages(w + NW) : 0;
   const float sc = NP == 1 ? A.scale * kLog2e : 1.0f, to = (RL & (RULE_CAP | RULE_SLOPES)) != 0 ? 1.0f : sc;
@@ -1417,7 +1449,7 @@ __device__ void piece_few_f32(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, cons
   const size_t half = (size_t)C.n_kv_heads * kPage * DH;
   const float* pool = (const float*)A.kv + (size_t)g * kPage * DH;
   const int* table = C.page_table + (size_t)it.table * C.max_pages;
-  auto page_at = [&](int t) { return table[min(key_of<RL>(it, start + t * KT) / kPage, last / kPage)]; };
+  auto page_at = [&](int t) { return table[min(page_of<RL>(key_of<RL>(it, start + t * KT), start, t, KT), last / kPage)]; };
   const int pg0 = w < tiles ? page_at(w) : 0;
   int pg = w < tiles ? page_at(w + NW) : 0;
   RowRule<RL> rule[QS];
@@ -1574,7 +1606,7 @@ __device__ void piece_f32(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const Re
       qf[s] = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
     }
   }
-  auto pages = [&](int t) { return table[min(key_of<RL>(it, start + t * KT) / kPage + (lane & 1), last / kPage)]; };
+  auto pages = [&](int t) { return table[min(page_of<RL>(key_of<RL>(it, start + t * KT), start, t, KT) + (lane & 1), last / kPage)]; };
   auto issue = [&](int buf, int t, int pg) {
 #pragma unroll
     for (int i = 0; i < LPT; i++) {
