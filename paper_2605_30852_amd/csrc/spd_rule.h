@@ -117,6 +117,9 @@ __device__ __forceinline__ Keys keys_of(int a, int b, const Sight& h, int tile) 
 // tanh(x), as spd_ruleattn.hip computes it.
 template <int RL>
 __device__ float tanh_of(float x);
+// 1 / x, within a unit in the last place
+template <int RL>
+__device__ float reciprocal(float x);
 
 // A row's part of a rule, of one head. In units of log2: a score s becomes top tanh(s to_x) - slope |center - key|. The distance
 // is measured from the nearest key that the row sees (its own one, or the last open one): the softmax is the same, and rows that

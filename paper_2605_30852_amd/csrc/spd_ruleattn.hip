@@ -4,6 +4,9 @@
 namespace spd {
 namespace {
 
+template <int RL>
+__device__ __forceinline__ float reciprocal(float x) { return __builtin_amdgcn_rcpf(x); }
+
 // tanh to 2^-22 of itself: below kTanhPoly a polynomial of x^2 (fitted to the least largest relative error, 9e-10; above it 1 - 2 / (1 +
 // e^2x) loses at most a bit.
 constexpr float kTanhPoly = 0.55f;
@@ -16,7 +19,7 @@ __device__ __forceinline__ float tanh_of(float x) {
   p = fmaf(y, p, 0.13332586f);
   p = fmaf(y, p, -0.333333164f);
   const float small = fmaf(x * y, p, x), t = __builtin_amdgcn_exp2f(fabsf(x) * 2.88539008177792681f);
-  const float big = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + t), 1.0f);
+  const float big = fmaf(-2.0f, reciprocal<RL>(1.0f + t), 1.0f);
   return fabsf(x) < kTanhPoly ? small : copysignf(big, x);
 }
 

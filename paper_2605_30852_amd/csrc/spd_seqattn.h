@@ -842,6 +842,15 @@ __device__ __forceinline__ void shape(V (&s)[NV], const RuleArgs& R, const RowRu
   }
   if (usual) {
     shape_by<RL, FEW_BITS ? 4 : 7, W, RAMP>(s, R.c, rule, to, away, off, at);
+  } else if ((RL & RULE_CAP) != 0 && FEW_BITS && R.limit > 0.f) {  // top - 2 top / (1 + e^2x): off by 2^-23 of top, at most 738, is little
+    const float twice = 2.0f * kLog2e * to * rule.to_x;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      float e = fmaf(-2.0f * rule.top, reciprocal<RL>(1.0f + __builtin_amdgcn_exp2f(s[i / W][i % W] * twice)), rule.top - off);
+      if constexpr ((RL & RULE_SLOPES) != 0) e = fmaf(-rule.slope, fabsf(away - (float)at(i)), e);
+      asm volatile("" : "+v"(e));
+      s[i / W][i % W] = e;
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < N; i++) {
@@ -1009,7 +1018,7 @@ __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const R
   const float sc = NP == 1 ? A.scale * kLog2e : 1.0f;  // from products to scores in units of log2
   constexpr bool SHAPED = (RL & (RULE_CAP | RULE_SLOPES)) != 0, FIXED = (RL & RULE_FIXED) != 0;
   // The values of a tile's second half are read, and the next tile requested, behind the first half's probabilities
-  constexpr bool LATE = SB > 1 && (RL & RULE_SLOPES) != 0;
+  constexpr bool LATE = SB > 1 && SHAPED;
   // Distances without a cap: the products of a block start at the slope times the keys' distances from its first one (in products'
   // units), 16 numbers of the lane's that every block has, and come out with them.
   constexpr bool RAMP = (RL & RULE_SLOPES) != 0 && (RL & RULE_CAP) == 0 && NP == 1;

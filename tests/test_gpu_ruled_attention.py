@@ -433,3 +433,84 @@ def test_small_values_under_a_cap(types):
         out = cache.prompt_attention(0, q, i32([0]), i32([0, 200]), rule=rule_of(55.0, slopes, 0, None, None))
         want, mag = attend(q, k, v, [(r, 0, 0) for r in range(200)], 55.0, slopes)
         check(out, want, mag, (types[0], slopes))
+
+
+@pytest.mark.parametrize("types", TYPES, ids="-".join)
+def test_open_lengths_and_first_keys_out_of_range(types):
+    """A sequence's open keys are at most its own, none below 0; first keys below 0 are the first."""
+    from tests.ruled import attend, check
+    from tests.seqcache import filled, i32
+    hq, hkv, dh = 8, 2, 64
+    cache, kv = filled([90, 40], hkv, dh, dt(types[1]), 15)
+    q = (1.5 * torch.randn(70, hq, dh, generator=torch.Generator().manual_seed(6))).to(dt(types[0])).cuda()
+    for opened in ([1 << 30, -7], [-1 << 31, (1 << 31) - 1]):
+        first = [-5 - i for i in range(70)]
+        for max_len in (0, 90):
+            out = cache.prompt_attention(0, q, i32([0, 1]), i32([0, 30, 70]), max_len=max_len, rule=rule_of(7.0, None, 9, first, opened))
+            for i, (a, b, n) in enumerate(((0, 30, 90), (30, 70, 40))):
+                want, mag = attend(q[a:b], kv[i][0, 0], kv[i][0, 1], [(n - (b - r), 0, min(max(opened[i], 0), n)) for r in range(a, b)], 7.0, None, 9)
+                check(out[a:b], want, mag, (types[0], opened, i))
+
+
+@pytest.mark.parametrize("types", TYPES, ids="-".join)
+def test_many_decode_rows_under_a_window(types):
+    """As many rows as fill the GPU go without a plan, whatever their lengths and open keys."""
+    from tests.ruled import attend, check
+    from tests.seqcache import filled, i32
+    hq, hkv, dh = 8, 8, 64
+    rng = random.Random(8)
+    lens = [rng.choice([0, 1, 15, 700, 701, 1500, rng.randint(1, 1900)]) for _ in range(66)]
+    opened = [rng.choice([0, 1, 4, 33, n]) for n in lens]
+    cache, kv = filled(lens, hkv, dh, dt(types[1]), 16)
+    q = (1.5 * torch.randn(66, hq, dh, generator=torch.Generator().manual_seed(6))).to(dt(types[0])).cuda()
+    slopes = slopes_of(hq)
+    for max_len in (0, 1900):
+        seqs = list(range(66))
+        seqs[5] = 66  # none
+        out = torch.full_like(q, 7.0)
+        cache.prefix_attention(0, q, i32(seqs), out=out, max_len=max_len, rule=rule_of(7.0, slopes, 700, None, opened))
+        for s in range(66):
+            if s == 5:
+                assert (out[s] == 7.0).all()
+                continue
+            want, mag = attend(q[s:s + 1], kv[s][0, 0], kv[s][0, 1], [(lens[s] - 1, 0, opened[s])], 7.0, slopes, 700)
+            check(out[s:s + 1], want, mag, (types[0], s))
+
+
+@pytest.mark.parametrize("types", TYPES, ids="-".join)
+@pytest.mark.parametrize("cap", [0.0, 7.0])
+def test_scores_that_rise_with_the_distance(types, cap):
+    """Slopes below 0: the farthest keys count most."""
+    from tests.ruled import attend, check
+    from tests.seqcache import filled, i32
+    hq, hkv, dh = 4, 2, 128
+    cache, kv = filled([900], hkv, dh, dt(types[1]), 17)
+    q = (1.5 * torch.randn(200, hq, dh, generator=torch.Generator().manual_seed(6))).to(dt(types[0])).cuda()
+    slopes = [-0.01, -0.002, 0.0, -0.02]
+    out = cache.prompt_attention(0, q, i32([0]), i32([0, 200]), rule=rule_of(cap, slopes, 0, None, None))
+    rows = list(range(0, 200, 7))
+    want, mag = attend(q[rows], kv[0][0, 0], kv[0][0, 1], [(700 + r, 0, 0) for r in rows], cap, slopes)
+    check(out[rows], want, mag, (types[0], cap))
+
+
+@pytest.mark.parametrize("types", TYPES, ids="-".join)
+def test_a_large_pool(types):
+    """Pages whose bytes lie past 2^32 of the pool."""
+    from paper_2605_30852_amd.cache import AttentionRule, PagedCache
+    from tests.ruled import attend, check
+    from tests.seqcache import i32
+    hkv, dh, item = 8, 128, 2 if types[1] == "bf16" else 4
+    page = 2 * hkv * 16 * dh * item
+    num = (1 << 32) // page + 40
+    cache = PagedCache.empty(1, num, hkv, dh, 1, 32, dtype=dt(types[1]))
+    ids = [num - 1 - 2 * i for i in range(13)]
+    cache.page_table[0, :13] = i32(ids)
+    cache.lens[0] = 200
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn(13, 2, hkv, 16, dh, generator=g).to(dt(types[1]))
+    cache.kv[0, ids] = x.cuda()
+    k, v = (x[:, i].transpose(0, 1).flatten(1, 2)[:, :200] for i in range(2))
+    q = (1.5 * torch.randn(40, 16, dh, generator=g)).to(dt(types[0])).cuda()
+    out = cache.prompt_attention(0, q, i32([0]), i32([0, 40]), rule=AttentionRule(cap=7.0, window=90))
+    want, mag = attend(q[::5], k, v, [(160 + r, 0, 0) for r in range(0, 40, 5)], 7.0, None, 90)
+    check(out[::5], want, mag, (types[0],))
