@@ -527,7 +527,7 @@ spd_status spd_cache_append_heads(const spd_cache* c, int32_t layer, const void*
 typedef struct spd_attention_rule {
   float cap;                /* 0: scores as they are; otherwise in [2^-20, 2^20] */
   int32_t window;           /* 0: none */
-  const float* slopes;      /* device fp32 [n_q_heads], finite; NULL: none */
+  const float* slopes;      /* device fp32 [n_q_heads], finite (below 0: right, but slower); NULL: none */
   const int32_t* first;     /* device int32 [rows], a row's first key (of its document); NULL: 0 */
   const int32_t* open_lens; /* device int32 [nseqs]; NULL: 0 */
 } spd_attention_rule;

@@ -1,4 +1,5 @@
-// Attention over a cache of several sequences under a rule (spd_rule.h): its calls.
+// Attention over a cache of several sequences under a rule (spd_rule.h): its calls. The kernels are spd_seqattn.h's, one for each set of
+// a rule's parts: keys alone, a cap, distances, both, and both with a cap too high for one offset.
 #include "spd_seqattn.h"
 
 namespace spd {

@@ -963,6 +963,10 @@ __device__ void finish_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const 
 // rows 135 us, 720 TFLOP/s, 40% of the cycles in the matrix cores: a piece costs some 6 us beside its steps (item, pages, first
 // keys, output), which workgroups that stay and take piece after piece did not shorten (149 us where the others took 143). fp32
 // queries, 2048 rows: 110 us, 312 TFLOP/s of the scores and outputs, three times that in products, 57% of the cycles.
+// Under a rule (RL) the same steps, with the scores shaped between the products; bf16 rows of 32 heads of 128 over 8: 8192 causal rows
+// 570 us without a rule, 585 with keys alone (RULE_KEYS), 615 capped at 50, 640 lowered with the distance, 645 both; capped at 20, where
+// some tiles leave the polynomials, 650, at 5, where all do, 680. 16381 capped rows 2.42 ms, 909 TFLOP/s. What a tile has more than without a
+// rule is vector work: 16 instructions for the largest |S|, three or four a score for the cap.
 template <typename T, int DH, int RL>
 __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const Records R, int g, char* lds) {
   constexpr int NP = sizeof(T) == 4 ? 3 : 1;
