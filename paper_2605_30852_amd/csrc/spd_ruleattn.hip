@@ -110,7 +110,7 @@ extern "C" spd_status spd_prompt_attention_ruled(const spd_cache* c, int32_t lay
   SeqArgs a = args_of(c, layer, q, q_stride, out, out_stride, n_q_heads, seqs, nseqs);
   a.cu = cu_rows;
   a.rows = rows;
-  run_ruled(a, *rule, dtype, request(*c, n_q_heads, nseqs, rows, 0, max_len, false, true, rule->window), false, workspace, (hipStream_t)stream);
+  run_ruled(a, *rule, dtype, request(*c, n_q_heads, nseqs, rows, 0, max_len, false, true, rule->window, rule->open_lens != nullptr), false, workspace, (hipStream_t)stream);
   return check_launch(call);
 }
 
@@ -145,6 +145,6 @@ extern "C" spd_status spd_prefix_attention_ruled(const spd_cache* c, int32_t lay
   a.prefix = prefix_lens;
   a.ngroups = ngroups;
   a.rows = nseqs;
-  run_ruled(a, *rule, dtype, request(*c, n_q_heads, nseqs, nseqs, ngroups, max_len, true, true, rule->window), true, workspace, (hipStream_t)stream);
+  run_ruled(a, *rule, dtype, request(*c, n_q_heads, nseqs, nseqs, ngroups, max_len, true, true, rule->window, rule->open_lens != nullptr), true, workspace, (hipStream_t)stream);
   return check_launch(call);
 }

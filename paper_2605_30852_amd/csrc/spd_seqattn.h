@@ -1899,16 +1899,16 @@ struct Request {
 };
 
 Request request(const spd_cache& c, int n_q_heads, int nseqs, int rows, int ngroups, int max_len, bool prefix, bool ruled = false,
-                int window = 0) {
+                int window = 0, bool open = false) {
   Request q{};
   const int hkv = c.n_kv_heads, G = n_q_heads / hkv;
   // Short calls go without a plan, one launch, every piece of at most 16 queries over all its keys: prompts whose tiles are at
   // most two a CU, decode rows (a shared prefix of so few keys is in the L2 for all of a group that the GPU holds at once). Planned and
   // so: 3 fp32 prompts of 21 rows 13.9 and 5.2 us, 4 bf16 prompts of 16 rows behind 300 keys 17.1 and 9.3, decode rows of
   // 300 keys 15.9 and 8.2, 256 of 512 keys 89 and 85. Longer calls need the splits, larger prompts the wide tiles.
-  // A window bounds a row's keys as a short sequence does (a tile's rows and open keys come on top).
-  const int reach = window > 0 && (max_len == 0 || window < max_len) ? window : max_len;
-  const bool fits = reach > 0 && reach <= 512;
+  // A window bounds a row's keys as a short sequence does (a tile's rows come on top), unless some may be open beside it.
+  const int reach = window > 0 && (max_len == 0 || window < max_len) ? window : max_len, keys = open ? max_len : reach;
+  const bool fits = keys > 0 && keys <= 512;
   q.rpt = 16 / G;
   q.direct = fits && (prefix ? nseqs * hkv <= (ngroups > 0 ? 512 : 2048) : ((long long)rows / q.rpt + nseqs) * hkv <= 512);
   // Decode rows under a window that fill the GPU are as good as equal: 64 of 8 KV heads and up to 1028 keys
