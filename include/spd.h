@@ -503,7 +503,7 @@ spd_status spd_rope_table(const double* freq, int32_t pairs, int64_t first, int3
                           float* cosines, float* sines, void* stream);
 
 /* What spd_cache_append_heads makes of the heads of q and k. gains: device fp32 [head_dim], 16-byte aligned; a head x
- * becomes x / sqrt(mean(x^2) + eps) * gain, in fp32 (NULL: as it is). Then its first `rot` dims (a multiple of 16) turn: dims i and i +
+ * becomes x / sqrt(mean(x^2) + eps) * gain, in fp32 (NULL: as it is; q_gain only where q is given). Then its first `rot` dims (a multiple of 16) turn: dims i and i +
  * rot / 2, or (interleaved) 2i and 2i + 1, by cos and sin [rope_positions][rot / 2] at the row's position. */
 typedef struct spd_head_rule {
   const float* q_gain;

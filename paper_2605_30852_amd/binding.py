@@ -494,7 +494,7 @@ def spd_cache_append_heads(cache: spd_cache, layer: int, k: int, k_stride: int, 
 
 def spd_rope_frequencies(dims: int, base: float, scaling: Optional[spd_rope_scaling] = None) -> "ct.Array":
     """dims / 2 doubles, a ctypes array."""
-    out = (ct.c_double * max(1, dims // 2))()
+    out = (ct.c_double * max(1, min(dims, 256) // 2))()  # 256: what the call takes
     _check("spd_rope_frequencies",
            lib().spd_rope_frequencies(dims, base, ct.byref(scaling) if scaling is not None else None, out))
     return out

@@ -8,10 +8,10 @@ namespace spd {
 namespace {
 
 // Parts of a rule that a kernel is made for: keys unseen (all rules), capped scores, scores lowered with the distance; caps low
-// enough for one offset of the exponents.
-// That offset, kFixed: the nearest key that a row sees has a distance of 0 (RowRule), and so the largest of its exponents lies in [-top,
-// top] (slopes below 0 may raise others past it; sums that leave fp32's range are made again by plain_query). With top of at most kFixedTop no running maximum is needed: probabilities, 2^-64 to 2^96, have sums over 2^20 keys below 2^116,
-// and of keys that the distance lowers below fp32's range none counts beside 2^-64.
+// enough for one offset of the exponents, kFixed. The nearest key that a row sees has a distance of 0 (RowRule), and so the largest of
+// its exponents lies in [-top, top]. With top of at most kFixedTop no running maximum is needed: probabilities, 2^-64 to 2^96, have sums
+// over 2^20 keys below 2^116, and of keys that the distance lowers below fp32's range none counts beside 2^-64. (Slopes below 0 may raise
+// others past top: sums that leave fp32's range are made again by plain_query.)
 enum { RULE_KEYS = 1, RULE_CAP = 2, RULE_SLOPES = 4, RULE_FIXED = 8 };
 constexpr float kFixed = -16.0f, kFixedTop = 80.0f;
 

@@ -8,7 +8,7 @@ namespace {
 template <int RL>
 __device__ __forceinline__ float reciprocal(float x) { return __builtin_amdgcn_rcpf(x); }
 
-// tanh to 2^-22 of itself: below kTanhPoly a polynomial of x^2 (fitted to the least largest relative error, 9e-10; above it 1 - 2 / (1 +
+// tanh to 2^-22 of itself: below kTanhPoly a polynomial of x^2, fitted to the least largest relative error, 1e-9; above it 1 - 2 / (1 +
 // e^2x) loses at most a bit.
 constexpr float kTanhPoly = 0.55f;
 template <int RL>
@@ -26,7 +26,7 @@ __device__ __forceinline__ float tanh_of(float x) {
 
 // tanh(x) / x in powers of x^2, for x from 0 up to `to`, fitted to the least largest error of tanh(x) relative to itself. Three terms,
 // 3.9e-5, and four, 4.0e-5, are enough for probabilities that are rounded to bf16: a score of 10 is off by 4e-4, as p of itself, its
-// rounding by up to 2e-3; five, 3.2e-08, and seven, 5e-8, are what fp32 holds.
+// rounding by up to 2e-3; five, 3e-8, and seven, 5e-8, are what fp32 holds.
 struct Tanh {
   double to;
   int terms;

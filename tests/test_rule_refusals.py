@@ -113,7 +113,7 @@ def test_rope():
                 continue
             for got, want in zip(B.spd_rope_frequencies(dims, base, s), frequencies(dims, base, *ref)):
                 assert abs(got - want) <= 1e-13 * want  # two ways to a power, some roundings of 2^-53 times log(base)
-    for bad in ((3, 1e4, None), (0, 1e4, None), (258, 1e4, None), (64, 1.0, None), (64, float("inf"), None), (64, float("nan"), None),
+    for bad in ((3, 1e4, None), (0, 1e4, None), (258, 1e4, None), (1 << 30, 1e4, None), (-2, 1e4, None), (64, 1.0, None), (64, float("inf"), None), (64, float("nan"), None),
                 (64, 1e4, S(4, 0, 2.0, 0, 0)), (64, 1e4, S(-1, 0, 2.0, 0, 0)), (64, 1e4, S(1, 0, 0.0, 0, 0)), (64, 1e4, S(1, 0, float("nan"), 0, 0)),
                 (2, 1e4, S(2, 0, 2.0, 0, 0)), (64, 1e4, S(3, 0, 2.0, 1.0, 4.0)), (64, 1e4, S(3, 9, 2.0, 4.0, 4.0)),
                 (64, 1e4, S(3, 9, 2.0, 1.0, float("inf")))):
