@@ -133,3 +133,34 @@ def test_pages_that_are_none_and_sequences_that_are_none():
     assert changed > 0
     pages = (torch.nan_to_num(cache.kv, nan=9.0) != torch.nan_to_num(before, nan=9.0)).flatten(2).any(-1)[0]
     assert set(pages.nonzero().flatten().tolist()) <= {int(cache.page_table[0, 0]), int(cache.page_table[1, 0])}
+
+
+def test_in_a_graph():
+    """A captured call follows the lengths and the rows on replay, with eager calls in between."""
+    from paper_2605_30852_amd.cache import HeadRule
+    from tests.seqcache import PAGE, filled, i32
+    cache, _ = filled([100, 60], 2, 64, torch.bfloat16, 21)
+    other, _ = filled([100, 60], 2, 64, torch.bfloat16, 21)
+    g = torch.Generator().manual_seed(2)
+    x = torch.randn(5, 8, 64, generator=g).bfloat16().cuda()
+    rope = tuple(torch.randn(PAGE * cache.max_pages, 16, generator=g).cuda() for _ in range(2))
+    rule = HeadRule(q_gain=torch.rand(64, generator=g).cuda(), k_gain=torch.rand(64, generator=g).cuda())
+    seqs, cu = i32([1, 0]), i32([0, 2, 5])
+
+    def call(c):
+        return c.append_heads(0, x[:, 4:6], x[:, 6:], seqs, cu, rule, q=x[:, :4], rope=rope)
+
+    call(cache), call(other)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call(cache)
+    for k in range(4):
+        x.copy_(torch.randn(5, 8, 64, generator=g))
+        for c in (cache, other):
+            c.lens.copy_(i32([100 - 9 * k, 60 - 7 * k]))
+        graph.replay()
+        want = call(other)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        assert torch.equal(torch.nan_to_num(cache.kv, nan=9.0), torch.nan_to_num(other.kv, nan=9.0)), k
