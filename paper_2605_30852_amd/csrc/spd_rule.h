@@ -11,9 +11,10 @@ namespace {
 // enough for one offset of the exponents, kFixed. The nearest key that a row sees has a distance of 0 (RowRule), and so the largest of
 // its exponents lies in [-top, top]. With top of at most kFixedTop no running maximum is needed: probabilities, 2^-64 to 2^96, have sums
 // over 2^20 keys below 2^116, and of keys that the distance lowers below fp32's range none counts beside 2^-64. (Slopes below 0 may raise
-// others past top: sums that leave fp32's range are made again by plain_query.)
+// others past top: a piece whose sum reaches kMostSum, behind which its reciprocal is no normal number, is made again by
+// plain_query, with its own maximum.)
 enum { RULE_KEYS = 1, RULE_CAP = 2, RULE_SLOPES = 4, RULE_FIXED = 8 };
-constexpr float kFixed = -16.0f, kFixedTop = 80.0f;
+constexpr float kFixed = -16.0f, kFixedTop = 80.0f, kMostSum = 0x1p126f;
 
 // Without a cap the offset starts at the maximum of the first tile, but not below this: a row's nearest key decides, and the offsets that
 // keys far from it would set would take the bits of its score. Rows whose sum stays below kLeastSum are computed again (plain_query).

@@ -884,11 +884,12 @@ __device__ void plain_piece(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const 
   }
 }
 
-// Whether the sum of a row that sees some key has to be made again. Scores that fall with the distance leave little or nothing of a
+// Whether the sum of a row that sees some key has to be made again. Under one offset scores that rise with the distance may sum to more
+// than fp32 holds while outputs of mixed signs stay finite. Scores that fall with the distance leave little or nothing of a
 // piece of far keys: that is seen by the merge, which has all of them (whole: the piece is all of the row's).
 template <int RL>
 __device__ __forceinline__ bool small_sum(float l, bool whole) {
-  if constexpr ((RL & RULE_FIXED) != 0) return !(l >= 0.f);
+  if constexpr ((RL & RULE_FIXED) != 0) return !(l >= 0.f && l < kMostSum);
   else if constexpr ((RL & RULE_SLOPES) != 0) return !(l >= (whole ? kLeastSum : 0.f));
   else return !(l > 0.f);
 }
@@ -918,6 +919,15 @@ __device__ void finish_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const 
     if (mine) {
       const size_t at = (size_t)max(it.rec, 0) + (size_t)g * nq + jq;
       const float inv = rule.sees_any(0, 0x7fffffff) ? 1.0f / l_run : 0.f;
+      // Records under one offset: a large sum comes to [1, 2), its power of two to m, where the merge compares it with other records. Beside one
+      // that plain_query made, of exponents past 100, 2^(kFixed - m) would be 0 and what counts here with it.
+      float lower = 1.0f;
+      if constexpr ((RL & RULE_FIXED) != 0) {
+        const int up = max((int)(__float_as_uint(l_run) >> 23) - 127, 0);
+        lower = ldexpf(1.0f, -up);
+        m_run += (float)up;
+        if (it.rec >= 0) l_run *= lower;
+      }
 #pragma unroll
       for (int tt = 0; tt < NT; tt++)
 #pragma unroll
@@ -927,7 +937,7 @@ __device__ void finish_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const 
           if (it.rec < 0)
             store4((T*)A.out + row * A.os + head * DH + d, x, inv);
           else
-            store4(R.o + at * DH + d, x, 1.0f);
+            store4(R.o + at * DH + d, x, lower);
         }
       if (it.rec >= 0 && h == 0) R.ml[at] = make_float2(m_run, l_run);
     }
