@@ -523,7 +523,9 @@ spd_status spd_cache_append_heads(const spd_cache* c, int32_t layer, const void*
 /* A rule for the attention of other decoders' layers. Of its sequence's keys, the row of key p sees the first
  * open_lens[i] (of batch sequence i, at most its length; also those behind p), and those of [max(first[row], p - window + 1), p].
  * A row that sees nothing, or would stand for a key before the first, gets zeros; keys unseen count nothing, whatever they hold. A
- * score s (scaled) becomes cap * tanh(s / cap), then slopes[head] * |p - key| is taken from it. */
+ * score s (scaled by 1 / sqrt(head_dim)) becomes cap * tanh(s / cap), then slopes[head] * |p - key| is taken from it. fp32 queries: the
+ * tanh to some 2^-22 of itself. bf16 queries: to 4e-5 of itself for caps up to 55 (a probability moves by at most 1.6e-3 of itself, its
+ * rounding to bf16 by 3.9e-3), to 3.4e-4 of a score's unit for caps up to 512, above that as for fp32 queries. */
 typedef struct spd_attention_rule {
   float cap;                /* 0: scores as they are; otherwise in [2^-20, 2^20] */
   int32_t window;           /* 0: none */

@@ -28,7 +28,7 @@ struct RuleArgs {
   const float* slopes;
   const int *first, *open;
   // Of products S up to `limit`, top tanh(S / (top to)) = S (c[0] + y (c[1] + ...)), y = S^2, in units of log2 (scaled_polys); up to
-  // `near` the fewer of n are enough
+  // `near` the fewer of n are enough. limit 0: the exponential formula alone; below 0: neither
   float limit, c[kTanhTerms], near, n[kNearTerms];
 };
 

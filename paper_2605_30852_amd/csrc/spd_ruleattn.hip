@@ -25,8 +25,10 @@ __device__ __forceinline__ float tanh_of(float x) {
 }
 
 // tanh(x) / x in powers of x^2, for x from 0 up to `to`, fitted to the least largest error of tanh(x) relative to itself. Three terms,
-// 3.9e-5, and four, 4.0e-5, are enough for probabilities that are rounded to bf16: a score of 10 is off by 4e-4, as p of itself, its
-// rounding by up to 2e-3; five, 3e-8, and seven, 5e-8, are what fp32 holds.
+// 3.9e-5, and four, 4.0e-5, are enough for probabilities that are rounded to bf16, of caps up to 55: the largest score that they take, 0.72 of
+// the cap, is off by 1.6e-3, as p of itself, its rounding by up to 3.9e-3. It does not cancel in the softmax, where tiles of other
+// ranges have other formulas: at a cap of 512 equal scores would differ by 1.5e-2, so higher caps of bf16 queries take the exponential
+// formula, which is off by 3.4e-4 there. Five terms, 3e-8, and seven, 5e-8, are what fp32 holds.
 struct Tanh {
   double to;
   int terms;
@@ -36,11 +38,18 @@ constexpr Tanh kTanh3{0.55, 3, {0.999961253, -0.330998277, 0.111880151}}, kTanh4
     kTanh5{0.55, 5, {0.999999968, -0.33332795, 0.133188769, -0.0525893176, 0.0163154405}},
     kTanh7{1.0, 7, {0.99999995, -0.333328392, 0.133252041, -0.0534570295, 0.0202899804, -0.00620337906, 0.00104102262}};
 
+// Whether the exponents of scores under a cap lie in a range that one offset serves.
+bool one_offset(float cap) { return cap * kLog2e <= kFixedTop; }
+
 // The polynomials with the scale of the products S in their coefficients. Caps for which these would leave fp32's range have none (a
 // limit of -1): their scores take the other formula.
 void scaled_polys(RuleArgs& r, int dtype, float scale) {
   r.limit = r.near = -1.f;
   if (!(r.cap >= 0x1p-6f && r.cap <= 0x1p9f)) return;
+  if (dtype == SPD_BF16 && !one_offset(r.cap)) {
+    r.limit = 0.f;
+    return;
+  }
   const double top = (double)r.cap * kLog2e, k = dtype == SPD_BF16 ? (double)scale / r.cap : 1.0 / top;  // x = S k
   auto take = [&](const Tanh& t, float* c) {
     double power = k * top;
@@ -68,7 +77,7 @@ void run_ruled(const SeqArgs& plain, const spd_attention_rule& r, int dtype, con
   if (r.cap == 0.f)
     r.slopes ? run_attention<RULE_KEYS | RULE_SLOPES>(a, dtype, q, prefix, workspace, s)
              : run_attention<RULE_KEYS>(a, dtype, q, prefix, workspace, s);
-  else if (r.cap * kLog2e > kFixedTop)
+  else if (!one_offset(r.cap))
     run_attention<CAP | RULE_SLOPES>(a, dtype, q, prefix, workspace, s);
   else
     r.slopes ? run_attention<CAP | RULE_SLOPES | RULE_FIXED>(a, dtype, q, prefix, workspace, s)

@@ -830,7 +830,9 @@ __device__ __forceinline__ void shape(V (&s)[NV], const RuleArgs& R, const RowRu
   const float away = (RL & RULE_SLOPES) != 0 ? (float)(rule.center - k) : 0.f;
   bool usual = true;
   if constexpr ((RL & RULE_SLOPES) != 0) usual = one_side;
-  if constexpr ((RL & RULE_CAP) != 0) {
+  if constexpr ((RL & RULE_CAP) != 0 && FEW_BITS && (RL & RULE_FIXED) == 0) {
+    usual = false;  // a cap too high for their polynomials
+  } else if constexpr ((RL & RULE_CAP) != 0) {
     float far = 0.f;
 #pragma unroll
     for (int i = 0; i < N; i += 2) far = fmaxf(fmaxf(far, fabsf(s[i / W][i % W])), fabsf(s[(i + 1) / W][(i + 1) % W]));
@@ -842,7 +844,7 @@ __device__ __forceinline__ void shape(V (&s)[NV], const RuleArgs& R, const RowRu
   }
   if (usual) {
     shape_by<RL, FEW_BITS ? 4 : 7, W, RAMP>(s, R.c, rule, to, away, off, at);
-  } else if ((RL & RULE_CAP) != 0 && FEW_BITS && R.limit > 0.f) {  // top - 2 top / (1 + e^2x): off by 2^-23 of top, at most 738, is little
+  } else if ((RL & RULE_CAP) != 0 && FEW_BITS && R.limit >= 0.f) {  // top - 2 top / (1 + e^2x): off by some 2^-22 of top, at most 738
     const float twice = 2.0f * kLog2e * to * rule.to_x;
 #pragma unroll
     for (int i = 0; i < N; i++) {
