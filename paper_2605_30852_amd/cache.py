@@ -17,11 +17,14 @@ _FORK_WORKSPACE = 256
 _DTYPES = {torch.float32: B.SPD_F32, torch.bfloat16: B.SPD_BF16}
 
 
-def _optional(name: str, t: Optional[torch.Tensor], dtype: torch.dtype) -> int:
+def _optional(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, size: Optional[int] = None, gpu: Optional[int] = None) -> int:
+    """A rule's tensor, of any size on any GPU where a call has not said which."""
     if t is None:
         return 0
     if t.dtype is not dtype or t.dim() != 1 or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of one dimension on a GPU")
+    if size is not None and (t.shape[0] != size or t.get_device() != gpu):
+        raise ValueError(f"the rule's {name} must have {size} entries on the cache's device")
     return t.data_ptr()
 
 
@@ -30,23 +33,24 @@ class AttentionRule:
     (batch sequence i; also those behind p), and the keys of [max(first[row], p - window + 1), p]: `first` gives each row the
     first key of its document (one behind p: a padding row), window 0 is none. cap: a score s becomes cap tanh(s / cap), 0: not.
     slopes: fp32 [heads], slopes[head] |p - key| is taken from it. Index tensors are int32; the tensors stay the caller's and are
-    read by every call under the rule."""
+    read by every call under the rule; attributes may be set anew between calls."""
 
     def __init__(self, cap: float = 0.0, slopes: Optional[torch.Tensor] = None, window: int = 0,
                  first: Optional[torch.Tensor] = None, open_lens: Optional[torch.Tensor] = None):
         self.cap, self.window, self.slopes, self.first, self.open_lens = cap, window, slopes, first, open_lens
+        self.check()
+
+    def check(self, rows: Optional[int] = None, seqs: Optional[int] = None, heads: Optional[int] = None,
+              gpu: Optional[int] = None) -> "B.spd_attention_rule":
+        """What a call of so many rows, sequences and heads passes on: the attributes as they are now."""
+        cap, window = self.cap, self.window
         if not (cap == 0 or 2.0 ** -20 <= cap <= 2.0 ** 20):
             raise ValueError("cap must be 0 or in [2^-20, 2^20]")
         if not 0 <= window < 1 << 31:
             raise ValueError("window must be in [0, 2^31)")
-        self.c = B.spd_attention_rule(cap, window, _optional("slopes", slopes, torch.float32), _optional("first", first, torch.int32),
-                                      _optional("open_lens", open_lens, torch.int32))
-
-    def check(self, rows: int, seqs: int, heads: int, gpu: int) -> "B.spd_attention_rule":
-        for name, t, n in (("slopes", self.slopes, heads), ("first", self.first, rows), ("open_lens", self.open_lens, seqs)):
-            if t is not None and (t.shape[0] != n or t.get_device() != gpu):
-                raise ValueError(f"the rule's {name} must have {n} entries on the cache's device")
-        return self.c
+        return B.spd_attention_rule(cap, window, _optional("slopes", self.slopes, torch.float32, heads, gpu),
+                                    _optional("first", self.first, torch.int32, rows, gpu),
+                                    _optional("open_lens", self.open_lens, torch.int32, seqs, gpu))
 
 
 class HeadRule:
@@ -56,16 +60,13 @@ class HeadRule:
     def __init__(self, q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
                  interleaved: bool = False):
         self.q_gain, self.k_gain, self.eps, self.interleaved = q_gain, k_gain, eps, interleaved
-        self._gains = (_optional("q_gain", q_gain, torch.float32), _optional("k_gain", k_gain, torch.float32))
-        self._c = B.spd_head_rule(*self._gains, eps, 0, 1 if interleaved else 0)
+        self.check()
 
-    def check(self, head_dim: int, gpu: int, rot: int) -> "B.spd_head_rule":
-        for name, t in (("q_gain", self.q_gain), ("k_gain", self.k_gain)):
-            if t is not None and (t.shape[0] != head_dim or t.get_device() != gpu):
-                raise ValueError(f"the rule's {name} must have {head_dim} entries on the cache's device")
-        if self._c.rot != rot:
-            self._c = B.spd_head_rule(*self._gains, self.eps, rot, 1 if self.interleaved else 0)
-        return self._c
+    def check(self, head_dim: Optional[int] = None, gpu: Optional[int] = None, rot: int = 0) -> "B.spd_head_rule":
+        """What a call with heads of head_dim passes on, rot dims of which turn: the attributes as they are now."""
+        return B.spd_head_rule(_optional("q_gain", self.q_gain, torch.float32, head_dim, gpu),
+                               _optional("k_gain", self.k_gain, torch.float32, head_dim, gpu), self.eps, rot,
+                               1 if self.interleaved else 0)
 
 
 class PagedCache:
