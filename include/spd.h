@@ -493,7 +493,7 @@ typedef struct spd_rope_scaling {
 } spd_rope_scaling;
 
 /* The frequencies in double precision. dims even, in [2, 256] (BASE: at least 4); base finite and above 1; scaling NULL:
- * PLAIN; freq: host [dims / 2]. Host-only. */
+ * PLAIN; freq: host [dims / 2]. A scaling that leaves double precision's range (its base or a frequency) is refused. Host-only. */
 spd_status spd_rope_frequencies(int32_t dims, double base, const spd_rope_scaling* scaling, double* freq);
 
 /* Rows first .. first + positions - 1 of a rotary table: amplitude * cos and sin of position * freq[i], the angle reduced exactly

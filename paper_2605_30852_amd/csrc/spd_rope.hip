@@ -99,6 +99,7 @@ extern "C" spd_status spd_rope_frequencies(int32_t dims, double base, const spd_
       return invalid(call, "low must be below high, both finite");
   }
   if (kind == SPD_ROPE_BASE) base *= std::pow(f, (double)dims / (dims - 2));
+  if (!std::isnormal(base)) return invalid(call, "the changed base is no normal number");  // subnormal ones have fewer bits
   for (int i = 0; i < dims / 2; i++) {
     double t = std::pow(base, -2.0 * i / dims);
     if (kind == SPD_ROPE_LINEAR) t /= f;
@@ -107,6 +108,7 @@ extern "C" spd_status spd_rope_frequencies(int32_t dims, double base, const spd_
       const double part = std::min(1.0, std::max(0.0, (turns - scaling->low) / (scaling->high - scaling->low)));
       t = (1.0 - part) * t / f + part * t;
     }
+    if (!std::isfinite(t)) return invalid(call, "a frequency is not finite");
     freq[i] = t;
   }
   return SPD_OK;
