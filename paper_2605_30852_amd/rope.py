@@ -18,7 +18,8 @@ _KINDS = {"linear": B.SPD_ROPE_LINEAR, "ntk": B.SPD_ROPE_BASE, "parts": B.SPD_RO
 class RopeScaling:
     """kind "linear": all frequencies / factor; "ntk": the base grows with factor, so that the highest frequency stays and the
     lowest is divided by it; "parts": frequencies that turn `low` times or less over the original context are divided by
-    factor, those that turn `high` times or more stay, with a linear passage between them."""
+    factor, those that turn `high` times or more stay, with a passage between them that is linear in the turns. (Where a
+    checkpoint's passage is linear in the pair's index, its frequencies are the caller's to compute: `rope_table` takes any.)"""
 
     kind: str
     factor: float
@@ -33,7 +34,11 @@ def rope_frequencies(dims: int, base: float, scaling: Optional[RopeScaling] = No
     if scaling is not None:
         if scaling.kind not in _KINDS:
             raise ValueError(f"scaling must be one of {sorted(_KINDS)}")
+        if not 0 <= scaling.original < 1 << 31:  # ctypes would cut it to 32 bits
+            raise ValueError("original must be in [0, 2^31)")
         s = B.spd_rope_scaling(_KINDS[scaling.kind], scaling.original, scaling.factor, scaling.low, scaling.high)
+    if not 0 <= dims < 1 << 31:
+        raise ValueError("dims must be in [0, 2^31)")
     return torch.frombuffer(B.spd_rope_frequencies(dims, base, s), dtype=torch.float64)
 
 
@@ -43,10 +48,12 @@ def rope_table(freq: torch.Tensor, positions: int, first: int = 0, amplitude: fl
     tensors on `device`. Angles are those of the frequencies in 64 bits, at any position; each value is rounded once."""
     if freq.dtype is not torch.float64 or freq.dim() != 1 or freq.is_cuda or not freq.is_contiguous():
         raise ValueError("freq must be a contiguous float64 tensor of one dimension on the host")
+    if not 0 <= positions < 1 << 31:
+        raise ValueError("positions must not be negative, nor 2^31 or more")
+    if abs(first) > 1 << 30:
+        raise ValueError("first must lie within 2^30 of 0")
     pairs = freq.shape[0]
     if out is None:
-        if positions < 0:
-            raise ValueError("positions must not be negative")
         cos = torch.empty((positions, pairs), dtype=torch.float32, device=device)
         sin = torch.empty_like(cos)
         if not cos.is_cuda:

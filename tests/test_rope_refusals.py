@@ -12,3 +12,20 @@ from tests.test_cache_refusals import refused
 def test_scalings_that_leave_the_range(kind, factor, base):
     """Their frequencies came out as 0 or as infinities."""
     refused(B.spd_rope_frequencies, 64, base, B.spd_rope_scaling(kind, 4096, factor, 1.0, 32.0))
+
+
+def test_numbers_of_more_bits_than_the_call_takes():
+    """ctypes cuts them without a word: 2^32 + 64 dims were 64 with as many zeros behind them."""
+    torch = pytest.importorskip("torch")
+    from paper_2605_30852_amd.rope import RopeScaling, rope_frequencies, rope_table
+    freq = rope_frequencies(64, 1e4)
+    for dims in ((1 << 32) + 64, -(1 << 32) + 64):
+        with pytest.raises(ValueError, match="dims"):
+            rope_frequencies(dims, 1e4)
+    with pytest.raises(ValueError, match="original"):
+        rope_frequencies(64, 1e4, RopeScaling("parts", 4.0, original=(1 << 32) + 4096))
+    with pytest.raises(ValueError, match="positions"):
+        rope_table(freq, (1 << 32) + 5, out=(torch.empty(0), torch.empty(0)))
+    for first in (1 << 64, -(1 << 64), (1 << 30) + 1):
+        with pytest.raises(ValueError, match="first"):
+            rope_table(freq, 5, first=first, out=(torch.empty(0), torch.empty(0)))
