@@ -498,7 +498,7 @@ spd_status spd_rope_frequencies(int32_t dims, double base, const spd_rope_scalin
 
 /* Rows first .. first + positions - 1 of a rotary table: amplitude * cos and sin of position * freq[i], the angle reduced exactly
  * and both rounded once to fp32. freq: host [pairs], pairs in [1, 128], each of at most 1000 (radians a position), read during the call;
- * first within 2^30 of 0. cosines, sines: device fp32 [positions][pairs], 16-byte aligned. Asynchronous on stream (a hipStream_t). */
+ * first within 2^30 of 0. cosines, sines: device fp32 [positions][pairs], 16-byte aligned, apart from each other. Asynchronous on stream (a hipStream_t). */
 spd_status spd_rope_table(const double* freq, int32_t pairs, int64_t first, int32_t positions, double amplitude,
                           float* cosines, float* sines, void* stream);
 

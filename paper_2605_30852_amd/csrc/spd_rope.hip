@@ -129,6 +129,9 @@ extern "C" spd_status spd_rope_table(const double* freq, int32_t pairs, int64_t 
   }
   if (positions == 0) return SPD_OK;
   if (!cosines || !sines || misaligned(cosines, 16) || misaligned(sines, 16)) return invalid(call, "NULL or misaligned pointer");
+  const size_t bytes = (size_t)positions * pairs * sizeof(float);
+  if ((uintptr_t)cosines < (uintptr_t)sines + bytes && (uintptr_t)sines < (uintptr_t)cosines + bytes)
+    return invalid(call, "cosines and sines overlap");
   const bool fours = pairs % 4 == 0;
   const int rows = kWG / (fours ? pairs / 4 : pairs);
   const dim3 grid(std::min((positions - 1) / rows + 1, kTableWGs));

@@ -29,3 +29,12 @@ def test_numbers_of_more_bits_than_the_call_takes():
     for first in (1 << 64, -(1 << 64), (1 << 30) + 1):
         with pytest.raises(ValueError, match="first"):
             rope_table(freq, 5, first=first, out=(torch.empty(0), torch.empty(0)))
+
+
+@pytest.mark.parametrize("cos, sin", [(1 << 20, 1 << 20), (1 << 20, (1 << 20) + 16), ((1 << 20) + 32, 1 << 20)])
+def test_tables_that_overlap(cos, sin):
+    """Each would hold some of the other's values. (Addresses that the call would launch with: no GPU is here, and that is an error of
+    another kind.)"""
+    with pytest.raises(B.SPDError) as e:
+        B.spd_rope_table((ct.c_double * 4)(1.0, 0.5, 0.1, 0.0), 4, 0, 3, 1.0, cos, sin, 0)
+    assert e.value.status == B.SPD_E_INVAL
