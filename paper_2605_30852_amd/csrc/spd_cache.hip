@@ -543,17 +543,17 @@ __global__ __launch_bounds__(kWG) void k_append_heads(spd_cache c, HeadArgs A) {
 #pragma unroll
       for (int e = 0; e < 8; e++) ss = fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
       ss = lanes_sum<UPH>(ss);
-      float f;
-      if (ss < INFINITY) {
-        f = 1.0f / sqrtf(ss * (1.0f / DH) + A.eps);
-      } else {  // squares past fp32's range: the same of rows 2^-70 as large, of which eps is nothing
+      const float mean = ss * (1.0f / DH) + A.eps;
+      float f = 1.0f / sqrtf(mean);
+      if (!(mean > 0x1p-100f && mean < INFINITY)) {  // past fp32's range, or where squares are no normal numbers: the same, scaled
+        const float by = mean > 1.0f ? 0x1p-70f : 0x1p60f;
         ss = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-          const float y = a[e] * 0x1p-70f, z = b[e] * 0x1p-70f;
+          const float y = a[e] * by, z = b[e] * by;
           ss = fmaf(y, y, fmaf(z, z, ss));
         }
-        f = 0x1p-70f / sqrtf(lanes_sum<UPH>(ss) * (1.0f / DH));
+        f = by / sqrtf(lanes_sum<UPH>(ss) * (1.0f / DH) + A.eps * by * by);
       }
       float ga[8], gb[8];
       load8(gain + da, ga);
