@@ -12,9 +12,10 @@ namespace {
 // its exponents lies in [-top, top]. With top of at most kFixedTop no running maximum is needed: probabilities, 2^-64 to 2^96, have sums
 // over 2^20 keys below 2^116, and of keys that the distance lowers below fp32's range none counts beside 2^-64. (Slopes below 0 may raise
 // others past top: a piece whose sum reaches kMostSum, behind which its reciprocal is no normal number, is made again by
-// plain_query, with its own maximum.)
+// plain_query, with its own maximum.) A slope of kSteepest leaves nothing of any key but the nearest, 2^(2 top - 512) of it,
+// and so steeper ones are taken as it: in sums of their multiples the nearest key's exponent would be lost.
 enum { RULE_KEYS = 1, RULE_CAP = 2, RULE_SLOPES = 4, RULE_FIXED = 8 };
-constexpr float kFixed = -16.0f, kFixedTop = 80.0f, kMostSum = 0x1p126f;
+constexpr float kFixed = -16.0f, kFixedTop = 80.0f, kMostSum = 0x1p126f, kSteepest = 512.0f;
 
 // Without a cap the offset starts at the maximum of the first tile, but not below this: a row's nearest key decides, and the offsets that
 // keys far from it would set would take the bits of its score. Rows whose sum stays below kLeastSum are computed again (plain_query).

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <type_traits>
 
@@ -677,6 +678,8 @@ __device__ __forceinline__ RowRule<RL> rule_of(const SeqArgsOf<RL>& A, int row, 
   x.top = A.rule.cap * kLog2e;
   x.to_x = 1.0f / x.top;
   x.slope = (RL & RULE_SLOPES) != 0 && A.rule.slopes != nullptr ? A.rule.slopes[head] * kLog2e : 0.f;
+  if (fabsf(x.slope) > FLT_MAX) x.slope = copysignf(FLT_MAX, x.slope);  // of slopes up to FLT_MAX: times a distance of 0 it is 0
+  if constexpr ((RL & RULE_FIXED) != 0) x.slope = x.slope > kSteepest ? kSteepest : x.slope;
   return x;
 }
 template <int RL>
