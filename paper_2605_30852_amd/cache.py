@@ -28,7 +28,21 @@ def _optional(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, size: Op
     return t.data_ptr()
 
 
-class AttentionRule:
+class _Rule:
+    """Attributes that may be set anew between calls, and the structs made of them that calls pass on: none outlives a change of an
+    attribute, a struct is never written again, and one made beside a change goes into the dict that the change has replaced."""
+
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        self.__dict__["_made"] = {}
+
+
+def _lies(t: Optional[torch.Tensor], at: Optional[int], size: Optional[int], gpu: Optional[int]) -> bool:
+    """Whether a rule's tensor, of so many entries on this GPU, still lies where the struct says."""
+    return t is None or (t.data_ptr() == at and t.shape[0] == size and t.get_device() == gpu)
+
+
+class AttentionRule(_Rule):
     """A rule for `prompt_attention` and `prefix_attention`. The row of key p sees the first open_lens[i] keys of its sequence
     (batch sequence i; also those behind p), and the keys of [max(first[row], p - window + 1), p]: `first` gives each row the
     first key of its document (one behind p: a padding row), window 0 is none. cap: a score s becomes cap tanh(s / cap), 0: not.
@@ -43,17 +57,23 @@ class AttentionRule:
     def check(self, rows: Optional[int] = None, seqs: Optional[int] = None, heads: Optional[int] = None,
               gpu: Optional[int] = None) -> "B.spd_attention_rule":
         """What a call of so many rows, sequences and heads passes on: the attributes as they are now."""
+        made = self._made
+        c = made.get(0)
+        slopes, first, opened = self.slopes, self.first, self.open_lens
+        if c is not None and _lies(slopes, c.slopes, heads, gpu) and _lies(first, c.first, rows, gpu) and _lies(opened, c.open_lens, seqs, gpu):
+            return c
         cap, window = self.cap, self.window
         if not (cap == 0 or 2.0 ** -20 <= cap <= 2.0 ** 20):
             raise ValueError("cap must be 0 or in [2^-20, 2^20]")
         if not 0 <= window < 1 << 31:
             raise ValueError("window must be in [0, 2^31)")
-        return B.spd_attention_rule(cap, window, _optional("slopes", self.slopes, torch.float32, heads, gpu),
-                                    _optional("first", self.first, torch.int32, rows, gpu),
-                                    _optional("open_lens", self.open_lens, torch.int32, seqs, gpu))
+        c = made[0] = B.spd_attention_rule(cap, window, _optional("slopes", slopes, torch.float32, heads, gpu),
+                                           _optional("first", first, torch.int32, rows, gpu),
+                                           _optional("open_lens", opened, torch.int32, seqs, gpu))
+        return c
 
 
-class HeadRule:
+class HeadRule(_Rule):
     """What `append_heads` makes of the heads of q and k: x / sqrt(mean(x^2) + eps) * gain (fp32 [head_dim]; None: as it is), then
     the rotation of its first dims, in half layout (dims i and i + half of them) or interleaved (2i and 2i + 1)."""
 
@@ -64,9 +84,14 @@ class HeadRule:
 
     def check(self, head_dim: Optional[int] = None, gpu: Optional[int] = None, rot: int = 0) -> "B.spd_head_rule":
         """What a call with heads of head_dim passes on, rot dims of which turn: the attributes as they are now."""
-        return B.spd_head_rule(_optional("q_gain", self.q_gain, torch.float32, head_dim, gpu),
-                               _optional("k_gain", self.k_gain, torch.float32, head_dim, gpu), self.eps, rot,
-                               1 if self.interleaved else 0)
+        made = self._made
+        c = made.get(rot)
+        q_gain, k_gain = self.q_gain, self.k_gain
+        if c is None or not (_lies(q_gain, c.q_gain, head_dim, gpu) and _lies(k_gain, c.k_gain, head_dim, gpu)):
+            c = made[rot] = B.spd_head_rule(_optional("q_gain", q_gain, torch.float32, head_dim, gpu),
+                                            _optional("k_gain", k_gain, torch.float32, head_dim, gpu), self.eps, rot,
+                                            1 if self.interleaved else 0)
+        return c
 
 
 class PagedCache:
