@@ -40,7 +40,8 @@ __device__ __forceinline__ void cos_sin(double u, double& c, double& s) {
 // A thread has V pairs of every n-th position. The angle is the position times the frequency in quarter turns: its product, with the
 // error that an FMA gives, loses its whole quarters exactly (1.5 2^52 leaves them in the sum's low bits), and what is left is right for
 // any position. Both values are rounded once, from 64 bits. Some 20 fp64 instructions a pair take as long as its 8 bytes to memory:
-// 131072 positions of 64 pairs, 67 MB, 15.6 us, 4.3 TB/s (a copy reaches 5.1).
+// 131072 positions of 64 pairs, 67 MB, 15.4 us a launch into buffers in turn, 4.4 TB/s (a copy reaches 5.1), 13.7 into the same ones,
+// which the last-level cache holds in part.
 template <int V>
 __global__ __launch_bounds__(kWG) void k_rope_table(Turns T, int pairs, long long first, int positions, double amplitude, float* cosines,
                                                     float* sines) {

@@ -980,7 +980,7 @@ __device__ void finish_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const 
 // queries, 2048 rows: 110 us, 312 TFLOP/s of the scores and outputs, three times that in products, 57% of the cycles.
 // Under a rule (RL) the same steps, with the scores shaped between the products; bf16 rows of 32 heads of 128 over 8: 8192 causal rows
 // 570 us without a rule, 585 with keys alone (RULE_KEYS), 615 capped at 50, 640 lowered with the distance, 645 both; capped at 20, where
-// some tiles leave the polynomials, 650, at 5, where all do, 680. 16381 capped rows 2.42 ms, 909 TFLOP/s. What a tile has more than without a
+// some tiles leave the polynomials, 650, at 5, where all do, 680; at 60, above the polynomials' caps, 722. 16381 capped rows 2.42 ms, 909 TFLOP/s. What a tile has more than without a
 // rule is vector work: 16 instructions for the largest |S|, three or four a score for the cap.
 template <typename T, int DH, int RL>
 __device__ void piece_wide(const SeqArgsOf<RL>& A, const ItemOf<RL>& it, const Records R, int g, char* lds) {
@@ -1926,9 +1926,11 @@ Request request(const spd_cache& c, int n_q_heads, int nseqs, int rows, int ngro
   const bool fits = keys > 0 && keys <= 512;
   q.rpt = 16 / G;
   q.direct = fits && (prefix ? nseqs * hkv <= (ngroups > 0 ? 512 : 2048) : ((long long)rows / q.rpt + nseqs) * hkv <= 512);
-  // Decode rows under a window that fill the GPU are as good as equal: 64 of 8 KV heads and up to 1028 keys
-  // take 43 us so, 55 with a plan and its merge. A row with thousands of
-  // open keys beside it, which a plan would split, keeps its workgroup as long as they take.
+  // Decode rows under a window that fill the GPU are as good as equal, and the plan and its merge are what they spare: with 8 KV heads
+  // 64 rows of a window of 256, 1024 and 2048 keys take 13.9, 43.8 and 82.5 us so and 21.3, 51.2 and 90.0 with a plan, 65 rows (eight
+  // workgroups behind two full ones a CU) 18.1, 51.9 and 99.1 and 25.8, 59.9 and 107, 256 rows 49.0, 162 and 315 and 57.3, 169 and 323. Open
+  // keys beside the window, whose numbers the host does not know, are a row's workgroup's own: with 2000 of them in one row of 64 the
+  // call takes 61 us for 66, with 8000 112 for 68, with 8000 in all rows 345 for 353.
   q.direct = q.direct || (window > 0 && prefix && ngroups == 0 && reach <= 2048 && nseqs * hkv >= kWantedWGs);
   if (q.direct) {
     q.jobs = prefix ? nseqs : rows / q.rpt + nseqs;
